@@ -44,7 +44,7 @@ extern "C" {
 typedef enum fq_status {
     FQ_OK = 0,
     FQ_ERR_NULL = -1,          /* a required pointer is NULL */
-    FQ_ERR_DTYPE = -2,         /* dtype is not FQ_F16 / FQ_F32 */
+    FQ_ERR_DTYPE = -2,         /* dtype (or kind of state) is none that the field takes */
     FQ_ERR_SHAPE = -3,         /* negative extent, element/slab/block count overflow, bad n or mode */
     FQ_ERR_QRANGE = -4,        /* need qmin <= 0 <= qmax, qmin < qmax, |q| <= 32768; int8 codes need [-128,127] */
     FQ_ERR_ALIGN = -5,         /* pointer not aligned to its element size (workspace: 256 bytes) */
@@ -52,11 +52,17 @@ typedef enum fq_status {
     FQ_ERR_SCALE_PARAMS = -7,  /* need finite eps, 0 < s_min <= s_max, no NaN */
     FQ_ERR_LAUNCH = -8,        /* the HIP runtime reported an error while enqueuing */
     FQ_ERR_ALIAS = -9,         /* output partially overlaps its input (exact in-place is allowed; q may not
-                                  overlap x or y at all) */
-    FQ_ERR_OPTIMIZER = -10     /* bad fq_adam: step < 1, beta outside [0,1), lr/eps not finite or eps < 0 */
+                                  overlap x or y at all; nothing that fq_adamw or fq_linear writes may overlap
+                                  anything else of the same tensor or call) */
+    FQ_ERR_OPTIMIZER = -10     /* bad fq_adam or fq_adamw: step < 1, beta outside [0,1), lr/eps not finite or eps < 0;
+                                  bad fq_param: lr_scale or weight_decay not finite */
 } fq_status;
 
-typedef enum fq_dtype { FQ_F16 = 0, FQ_F32 = 1 } fq_dtype;
+typedef enum fq_dtype {
+    FQ_F16 = 0,
+    FQ_F32 = 1,
+    FQ_I8 = 2                  /* integer codes: the x of fq_linear only */
+} fq_dtype;
 
 enum {
     /* Backward: do not write gx.  For tensors whose values are frozen and only the
@@ -290,6 +296,96 @@ fq_status fq_distill_loss(const fq_distill *d, void *workspace, size_t ws_bytes,
  * the loss.  Same results bit for bit, of use to nobody but a test of that way.
  */
 fq_status fq_distill_loss_no_poll(const fq_distill *d, void *workspace, size_t ws_bytes, void *hip_stream);
+
+/*
+ * One AdamW step over a list of tensors, in one launch: the weights, biases and scale parameters that a fake-quantized
+ * network trains with (Loshchilov & Hutter 2019, Algorithm 2).  Per element, in binary32, each operation rounded on its
+ * own, with g = grad * *grad_scale:
+ *   m <- beta1*m + (1-beta1)*g;   v <- beta2*v + ((1-beta2)*g)*g;   r = sqrt(v)
+ *   p <- p*(1 - lr*weight_decay) - (lr/(1-beta1^step)) * (m / (r/sqrt(1-beta2^step) + eps)),   lr = lr * lr_scale
+ * (root and quotient of the last line to 2 units in the last place; they go into p, and into the codes of r, alone).
+ * An element whose new v is not finite (a gradient that is NaN or infinite, or whose (1-beta2)*g*g overflows) keeps m, v and p; so a
+ * grad_scale of NaN or infinity leaves the whole list as it is.  The constants are evaluated in binary64 on the host and
+ * rounded to binary32 once each.
+ *
+ * States.  FQ_STATE_F32: m and v are floats.  FQ_STATE_F8: a quarter of that.  Elements 256*b to 256*b+255 of a tensor
+ * share a scale each for m and for r = sqrt(v): m = m8 * m_scale[b], v = (v8 * v_scale[b])^2, where m8 and v8 are OCP
+ * e4m3 codes (torch.float8_e4m3fn) and the scales powers of two, the least 2^e of e >= -126 (v: -63) with which no
+ * code of the block is over 448.  Codes are rounded stochastically: with 16 random bits u of the element's own the
+ * magnitude's 23-bit fraction below the last code bit is raised by (u + 1/2) / 2^16 of a code step and cut off.  (Rounding
+ * to nearest would stop the averages: with beta2 = 0.999 a step changes r by 0.05 %, a code step is 6 to 12 %.)  A v that
+ * is not zero does not round to zero.  The bits (lower 16 for m, upper 16 for v) are a hash of the element's place c, 256 times
+ * the number of blocks of the tensors before its own in the list plus its index, under a key of seed and step; all
+ * products modulo 2^32 (k: 2^64), >> shifting in zeros:
+ *   k = seed*0x9E3779B97F4A7C15 + step*0xD1B54A32D192ED03;  k = (k ^ (k >> 32)) * 0x9E3779B97F4A7C15;  key = k >> 32
+ *   x = c*0x9E3779B1 + key;  x = (x ^ (x >> 16))*0x6A09E667;  x = (x ^ (x >> 15))*0xBB67AE85;  x = x ^ (x >> 16)
+ * So a step is reproducible bit for bit.  A fresh state is all zeros: codes, scales and floats.
+ */
+typedef enum fq_state { FQ_STATE_F32 = 0, FQ_STATE_F8 = 1 } fq_state;
+
+/* One tensor of the list.  Host struct; the pointers inside are device pointers. */
+typedef struct fq_param {
+    int64_t n;                        /* elements, contiguous; may be 0 */
+    int32_t p_dtype, g_dtype;         /* FQ_F16 or FQ_F32 each (an FP16 p is rounded to nearest once per step) */
+    int32_t state;                    /* fq_state */
+    float lr_scale, weight_decay;     /* finite; 1 and 0 for nothing special */
+    void *p;                          /* in/out */
+    const void *g;                    /* in */
+    void *p16;                        /* out, optional, with p_dtype FQ_F32: the new p in FP16 */
+    void *m, *v;                      /* in/out: n floats, or n e4m3 codes */
+    float *m_scale, *v_scale;         /* in/out: (n + 255) / 256 floats; FQ_STATE_F8 only */
+} fq_param;
+
+/* What changes from step to step.  Host struct. */
+typedef struct fq_adamw {
+    double lr, beta1, beta2, eps;     /* finite; 0 <= beta < 1, eps >= 0 */
+    int64_t step;                     /* t >= 1: this is the t-th update */
+    uint64_t seed;                    /* of the stochastic rounding; the same in every step */
+    const float *grad_scale;          /* device pointer, optional: one float, e.g. 1 / loss scale times a clipping factor */
+} fq_adamw;
+
+/*
+ * The list is prepared once: fq_adamw_create checks it, copies a table to `workspace` (fq_adamw_workspace_bytes of it,
+ * not initialised by the caller) on `stream` and returns a plan; see fq_plan_create for what holds of the copy, of the
+ * tensors' and the workspace's addresses, and of order.  fq_adamw_step enqueues one kernel and nothing else; under
+ * graph capture it may be captured, and every replay then repeats the step number it was given.  Different tensors'
+ * memory must not overlap (not checked).
+ */
+typedef struct fq_adamw_plan fq_adamw_plan;
+size_t fq_adamw_workspace_bytes(const fq_param *ps, int n);      /* 0 if the list does not validate; host only */
+fq_status fq_adamw_create(const fq_param *ps, int n, void *workspace, size_t ws_bytes, void *hip_stream,
+                          fq_adamw_plan **plan);
+fq_status fq_adamw_step(const fq_adamw_plan *plan, const fq_adamw *h, void *hip_stream);
+void fq_adamw_destroy(fq_adamw_plan *plan);
+
+/*
+ * Int8 linear layer: what a layer computes from the codes that fq_forward emits, with a scale per token and per output
+ * channel (the "true INT8" deployment that the paper names as its target: Sec. 3.1, 5.2).
+ *   y[i][j] = (sum over l of q[i][l] * w[j][l]) * (xs[i] * ws[j]) + bias[j]
+ * The sum is exact (int32), the rest binary32, rounded to y's type once.  x is either codes (FQ_I8) with their scales, or
+ * FP16 / FP32 values that are quantized on the way, row by row:
+ *   xs[i] = max|x[i]| / 127 (the binary32 quotient),  q[i][l] = clip(round(x[i][l] / xs[i]), -127, 127)
+ * with round-half-to-even and the correctly rounded quotient, as in fq_forward.  A row whose greatest magnitude is under
+ * 127 * FLT_MIN has scale and codes 0; a row with a NaN or an infinity makes its row of y NaN.
+ * A 1x1 convolution is this with positions for tokens, a larger kernel with unfolded patches.
+ * Rows may lie any distance apart (ldx, ldw, ldy, in elements) and at any address that their type allows; nothing of x or w
+ * outside the rows is read.  Fastest where the rows of x (FQ_I8) and w begin on 16-byte boundaries and k is a multiple of
+ * 16.  One to three launches.  The workspace need not be initialised and may be shared by calls that do not overlap in time.
+ */
+typedef struct fq_linear {
+    int64_t m, n, k;                  /* tokens, output channels, values per token; any may be 0; k <= 131071 */
+    int32_t x_dtype, y_dtype;         /* FQ_F16, FQ_F32 or FQ_I8; FQ_F16 or FQ_F32 */
+    int64_t ldx, ldw, ldy;            /* >= k, k, n */
+    const void *x;                    /* in  [m][ldx] */
+    const float *xs;                  /* in, FQ_I8 only: the scales of the codes */
+    const int8_t *w;                  /* in  [n][ldw] */
+    const float *ws;                  /* in  the scales of w */
+    const float *bias;                /* in, optional: [n] */
+    void *y;                          /* out [m][ldy] */
+    int32_t xs_step, ws_step;         /* 1: a scale per token / channel; 0: one scale for all */
+} fq_linear;
+size_t fq_linear_workspace_bytes(const fq_linear *d);     /* 0 if d does not validate; host only */
+fq_status fq_linear_forward(const fq_linear *d, void *workspace, size_t ws_bytes, void *hip_stream);
 
 /*
  * Measurement aid, not part of the operation: a streaming kernel without arithmetic in the launch

@@ -10,6 +10,8 @@ from . import workloads  # noqa: F401
 _API = ("fq_forward", "fq_backward", "fq_multi_tensor", "fq_workspace_bytes", "fq_workspace_init",
         "fq_validate", "fq_status_string", "fq_plan_create", "fq_plan_run", "fq_plan_run_adam", "fq_plan_destroy",
         "fq_layout", "FqLayoutInfo", "fq_distill_loss", "fq_distill_workspace_bytes", "FqDistill", "FqTensor", "FqAdam", "FqTensorArray", "fq_tensor_array", "FqError", "library_path",
+        "fq_linear_forward", "fq_linear_workspace_bytes", "FqLinear", "fq_adamw_create", "fq_adamw_step", "fq_adamw_destroy",
+        "fq_adamw_workspace_bytes", "FqParam", "FqAdamW", "FQ_I8", "FQ_STATE_F32", "FQ_STATE_F8",
         "FQ_F16", "FQ_F32", "FQ_FLAG_NO_DX", "FQ_FLAG_TWO_PASS", "FQ_FLAG_NO_POLL", "FQ_MODE_FORWARD", "FQ_MODE_BACKWARD")
 
 

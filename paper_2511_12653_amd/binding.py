@@ -15,7 +15,8 @@ import os
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libfq.so")
 
-FQ_F16, FQ_F32 = 0, 1
+FQ_F16, FQ_F32, FQ_I8 = 0, 1, 2
+FQ_STATE_F32, FQ_STATE_F8 = 0, 1
 FQ_FLAG_NO_DX, FQ_FLAG_TWO_PASS, FQ_FLAG_NO_POLL = 1, 2, 4
 FQ_MODE_FORWARD, FQ_MODE_BACKWARD = 1, 2
 FLT_MIN = 1.1754943508222875e-38
@@ -139,6 +140,129 @@ class FqDistill(ctypes.Structure):
         return self
 
 
+def _device_of(tensors):
+    """The one GPU that all given tensors are on."""
+    device = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("tensors must be on the GPU (no CPU fallback)")
+        if device is not None and t.device != device:
+            raise ValueError("tensors are on different GPUs")
+        device = t.device
+
+
+class FqParam(ctypes.Structure):
+    """Mirror of `struct fq_param` (host struct; the pointers inside are device pointers)."""
+    _fields_ = [("n", ctypes.c_int64), ("p_dtype", ctypes.c_int32), ("g_dtype", ctypes.c_int32),
+                ("state", ctypes.c_int32), ("lr_scale", ctypes.c_float), ("weight_decay", ctypes.c_float),
+                ("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("p16", ctypes.c_void_p),
+                ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+    @classmethod
+    def from_torch(cls, p, g, m, v, m_scale=None, v_scale=None, p16=None, lr_scale=1.0, weight_decay=0.0):
+        """Parameters, gradients and states of one tensor; float32 m and v, or float8_e4m3fn ones with their scales."""
+        import torch
+        dtypes = {torch.float16: FQ_F16, torch.float32: FQ_F32}
+        n, f8 = p.numel(), m.dtype == torch.float8_e4m3fn
+        if p.dtype not in dtypes or g.dtype not in dtypes:
+            raise TypeError("p and g must be float16 or float32")
+        if m.dtype != v.dtype or not (f8 or m.dtype == torch.float32):
+            raise TypeError("m and v must both be float32 or both float8_e4m3fn")
+        if f8 != (m_scale is not None) or f8 != (v_scale is not None):
+            raise ValueError("m_scale and v_scale belong to float8 states, and to no others")
+        if p16 is not None and (p16.dtype != torch.float16 or p.dtype != torch.float32):
+            raise TypeError("p16 is the float16 copy of a float32 p")
+        for t in (g, m, v, p16):
+            if t is not None and t.numel() != n:
+                raise ValueError("tensor has %d elements, p has %d" % (t.numel(), n))
+        for t in (m_scale, v_scale):
+            if t is not None and (t.dtype != torch.float32 or t.numel() != (n + 255) // 256):
+                raise ValueError("scales must be %d float32 values" % ((n + 255) // 256))
+        given = (p, g, m, v, m_scale, v_scale, p16)
+        _device_of(given)
+        if any(t is not None and not t.is_contiguous() for t in given):
+            raise ValueError("tensors must be contiguous")
+        ptr = lambda t: None if t is None else t.data_ptr()
+        self = cls(n, dtypes[p.dtype], dtypes[g.dtype], FQ_STATE_F8 if f8 else FQ_STATE_F32, lr_scale, weight_decay,
+                   ptr(p), ptr(g), ptr(p16), ptr(m), ptr(v), ptr(m_scale), ptr(v_scale))
+        self._keep = given
+        return self
+
+
+class FqAdamW(ctypes.Structure):
+    """Mirror of `struct fq_adamw` (host struct); change lr and step in place from step to step."""
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_int64), ("seed", ctypes.c_uint64),
+                ("grad_scale", ctypes.c_void_p)]
+
+    def __init__(self, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1, seed=0, grad_scale=None):
+        """grad_scale: one float32 on the GPU, or None."""
+        pointer = None
+        if grad_scale is not None:
+            import torch
+            if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1:
+                raise TypeError("grad_scale must be one float32")
+            _device_of((grad_scale,))
+            pointer = grad_scale.data_ptr()
+        super().__init__(lr, beta1, beta2, eps, step, seed, pointer)
+        self._keep = grad_scale
+
+
+class FqLinear(ctypes.Structure):
+    """Mirror of `struct fq_linear` (host struct; the pointers inside are device pointers)."""
+    _fields_ = [("m", ctypes.c_int64), ("n", ctypes.c_int64), ("k", ctypes.c_int64),
+                ("x_dtype", ctypes.c_int32), ("y_dtype", ctypes.c_int32),
+                ("ldx", ctypes.c_int64), ("ldw", ctypes.c_int64), ("ldy", ctypes.c_int64),
+                ("x", ctypes.c_void_p), ("xs", ctypes.c_void_p), ("w", ctypes.c_void_p), ("ws", ctypes.c_void_p),
+                ("bias", ctypes.c_void_p), ("y", ctypes.c_void_p),
+                ("xs_step", ctypes.c_int32), ("ws_step", ctypes.c_int32)]
+
+    @classmethod
+    def from_torch(cls, x, w, w_scale, y, bias=None, x_scale=None):
+        """x [m, k] float16, float32 or int8 (then with x_scale), w [n, k] int8, y [m, n] float16 or float32, whose
+        rows may lie any distance apart; w_scale n values or one, x_scale m values or one, bias n values (float32)."""
+        import torch
+        x_types = {torch.float16: FQ_F16, torch.float32: FQ_F32, torch.int8: FQ_I8}
+        if x.dtype not in x_types or w.dtype != torch.int8 or y.dtype not in (torch.float16, torch.float32):
+            raise TypeError("x must be float16, float32 or int8, w int8, y float16 or float32")
+        if x.dim() != 2 or w.dim() != 2 or y.dim() != 2:
+            raise ValueError("x, w and y must have two dimensions")
+        (m, k), n = x.shape, w.shape[0]
+        if w.shape[1] != k or tuple(y.shape) != (m, n):
+            raise ValueError("x %s, w %s and y %s do not fit" % (tuple(x.shape), tuple(w.shape), tuple(y.shape)))
+        if (x.dtype == torch.int8) != (x_scale is not None):
+            raise ValueError("x_scale belongs to int8 codes, and to nothing else")
+        for t, count, name in ((w_scale, n, "w_scale"), (x_scale, m, "x_scale"), (bias, n, "bias")):
+            if t is None:
+                continue
+            if t.dtype != torch.float32 or not t.is_contiguous():
+                raise TypeError("%s must be contiguous float32" % name)
+            if t.numel() != count and (t.numel() != 1 or t is bias):
+                raise ValueError("%s has %d values, want %d" % (name, t.numel(), count))
+        _device_of((x, w, w_scale, y, bias, x_scale))
+
+        def pitch(t):
+            rows, cols = t.shape
+            if cols > 1 and t.stride(1) != 1:
+                raise ValueError("the values of a row must be contiguous")
+            if rows <= 1:
+                return cols
+            if t.stride(0) < cols:
+                raise ValueError("rows must not overlap")
+            return t.stride(0)
+
+        ptr = lambda t: None if t is None else t.data_ptr()
+        self = cls(m, n, k, x_types[x.dtype], FQ_F16 if y.dtype == torch.float16 else FQ_F32, pitch(x), pitch(w), pitch(y),
+                   ptr(x), ptr(x_scale), ptr(w), ptr(w_scale), ptr(bias), ptr(y),
+                   0 if x_scale is None or (x_scale.numel() == 1 and m != 1) else 1,
+                   0 if w_scale.numel() == 1 and n != 1 else 1)
+        self._keep = (x, w, w_scale, y, bias, x_scale)
+        return self
+
+
 class FqLayoutInfo(ctypes.Structure):
     """Mirror of `struct fq_layout_info`."""
     _fields_ = [("blocks", ctypes.c_int64), ("units_per_channel", ctypes.c_int64),
@@ -186,6 +310,19 @@ _lib.fq_distill_loss_no_poll.argtypes = [ctypes.POINTER(FqDistill), ctypes.c_voi
 _lib.fq_distill_loss_no_poll.restype = ctypes.c_int
 _lib.fq_distill_reads_of_pair.argtypes = [ctypes.POINTER(FqDistill)]
 _lib.fq_distill_reads_of_pair.restype = ctypes.c_int
+_lib.fq_adamw_workspace_bytes.argtypes = [ctypes.POINTER(FqParam), ctypes.c_int]
+_lib.fq_adamw_workspace_bytes.restype = ctypes.c_size_t
+_lib.fq_adamw_create.argtypes = [ctypes.POINTER(FqParam), ctypes.c_int, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p,
+                                 ctypes.POINTER(ctypes.c_void_p)]
+_lib.fq_adamw_create.restype = ctypes.c_int
+_lib.fq_adamw_step.argtypes = [ctypes.c_void_p, ctypes.POINTER(FqAdamW), ctypes.c_void_p]
+_lib.fq_adamw_step.restype = ctypes.c_int
+_lib.fq_adamw_destroy.argtypes = [ctypes.c_void_p]
+_lib.fq_adamw_destroy.restype = None
+_lib.fq_linear_workspace_bytes.argtypes = [ctypes.POINTER(FqLinear)]
+_lib.fq_linear_workspace_bytes.restype = ctypes.c_size_t
+_lib.fq_linear_forward.argtypes = [ctypes.POINTER(FqLinear), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+_lib.fq_linear_forward.restype = ctypes.c_int
 _lib.fq_layout.argtypes = [ctypes.POINTER(FqTensor), ctypes.POINTER(FqLayoutInfo)]
 _lib.fq_layout.restype = ctypes.c_int
 _lib.fq_status_string.argtypes = [ctypes.c_int]
@@ -265,7 +402,7 @@ def _native(function):
 
 
 if _fqcall:
-    _fqcall.setup(FqTensor, FqDistill, ctypes.c_void_p, _check)
+    _fqcall.setup(FqTensor, FqDistill, ctypes.c_void_p, _check, FqLinear, FqAdamW)
 
 
 def fq_status_string(status) -> str:
@@ -350,6 +487,43 @@ def fq_distill_loss(d: FqDistill, workspace, stream=None):
 def fq_distill_loss_no_poll(d: FqDistill, workspace, stream=None):
     p, nbytes = _ws(workspace)
     _check(_lib.fq_distill_loss_no_poll(ctypes.byref(d), p, nbytes, _stream(stream)))
+
+
+def _params(params):
+    params = list(params)
+    return (FqParam * max(1, len(params)))(*params), len(params)
+
+
+def fq_adamw_workspace_bytes(params) -> int:
+    return int(_lib.fq_adamw_workspace_bytes(*_params(params)))
+
+
+def fq_adamw_create(params, workspace, stream=None):
+    """Returns an opaque plan handle (ctypes.c_void_p); release it with fq_adamw_destroy."""
+    arr, n = _params(params)
+    p, nbytes = _ws(workspace)
+    plan = ctypes.c_void_p()
+    _check(_lib.fq_adamw_create(arr, n, p, nbytes, _stream(stream), ctypes.byref(plan)))
+    return plan
+
+
+@_native
+def fq_adamw_step(plan, h: FqAdamW, stream=None):
+    _check(_lib.fq_adamw_step(plan, ctypes.byref(h), _stream(stream)))
+
+
+def fq_adamw_destroy(plan):
+    _lib.fq_adamw_destroy(plan)
+
+
+def fq_linear_workspace_bytes(d: FqLinear) -> int:
+    return int(_lib.fq_linear_workspace_bytes(ctypes.byref(d)))
+
+
+@_native
+def fq_linear_forward(d: FqLinear, workspace, stream=None):
+    p, nbytes = _ws(workspace)
+    _check(_lib.fq_linear_forward(ctypes.byref(d), p, nbytes, _stream(stream)))
 
 
 def fq_probe_stream(inputs, a, b, out, nbytes, stream=None):

@@ -19,12 +19,13 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfq.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("fq_kernels.hip", "fq_distill.hip", "fq_api.cpp")]
+SOURCES = [os.path.join(CSRC, f) for f in ("fq_kernels.hip", "fq_distill.hip", "fq_adamw.hip", "fq_linear.hip",
+                                               "fq_api.cpp", "fq_adamw_api.cpp", "fq_linear_api.cpp")]
 CALL_SOURCE = os.path.join(CSRC, "fq_call.c")
 CALL = os.path.join(HERE, "_fqcall" + sysconfig.get_config_var("EXT_SUFFIX"))
 CC = os.environ.get("CC", "gcc")
-HEADERS = [os.path.join(CSRC, "fq_internal.h"), os.path.join(CSRC, "fq_device.h"),
-           os.path.join(HERE, "..", "include", "fq.h")]
+HEADERS = [os.path.join(CSRC, f) for f in ("fq_internal.h", "fq_device.h", "fq_adamw.h", "fq_linear.h")] + [
+    os.path.join(HERE, "..", "include", "fq.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-ffp-contract=off",
          "-fno-fast-math", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

@@ -739,7 +739,7 @@ const char *fq_status_string(fq_status status)
     switch (status) {
     case FQ_OK: return "ok";
     case FQ_ERR_NULL: return "a required pointer is NULL";
-    case FQ_ERR_DTYPE: return "dtype must be FQ_F16 or FQ_F32";
+    case FQ_ERR_DTYPE: return "a dtype or state that the field does not take";
     case FQ_ERR_SHAPE: return "bad extent, count, n or mode";
     case FQ_ERR_QRANGE: return "bad integer code range";
     case FQ_ERR_ALIGN: return "pointer not aligned";
@@ -747,7 +747,7 @@ const char *fq_status_string(fq_status status)
     case FQ_ERR_SCALE_PARAMS: return "bad eps / s_min / s_max";
     case FQ_ERR_LAUNCH: return "HIP runtime error while enqueuing";
     case FQ_ERR_ALIAS: return "output partially overlaps an input";
-    case FQ_ERR_OPTIMIZER: return "bad Adam parameters";
+    case FQ_ERR_OPTIMIZER: return "bad Adam or AdamW parameters";
     }
     return "unknown status";
 }

@@ -3,7 +3,7 @@
  * counterpart in binding.py takes; it recognises the forms below and leaves every other one, and every error, to
  * that counterpart, which `wrap` hands over.
  *
- *   descriptor   FqTensor / FqDistill itself (not a subclass)
+ *   descriptor   FqTensor / FqDistill / FqLinear / FqAdamW itself (not a subclass)
  *   plan         ctypes.c_void_p
  *   workspace    torch.Tensor itself, or a tuple of two ints
  *   stream       left out: torch's current stream, once binding.py has given its lookups (`streams`)
@@ -16,12 +16,12 @@
 
 #include "../../include/fq.h"
 
-enum { FORWARD, BACKWARD, PLAN_RUN, PLAN_RUN_ADAM, DISTILL, LAYOUT_BYTES, CALLS };
+enum { FORWARD, BACKWARD, PLAN_RUN, PLAN_RUN_ADAM, DISTILL, LAYOUT_BYTES, LINEAR, ADAMW_STEP, CALLS };
 static const char *const names[CALLS] = {"fq_forward", "fq_backward", "fq_plan_run", "fq_plan_run_adam", "fq_distill_loss",
-                                         "fq_workspace_bytes"};
+                                         "fq_workspace_bytes", "fq_linear_forward", "fq_adamw_step"};
 
 static PyObject *python_form[CALLS];                     /* the counterparts */
-static PyObject *tensor_type, *distill_type, *pointer_type, *check;
+static PyObject *tensor_type, *distill_type, *pointer_type, *check, *linear_type, *adamw_type;
 static PyObject *raw_stream, *current_device, *torch_tensor;
 static PyObject *str_data_ptr, *str_numel, *str_element_size;
 
@@ -151,6 +151,42 @@ static PyObject *call_distill(PyObject *self, PyObject *const *args, Py_ssize_t 
     return done(status);
 }
 
+static PyObject *call_linear(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    (void)self;
+    if (nargs != 2 || kwnames || !raw_stream || !linear_type || !is_a(args[0], linear_type) || !is_workspace(args[1]))
+        return to_python(LINEAR, args, nargs, kwnames);
+    const fq_linear *d = memory_of(args[0]);
+    void *stream, *ws;
+    size_t bytes;
+    fq_status status;
+    if (!d) return NULL;
+    const int left = workspace(args[1], &ws, &bytes);
+    if (left > 0) return to_python(LINEAR, args, nargs, kwnames);
+    if (left || current_stream(&stream)) return NULL;
+    Py_BEGIN_ALLOW_THREADS
+    status = fq_linear_forward(d, ws, bytes, stream);
+    Py_END_ALLOW_THREADS
+    return done(status);
+}
+
+static PyObject *call_adamw_step(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
+{
+    (void)self;
+    if (nargs != 2 || kwnames || !raw_stream || !adamw_type || !is_a(args[0], pointer_type) || !is_a(args[1], adamw_type))
+        return to_python(ADAMW_STEP, args, nargs, kwnames);
+    void **plan = memory_of(args[0]);
+    const fq_adamw *h = plan ? memory_of(args[1]) : NULL;
+    void *stream;
+    fq_status status;
+    if (!h || current_stream(&stream)) return NULL;
+    const fq_adamw_plan *p = *plan;
+    Py_BEGIN_ALLOW_THREADS
+    status = fq_adamw_step(p, h, stream);
+    Py_END_ALLOW_THREADS
+    return done(status);
+}
+
 static PyObject *call_plan_run(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
 {
     (void)self;
@@ -208,13 +244,15 @@ static void keep(PyObject **slot, PyObject *value)
 
 static PyObject *setup(PyObject *self, PyObject *args)
 {
-    PyObject *t, *d, *p, *c;
+    PyObject *t, *d, *p, *c, *l = NULL, *a = NULL;
     (void)self;
-    if (!PyArg_ParseTuple(args, "OOOO", &t, &d, &p, &c)) return NULL;
+    if (!PyArg_ParseTuple(args, "OOOO|OO", &t, &d, &p, &c, &l, &a)) return NULL;
     keep(&tensor_type, t);
     keep(&distill_type, d);
     keep(&pointer_type, p);
     keep(&check, c);
+    keep(&linear_type, l);
+    keep(&adamw_type, a);
     Py_RETURN_NONE;
 }
 
@@ -253,7 +291,9 @@ static PyMethodDef methods[] = {
     {"fq_plan_run_adam", FAST(call_plan_run_adam), "fq_plan_run_adam(plan, step, stream=None)\n--\n\n"},
     {"fq_distill_loss", FAST(call_distill), "fq_distill_loss(d, workspace, stream=None)\n--\n\n"},
     {"fq_workspace_bytes", FAST(call_workspace_bytes), "fq_workspace_bytes(tensors, mode)\n--\n\n"},
-    {"setup", setup, METH_VARARGS, "setup(FqTensor, FqDistill, c_void_p, check)\n--\n\n"},
+    {"fq_linear_forward", FAST(call_linear), "fq_linear_forward(d, workspace, stream=None)\n--\n\n"},
+    {"fq_adamw_step", FAST(call_adamw_step), "fq_adamw_step(plan, h, stream=None)\n--\n\n"},
+    {"setup", setup, METH_VARARGS, "setup(FqTensor, FqDistill, c_void_p, check, FqLinear=None, FqAdamW=None)\n--\n\n"},
     {"streams", streams, METH_VARARGS, "streams(raw, device, Tensor)\n--\n\n"},
     {"wrap", wrap, METH_O, "wrap(function)\n--\n\nThe native form of the binding's function, which takes what that one leaves to it."},
     {NULL, NULL, 0, NULL}};

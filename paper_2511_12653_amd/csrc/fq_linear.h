@@ -1,0 +1,38 @@
+// Internal interface between the host side of the int8 linear layer (fq_linear_api.cpp) and its gfx950 kernels
+// (fq_linear.hip).  Not part of the C ABI.
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+namespace fq {
+
+constexpr long long kLinearMostK = 131071;       // k * 128 * 128 < 2^31
+constexpr long long kCodePitch = 128;            // rows of codes in the workspace: a multiple of this, zeros behind k
+
+struct LinearArgs {
+    const int8_t *x;           // codes
+    const float *xs;
+    const int8_t *w;
+    const float *ws;
+    const float *bias;
+    void *y;
+    long long ldx, ldw, ldy;
+    int m, n, k;
+    int xs_step, ws_step;
+    int y16;                   // 1: y is FP16
+};
+
+struct QuantizeArgs {
+    const void *x;
+    long long ldx;
+    int m, k;
+    int x16;                   // 1: x is FP16
+    int8_t *q;                 // [m][pitch]
+    float *s;                  // [m]
+    long long pitch;
+};
+
+int launch_quantize_rows(const QuantizeArgs &a, void *stream);
+int launch_linear(const LinearArgs &a, void *stream);
+
+}  // namespace fq

@@ -1,0 +1,120 @@
+// Host side of the int8 linear layer: validation, workspace and launches (declared in include/fq.h).
+#include <cstring>
+
+#include "../../include/fq.h"
+#include "fq_linear.h"
+
+namespace fq {
+namespace {
+
+constexpr size_t kAlign = 256;
+
+size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+
+bool aligned(const void *p, size_t a) { return (uintptr_t)p % a == 0; }
+
+size_t size_of(int32_t dtype) { return dtype == FQ_I8 ? 1 : dtype == FQ_F16 ? 2 : 4; }
+
+// Rows of a matrix in memory: bytes of one, from one to the next, and how many.
+struct Rows {
+    uintptr_t at;
+    size_t width, pitch, count;
+    size_t span() const { return count ? (count - 1) * pitch + width : 0; }
+};
+
+// Whether two matrices share memory.  Columns of one buffer (equal pitches, rows that fall into each other's gaps) do not.
+bool overlap(const Rows &a, const Rows &b)
+{
+    if (!a.at || !b.at || !a.width || !b.width || !a.count || !b.count) return false;
+    if (a.at >= b.at + b.span() || b.at >= a.at + a.span()) return false;
+    if (a.pitch == b.pitch) {
+        const size_t off = a.at <= b.at ? (b.at - a.at) % a.pitch : (a.pitch - (a.at - b.at) % a.pitch) % a.pitch;
+        if (off >= a.width && off + b.width <= a.pitch) return false;
+    }
+    return true;
+}
+
+struct Workspace {
+    long long pitch = 0;             // of a row of codes
+    size_t scales_off = 0, bytes = kAlign;
+};
+
+Workspace workspace_of(const fq_linear &d)
+{
+    Workspace w;
+    if (d.x_dtype == FQ_I8) return w;
+    w.pitch = (d.k + kCodePitch - 1) / kCodePitch * kCodePitch;
+    w.scales_off = round_up((size_t)d.m * (size_t)w.pitch, kAlign);
+    w.bytes = w.scales_off + round_up((size_t)d.m * sizeof(float), kAlign);
+    if (w.bytes < kAlign) w.bytes = kAlign;
+    return w;
+}
+
+bool pitch_fits(long long rows, long long pitch, long long width)
+{
+    return pitch >= width && pitch <= (1LL << 56) / (rows > 0 ? rows : 1);
+}
+
+fq_status validate(const fq_linear &d)
+{
+    if (d.x_dtype != FQ_F16 && d.x_dtype != FQ_F32 && d.x_dtype != FQ_I8) return FQ_ERR_DTYPE;
+    if (d.y_dtype != FQ_F16 && d.y_dtype != FQ_F32) return FQ_ERR_DTYPE;
+    if (d.m < 0 || d.n < 0 || d.k < 0 || d.m > 0x7fffff00LL || d.n > 0x7fffff00LL || d.k > kLinearMostK) return FQ_ERR_SHAPE;
+    if (!pitch_fits(d.m, d.ldx, d.k) || !pitch_fits(d.n, d.ldw, d.k) || !pitch_fits(d.m, d.ldy, d.n)) return FQ_ERR_SHAPE;
+    if ((d.xs_step != 0 && d.xs_step != 1) || (d.ws_step != 0 && d.ws_step != 1)) return FQ_ERR_SHAPE;
+    if (((d.m + 31) / 32) * ((d.n + 31) / 32) > 0x7fffffffLL) return FQ_ERR_SHAPE;
+    const size_t xb = size_of(d.x_dtype), yb = size_of(d.y_dtype);
+    if (!aligned(d.x, xb) || !aligned(d.xs, 4) || !aligned(d.ws, 4) || !aligned(d.bias, 4) || !aligned(d.y, yb)) return FQ_ERR_ALIGN;
+    if (d.m == 0 || d.n == 0) return FQ_OK;
+    if (!d.y || !d.ws || (d.x_dtype == FQ_I8 && !d.xs) || (d.k > 0 && (!d.x || !d.w))) return FQ_ERR_NULL;
+    const size_t m = (size_t)d.m, n = (size_t)d.n, k = (size_t)d.k;
+    const Rows y = {(uintptr_t)d.y, n * yb, (size_t)d.ldy * yb, m};
+    const Rows in[] = {{(uintptr_t)d.x, k * xb, (size_t)d.ldx * xb, m}, {(uintptr_t)d.w, k, (size_t)d.ldw, n},
+                       {(uintptr_t)d.ws, (d.ws_step ? n : 1) * 4, 0, 1}, {(uintptr_t)d.bias, n * 4, 0, 1},
+                       {d.x_dtype == FQ_I8 ? (uintptr_t)d.xs : 0, (d.xs_step ? m : 1) * 4, 0, 1}};
+    for (const Rows &r : in)
+        if (overlap(y, r)) return FQ_ERR_ALIAS;
+    return FQ_OK;
+}
+
+fq_status run(const fq_linear &d, void *workspace, size_t ws_bytes, void *stream)
+{
+    const fq_status st = validate(d);
+    if (st != FQ_OK || d.m == 0 || d.n == 0) return st;
+    const Workspace ws = workspace_of(d);
+    LinearArgs a;
+    std::memset(&a, 0, sizeof a);
+    a.x = (const int8_t *)d.x; a.xs = d.xs; a.ldx = d.ldx; a.xs_step = d.xs_step;
+    a.w = d.w; a.ws = d.ws; a.ldw = d.ldw; a.ws_step = d.ws_step;
+    a.bias = d.bias; a.y = d.y; a.ldy = d.ldy; a.y16 = d.y_dtype == FQ_F16;
+    a.m = (int)d.m; a.n = (int)d.n; a.k = (int)d.k;
+    if (d.x_dtype != FQ_I8) {
+        if (!workspace || ws_bytes < ws.bytes) return FQ_ERR_WORKSPACE;
+        if (!aligned(workspace, kAlign)) return FQ_ERR_ALIGN;
+        QuantizeArgs q;
+        std::memset(&q, 0, sizeof q);
+        q.x = d.x; q.ldx = d.ldx; q.m = a.m; q.k = a.k; q.x16 = d.x_dtype == FQ_F16;
+        q.q = (int8_t *)workspace; q.s = (float *)((char *)workspace + ws.scales_off); q.pitch = ws.pitch;
+        if (launch_quantize_rows(q, stream) != 0) return FQ_ERR_LAUNCH;
+        a.x = q.q; a.xs = q.s; a.ldx = ws.pitch; a.xs_step = 1;
+    }
+    return launch_linear(a, stream) == 0 ? FQ_OK : FQ_ERR_LAUNCH;
+}
+
+}  // namespace
+}  // namespace fq
+
+extern "C" {
+
+size_t fq_linear_workspace_bytes(const fq_linear *d)
+{
+    return d && fq::validate(*d) == FQ_OK ? fq::workspace_of(*d).bytes : 0;
+}
+
+fq_status fq_linear_forward(const fq_linear *d, void *workspace, size_t ws_bytes, void *hip_stream)
+{
+    if (!d) return FQ_ERR_NULL;
+    return fq::run(*d, workspace, ws_bytes, hip_stream);
+}
+
+}  // extern "C"
