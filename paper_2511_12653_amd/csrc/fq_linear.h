@@ -18,8 +18,11 @@ struct LinearArgs {
     void *y;
     long long ldx, ldw, ldy;
     int m, n, k;
+    int kx;                    // codes of a row of x that may be read: k, or up to the pitch where zeros lie behind k
     int xs_step, ws_step;
     int y16;                   // 1: y is FP16
+    int y_vec;                 // 1: rows of y begin on 16-byte boundaries
+    int aligned;               // 1: rows of x and w begin on 16-byte boundaries, kx is a multiple of 16, pitches are at most 2^22
 };
 
 struct QuantizeArgs {

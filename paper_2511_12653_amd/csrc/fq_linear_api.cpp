@@ -8,6 +8,7 @@ namespace fq {
 namespace {
 
 constexpr size_t kAlign = 256;
+constexpr long long kMostPitch = 1 << 22;        // 256 rows of it have 32-bit offsets
 
 size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
@@ -87,7 +88,7 @@ fq_status run(const fq_linear &d, void *workspace, size_t ws_bytes, void *stream
     a.x = (const int8_t *)d.x; a.xs = d.xs; a.ldx = d.ldx; a.xs_step = d.xs_step;
     a.w = d.w; a.ws = d.ws; a.ldw = d.ldw; a.ws_step = d.ws_step;
     a.bias = d.bias; a.y = d.y; a.ldy = d.ldy; a.y16 = d.y_dtype == FQ_F16;
-    a.m = (int)d.m; a.n = (int)d.n; a.k = (int)d.k;
+    a.m = (int)d.m; a.n = (int)d.n; a.k = a.kx = (int)d.k;
     if (d.x_dtype != FQ_I8) {
         if (!workspace || ws_bytes < ws.bytes) return FQ_ERR_WORKSPACE;
         if (!aligned(workspace, kAlign)) return FQ_ERR_ALIGN;
@@ -97,7 +98,12 @@ fq_status run(const fq_linear &d, void *workspace, size_t ws_bytes, void *stream
         q.q = (int8_t *)workspace; q.s = (float *)((char *)workspace + ws.scales_off); q.pitch = ws.pitch;
         if (launch_quantize_rows(q, stream) != 0) return FQ_ERR_LAUNCH;
         a.x = q.q; a.xs = q.s; a.ldx = ws.pitch; a.xs_step = 1;
+        a.kx = (int)ws.pitch;
     }
+    const size_t yb = size_of(d.y_dtype);
+    a.y_vec = aligned(a.y, 16) && (size_t)a.ldy * yb % 16 == 0;
+    a.aligned = aligned(a.x, 16) && aligned(a.w, 16) && a.ldx % 16 == 0 && a.ldw % 16 == 0 && a.kx % 16 == 0 &&
+                a.ldx <= kMostPitch && a.ldw <= kMostPitch;
     return launch_linear(a, stream) == 0 ? FQ_OK : FQ_ERR_LAUNCH;
 }
 
