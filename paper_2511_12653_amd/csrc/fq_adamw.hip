@@ -52,7 +52,7 @@ template <int CTRL, int ROW_MASK> __device__ __forceinline__ unsigned max_step(u
     return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, v), __builtin_bit_cast(u16x2, w)));
 }
 
-__device__ __forceinline__ unsigned wave_max(unsigned v)
+__device__ __forceinline__ unsigned halves_max(unsigned v)
 {
     v = max_step<0xB1, 0xf>(v);
     v = max_step<0x4E, 0xf>(v);
@@ -180,7 +180,7 @@ __device__ __forceinline__ void step_rows(const AdamwTensor &t, const AdamwStep 
             am = max(am, __builtin_bit_cast(unsigned, m[j]) & 0x7FFFFFFFu);
             av = max(av, __builtin_bit_cast(unsigned, v[j]) & 0x7FFFFFFFu);
         }
-        const unsigned both = wave_max(((am + 0x1FFFFFu) >> 23) | ((av + 0x3BFFFFu) >> 23) << 16);
+        const unsigned both = halves_max(((am + 0x1FFFFFu) >> 23) | ((av + 0x3BFFFFu) >> 23) << 16);
         const int em = max((int)(both & 0xFFFFu) - 127 - 8, -126);
         const int e2 = max((int)(both >> 16) - 127 - 17, -126);
         const int ev = (e2 + 1) >> 1;

@@ -43,6 +43,24 @@ __device__ __forceinline__ double wave_sum(double v)
     return v;
 }
 
+// The greatest of the lanes' values, in every lane: the same steps.
+template <int CTRL, int ROW_MASK> __device__ __forceinline__ unsigned dpp_max(unsigned v)
+{
+    const unsigned w = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROW_MASK, 0xf, false);   // masked rows get 0
+    return v > w ? v : w;
+}
+
+__device__ __forceinline__ unsigned wave_max(unsigned v)
+{
+    v = dpp_max<0xB1, 0xf>(v);
+    v = dpp_max<0x4E, 0xf>(v);
+    v = dpp_max<0x141, 0xf>(v);
+    v = dpp_max<0x140, 0xf>(v);
+    v = dpp_max<0x142, 0xa>(v);
+    v = dpp_max<0x143, 0xc>(v);
+    return (unsigned)__builtin_amdgcn_readlane((int)v, kSumLane);
+}
+
 // ---------------------------------------------------------------------------------------------
 // Memory access helpers.  Pointers inside the descriptor are generic; naming the address space
 // gives global_load/global_store (not flat) for tensor data and scalar (SMEM) loads for values

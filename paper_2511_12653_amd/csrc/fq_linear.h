@@ -9,8 +9,11 @@ namespace fq {
 constexpr long long kLinearMostK = 131071;       // k * 128 * 128 < 2^31
 constexpr long long kCodePitch = 128;            // rows of codes in the workspace: a multiple of this, zeros behind k
 
+constexpr long long kFewLds = 64 << 10;          // most codes of x in the LDS of a block of few tokens
+
 struct LinearArgs {
     const int8_t *x;           // codes
+    const void *raw;           // instead of x: values that the kernel quantizes itself (see linear_quantizes)
     const float *xs;
     const int8_t *w;
     const float *ws;
@@ -22,7 +25,8 @@ struct LinearArgs {
     int xs_step, ws_step;
     int y16;                   // 1: y is FP16
     int y_vec;                 // 1: rows of y begin on 16-byte boundaries
-    int aligned;               // 1: rows of x and w begin on 16-byte boundaries, kx is a multiple of 16, pitches are at most 2^22
+    int x16, x_vec;            // of raw, 1: FP16; rows begin on 16-byte boundaries
+    int aligned;               // 1: rows of x and w begin on 16-byte boundaries, k is a multiple of 16, pitches are at most 2^22
 };
 
 struct QuantizeArgs {
@@ -30,11 +34,13 @@ struct QuantizeArgs {
     long long ldx;
     int m, k;
     int x16;                   // 1: x is FP16
+    int vec;                   // 1: rows of x begin on 16-byte boundaries
     int8_t *q;                 // [m][pitch]
     float *s;                  // [m]
     long long pitch;
 };
 
+bool linear_quantizes(const LinearArgs &a);      // whether the kernel for these sizes takes values of x
 int launch_quantize_rows(const QuantizeArgs &a, void *stream);
 int launch_linear(const LinearArgs &a, void *stream);
 

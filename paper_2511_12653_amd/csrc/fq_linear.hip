@@ -13,36 +13,117 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 // ---------------------------------------------------------------------------------------------
-// Codes and scale of a row of x: a block per row, which reads it twice (the second time from the caches).
-__device__ __forceinline__ unsigned wave_umax(unsigned v)
+// Codes and scale of a row of x.
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+
+// Values [at, at + 8) of a row of k; zeros behind its end.
+template <typename T> __device__ __forceinline__ void load8(const T *row, int at, int k, bool vec, float *v)
 {
+    if (vec && at + 8 <= k) {
+        if constexpr (sizeof(T) == 2) {
+            const f16x8 h = *(const FQ_GLOBAL f16x8 *)(row + at);
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v = max(v, (unsigned)__shfl_xor((int)v, d));
-    return v;
+            for (int e = 0; e < 8; ++e) v[e] = (float)h[e];
+        } else {
+            const f32x4 a = *(const FQ_GLOBAL f32x4 *)(row + at), b = *(const FQ_GLOBAL f32x4 *)(row + at + 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[e + 4] = b[e]; }
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = at + e < k ? (float)ld_global(row + at + e) : 0.0f;
 }
 
-template <typename T>
+// Greatest magnitude of eight values, as bits (magnitudes order like their bits: NaN, infinity, numbers).
+__device__ __forceinline__ unsigned most8(const float *v)
+{
+    unsigned most = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = max(most, __builtin_bit_cast(unsigned, v[e]) & 0x7FFFFFFFu);
+    return most;
+}
+
+struct RowScale {
+    float s, inverse;                  // inverse 0: the row's codes are 0
+};
+
+__device__ __forceinline__ RowScale row_scale(unsigned most)
+{
+    const float largest = __builtin_bit_cast(float, most);
+    if (most >= 0x7F800000u) return {__builtin_nanf(""), 0.0f};
+    if (largest < 127.0f * 0x1p-126f) return {0.0f, 0.0f};
+    const float s = largest / 127.0f;
+    return {s, 1.0f / s};
+}
+
+// Codes of eight values.  x * (1 / s) is within 127 * 2^-22.4 of the quotient x / s, so unless it lies that near to a
+// half (a few vectors of a row) it rounds to the same integer.  Adding 1.5 * 2^23 rounds it, to even, and leaves the code in
+// the low byte.  No code leaves [-127, 127]: no |x| is over 127 * s * (1 + 2^-24).
+__device__ __forceinline__ u32x2 codes8(const float *v, RowScale r)
+{
+    constexpr float kMagic = 0x1.8p23f;
+    unsigned b[8];
+    float near = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float t = v[e] * r.inverse, f = t + kMagic;
+        b[e] = __builtin_bit_cast(unsigned, f);
+        near = __builtin_fmaxf(near, __builtin_fabsf(t - (f - kMagic)));
+    }
+    if (near > 0.49995f) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) b[e] = __builtin_bit_cast(unsigned, v[e] / r.s + kMagic);
+    }
+    const auto pack = [](unsigned p, unsigned q, unsigned s, unsigned t) {
+        return __builtin_amdgcn_perm(__builtin_amdgcn_perm(t, s, 0x0c0c0400u), __builtin_amdgcn_perm(q, p, 0x0c0c0400u), 0x05040100u);
+    };
+    u32x2 w = u32x2{pack(b[0], b[1], b[2], b[3]), pack(b[4], b[5], b[6], b[7])};
+    if (r.inverse == 0.0f) w = (u32x2)0u;
+    return w;
+}
+
+// THREADS of a block have a row, HELD vectors of eight each: read once, kept in registers.  Longer rows are read again
+// for the codes.
+template <typename T, int THREADS, int HELD>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs a)
 {
     __shared__ unsigned top[4];
-    const long long row = blockIdx.x;
+    const int at = threadIdx.x % THREADS;
+    const long long row = (long long)blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS;
+    if (THREADS < 256 && row >= a.m) return;
     const T *x = (const T *)a.x + row * a.ldx;
+    float v[HELD][8];
     unsigned most = 0;
-    for (int i = threadIdx.x; i < a.k; i += 256)
-        most = max(most, __builtin_bit_cast(unsigned, (float)ld_global(x + i)) & 0x7FFFFFFFu);
-    most = wave_umax(most);
-    if ((threadIdx.x & 63) == 0) top[threadIdx.x >> 6] = most;
-    __syncthreads();
-    most = max(max(top[0], top[1]), max(top[2], top[3]));
-    const float largest = __builtin_bit_cast(float, most);
-    const bool fine = most < 0x7F800000u;                    // no NaN and no infinity (magnitudes order like their bits)
-    const bool zero = largest < 127.0f * 0x1p-126f;
-    const float s = !fine ? __builtin_nanf("") : zero ? 0.0f : largest / 127.0f;
-    if (threadIdx.x == 0) st_global(a.s + row, s);
-    for (int i = threadIdx.x; i < a.pitch; i += 256) {
-        float q = 0.0f;
-        if (fine && !zero && i < a.k) q = __builtin_fminf(__builtin_fmaxf(__builtin_rintf((float)ld_global(x + i) / s), -127.0f), 127.0f);
-        st_global(a.q + row * a.pitch + i, (int8_t)q);
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) load8(x, (j * THREADS + at) * 8, a.k, a.vec, v[j]);
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) most = max(most, most8(v[j]));
+    for (int i = (HELD * THREADS + at) * 8; i < a.k; i += THREADS * 8) {
+        float more[8];
+        load8(x, i, a.k, a.vec, more);
+        most = max(most, most8(more));
+    }
+    most = wave_max(most);
+    if (THREADS == 256) {
+        if ((threadIdx.x & 63) == 0) top[threadIdx.x >> 6] = most;
+        __syncthreads();
+        most = max(max(top[0], top[1]), max(top[2], top[3]));
+    }
+    const RowScale r = row_scale(most);
+    if (at == 0) st_global(a.s + row, r.s);
+    int8_t *q = a.q + row * a.pitch;
+#pragma unroll
+    for (int j = 0; j < HELD; ++j) {
+        const int i = (j * THREADS + at) * 8;
+        if (i < a.pitch) *(FQ_GLOBAL u32x2 *)(q + i) = codes8(v[j], r);
+    }
+    for (int i = (HELD * THREADS + at) * 8; i < a.pitch; i += THREADS * 8) {
+        float more[8];
+        load8(x, i, a.k, a.vec, more);
+        *(FQ_GLOBAL u32x2 *)(q + i) = codes8(more, r);
     }
 }
 
@@ -132,7 +213,6 @@ __device__ __forceinline__ void store8(const LinearArgs &a, long long i, int j, 
 {
     if (a.y16) {
         _Float16 *to = (_Float16 *)a.y + i * a.ldy + j;
-        typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
         f16x8 v;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = (_Float16)y[e];
@@ -146,7 +226,6 @@ __device__ __forceinline__ void store8(const LinearArgs &a, long long i, int j, 
         return;
     }
     float *to = (float *)a.y + i * a.ldy + j;
-    typedef float f32x4 __attribute__((ext_vector_type(4)));
     if (a.y_vec && j + 8 <= a.n) {
         *(FQ_GLOBAL f32x4 *)to = f32x4{y[0], y[1], y[2], y[3]};
         *(FQ_GLOBAL f32x4 *)(to + 4) = f32x4{y[4], y[5], y[6], y[7]};
@@ -288,6 +367,151 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
     }
 }
 
+// ---------------------------------------------------------------------------------------------
+// Few tokens: what counts is to stream w once.  A block multiplies 16 * CH channels by all tokens (TOK times 16, lanes past
+// the last repeat it); its wavefronts share the codes of a row, a run of whole steps of 64 each, and their sums meet in
+// LDS.  w goes straight from memory into registers, kAhead steps of it requested before the first is used: 16 rows x 64
+// bytes to a load instruction.  With X FP16 or FP32 the block first turns the rows of x into codes in LDS, while the first
+// codes of w are on their way; with X int8 the codes of x come from memory like those of w.
+template <typename X, int TOK, int CH, int WAVES, bool ALIGNED>
+__global__ __launch_bounds__(WAVES * 64) void linear_few_kernel(LinearArgs a)
+{
+    constexpr bool kQuantize = sizeof(X) > 1;
+    constexpr int kAhead = 8 / CH, kPitch = 20;                  // (of 16 channels' sums in LDS)
+    extern __shared__ __attribute__((aligned(16))) int8_t lds[];
+    __shared__ int sums[WAVES * TOK * CH * 16 * kPitch];
+    __shared__ unsigned top[TOK * 16];
+    __shared__ float scales[TOK * 16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n0 = (int)blockIdx.x * (16 * CH);
+    const int steps = (a.k + 63) / 64, each = (steps + WAVES - 1) / WAVES;
+    const int begin = wave * each * 64, end = min(steps, (wave + 1) * each) * 64;
+    const int8_t *w[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) w[c] = a.w + (long long)min(n0 + c * 16 + lane % 16, a.n - 1) * a.ldw;
+    // Behind the end of a row: with ALIGNED any codes (those of x are 0 there).
+    auto load_w = [&](int c, int l) {
+        const int at = l + lane / 16 * 16;
+        return ALIGNED ? ld_stream((const i32x4 *)(w[c] + min(at, a.k - 16))) : load16(w[c], at, a.k);
+    };
+    i32x4 cw[kAhead][CH];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (begin + j * 64 < end) cw[j][c] = load_w(c, begin + j * 64);
+
+    const int8_t *x[TOK];
+    const int pitch = steps * 64 + 16;                           // of a row of codes in LDS: rows of a 16 begin in different banks
+    if constexpr (kQuantize) {
+        __builtin_amdgcn_sched_barrier(0);
+        // (row, part) pairs go round the wavefronts
+        const int parts = max(1, WAVES / a.m), span = ((a.k + parts - 1) / parts + 511) / 512 * 512;
+        const X *rows = (const X *)a.raw;
+        if (threadIdx.x < TOK * 16) top[threadIdx.x] = 0;
+        __syncthreads();
+        for (int i = wave; i < a.m * parts; i += WAVES) {
+            const int row = i / parts, from = i % parts * span;
+            unsigned most = 0;
+            for (int at = from + lane * 8; at < min(from + span, a.k); at += 512) {
+                float v[8];
+                load8(rows + row * a.ldx, at, a.k, a.x_vec, v);
+                most = max(most, most8(v));
+            }
+            most = wave_max(most);
+            if (lane == 0) atomicMax(&top[row], most);
+        }
+        __syncthreads();
+        for (int i = wave; i < a.m * parts; i += WAVES) {
+            const int row = i / parts, from = i % parts * span;
+            const RowScale r = row_scale(top[row]);
+            if (lane == 0) scales[row] = r.s;
+            for (int at = from + lane * 8; at < min(from + span, steps * 64); at += 512) {
+                float v[8];
+                load8(rows + row * a.ldx, at, a.k, a.x_vec, v);
+                *(u32x2 *)(lds + row * pitch + at) = codes8(v, r);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < TOK; ++t) x[t] = lds + min(t * 16 + lane % 16, a.m - 1) * pitch;
+    } else {
+#pragma unroll
+        for (int t = 0; t < TOK; ++t) x[t] = a.x + (long long)min(t * 16 + lane % 16, a.m - 1) * a.ldx;
+    }
+    auto load_x = [&](int t, int l) {
+        const int at = l + lane / 16 * 16;
+        if constexpr (kQuantize) return *(const i32x4 *)(x[t] + at);
+        if (!ALIGNED) return load16(x[t], at, a.k);
+        return at < a.kx ? ld_global((const i32x4 *)(x[t] + at)) : (i32x4)0;
+    };
+
+    i32x4 sum[CH][TOK];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int t = 0; t < TOK; ++t) sum[c][t] = (i32x4)0;
+    for (int l = begin; l < end; l += kAhead * 64) {
+        i32x4 cx[kAhead][TOK];
+        if (!kQuantize) {
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+                for (int t = 0; t < TOK; ++t)
+                    if (l + j * 64 < end) cx[j][t] = load_x(t, l + j * 64);
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            const int at = l + j * 64;
+            if (at >= end) break;
+#pragma unroll
+            for (int t = 0; t < TOK; ++t) {
+                const i32x4 codes = kQuantize ? load_x(t, at) : cx[j][t];
+#pragma unroll
+                for (int c = 0; c < CH; ++c) sum[c][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(cw[j][c], codes, sum[c][t], 0, 0, 0);
+            }
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+                if (at + kAhead * 64 < end) cw[j][c] = load_w(c, at + kAhead * 64);
+        }
+    }
+    // lane l has channels 4 (l / 16) to 4 (l / 16) + 3 of token l % 16
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int t = 0; t < TOK; ++t)
+            *(i32x4 *)(sums + (((wave * CH + c) * TOK + t) * 16 + lane % 16) * kPitch + lane / 16 * 4) = sum[c][t];
+    __syncthreads();
+    // four channels of a token to a thread
+    for (int i = threadIdx.x; i < CH * TOK * 64; i += WAVES * 64) {
+        const int group = i % 4, c = i / 4 % CH, m = i / (4 * CH), n = n0 + c * 16 + group * 4;
+        if (m >= a.m || n >= a.n) continue;
+        i32x4 all = (i32x4)0;
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v) all += *(const i32x4 *)(sums + ((v * CH + c) * TOK * 16 + m) * kPitch + group * 4);
+        const float xs = kQuantize ? scales[m] : ld_global(a.xs + (long long)m * a.xs_step);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int j = n + e;
+            if (j >= a.n) break;
+            float y = (float)all[e] * (xs * ld_global(a.ws + (long long)j * a.ws_step));
+            if (a.bias) y += ld_global(a.bias + j);
+            if (a.y16) st_global((_Float16 *)a.y + (long long)m * a.ldy + j, (_Float16)y);
+            else st_global((float *)a.y + (long long)m * a.ldy + j, y);
+        }
+    }
+}
+
+template <typename X, int TOK, int CH> int launch_few(const LinearArgs &a, void *stream)
+{
+    constexpr int WAVES = 8;
+    const unsigned blocks = (unsigned)((a.n + 16 * CH - 1) / (16 * CH));
+    const size_t lds = sizeof(X) > 1 ? (size_t)a.m * (size_t)((a.k + 63) / 64 * 64 + 16) : 0;
+    if (a.aligned) linear_few_kernel<X, TOK, CH, WAVES, true><<<blocks, WAVES * 64, lds, (hipStream_t)stream>>>(a);
+    else linear_few_kernel<X, TOK, CH, WAVES, false><<<blocks, WAVES * 64, lds, (hipStream_t)stream>>>(a);
+    return (int)hipGetLastError();
+}
+
 template <int BM, int BN, int WM, int WN> int launch_tiles(const LinearArgs &a, void *stream)
 {
     const unsigned blocks = (unsigned)(((long long)a.m + BM - 1) / BM * (((long long)a.n + BN - 1) / BN));
@@ -298,15 +522,36 @@ template <int BM, int BN, int WM, int WN> int launch_tiles(const LinearArgs &a, 
 
 }  // namespace
 
+template <typename T> static int quantize_rows(const QuantizeArgs &a, void *stream)
+{
+    if (a.k <= 512) quantize_rows_kernel<T, 64, 1><<<((unsigned)a.m + 3) / 4, 256, 0, (hipStream_t)stream>>>(a);
+    else if (a.k <= 2048) quantize_rows_kernel<T, 64, 4><<<((unsigned)a.m + 3) / 4, 256, 0, (hipStream_t)stream>>>(a);
+    else quantize_rows_kernel<T, 256, 4><<<(unsigned)a.m, 256, 0, (hipStream_t)stream>>>(a);
+    return (int)hipGetLastError();
+}
+
 int launch_quantize_rows(const QuantizeArgs &a, void *stream)
 {
-    if (a.x16) quantize_rows_kernel<_Float16><<<(unsigned)a.m, 256, 0, (hipStream_t)stream>>>(a);
-    else quantize_rows_kernel<float><<<(unsigned)a.m, 256, 0, (hipStream_t)stream>>>(a);
-    return (int)hipGetLastError();
+    return a.x16 ? quantize_rows<_Float16>(a, stream) : quantize_rows<float>(a, stream);
+}
+
+bool linear_quantizes(const LinearArgs &a)
+{
+    return a.k > 0 && a.m <= 16 && (long long)a.m * (a.k + 80) <= kFewLds;
 }
 
 int launch_linear(const LinearArgs &a, void *stream)
 {
+    if (a.raw) {
+        if (a.x16) return launch_few<_Float16, 1, 1>(a, stream);
+        return launch_few<float, 1, 1>(a, stream);
+    }
+    if (a.m <= 64 && a.k > 0) {
+        const bool wide = a.n >= 32 * 2 * kComputeUnits;
+        if (a.m <= 16) return wide ? launch_few<int8_t, 1, 2>(a, stream) : launch_few<int8_t, 1, 1>(a, stream);
+        if (a.m <= 32) return wide ? launch_few<int8_t, 2, 2>(a, stream) : launch_few<int8_t, 2, 1>(a, stream);
+        return wide ? launch_few<int8_t, 4, 2>(a, stream) : launch_few<int8_t, 4, 1>(a, stream);
+    }
     const long long large = ((long long)a.m + 255) / 256 * (((long long)a.n + 255) / 256);
     if (large >= kComputeUnits) return launch_tiles<256, 256, 2, 4>(a, stream);
     const long long medium = ((long long)a.m + 127) / 128 * (((long long)a.n + 127) / 128);

@@ -89,21 +89,29 @@ fq_status run(const fq_linear &d, void *workspace, size_t ws_bytes, void *stream
     a.w = d.w; a.ws = d.ws; a.ldw = d.ldw; a.ws_step = d.ws_step;
     a.bias = d.bias; a.y = d.y; a.ldy = d.ldy; a.y16 = d.y_dtype == FQ_F16;
     a.m = (int)d.m; a.n = (int)d.n; a.k = a.kx = (int)d.k;
+    const size_t xb = size_of(d.x_dtype), yb = size_of(d.y_dtype);
+    const bool x_vec = aligned(d.x, 16) && (size_t)d.ldx * xb % 16 == 0;
+    bool x_aligned = x_vec && a.ldx <= kMostPitch;
     if (d.x_dtype != FQ_I8) {
         if (!workspace || ws_bytes < ws.bytes) return FQ_ERR_WORKSPACE;
         if (!aligned(workspace, kAlign)) return FQ_ERR_ALIGN;
-        QuantizeArgs q;
-        std::memset(&q, 0, sizeof q);
-        q.x = d.x; q.ldx = d.ldx; q.m = a.m; q.k = a.k; q.x16 = d.x_dtype == FQ_F16;
-        q.q = (int8_t *)workspace; q.s = (float *)((char *)workspace + ws.scales_off); q.pitch = ws.pitch;
-        if (launch_quantize_rows(q, stream) != 0) return FQ_ERR_LAUNCH;
-        a.x = q.q; a.xs = q.s; a.ldx = ws.pitch; a.xs_step = 1;
-        a.kx = (int)ws.pitch;
+        x_aligned = true;
+        a.x16 = d.x_dtype == FQ_F16;
+        a.x_vec = x_vec;
+        if (linear_quantizes(a)) {
+            a.raw = d.x;
+        } else {
+            QuantizeArgs q;
+            std::memset(&q, 0, sizeof q);
+            q.x = d.x; q.ldx = d.ldx; q.m = a.m; q.k = a.k; q.x16 = a.x16; q.vec = x_vec;
+            q.q = (int8_t *)workspace; q.s = (float *)((char *)workspace + ws.scales_off); q.pitch = ws.pitch;
+            if (launch_quantize_rows(q, stream) != 0) return FQ_ERR_LAUNCH;
+            a.x = q.q; a.xs = q.s; a.ldx = ws.pitch; a.xs_step = 1;
+            a.kx = (int)ws.pitch;
+        }
     }
-    const size_t yb = size_of(d.y_dtype);
     a.y_vec = aligned(a.y, 16) && (size_t)a.ldy * yb % 16 == 0;
-    a.aligned = aligned(a.x, 16) && aligned(a.w, 16) && a.ldx % 16 == 0 && a.ldw % 16 == 0 && a.kx % 16 == 0 &&
-                a.ldx <= kMostPitch && a.ldw <= kMostPitch;
+    a.aligned = x_aligned && aligned(a.w, 16) && a.ldw % 16 == 0 && a.ldw <= kMostPitch && a.k % 16 == 0;
     return launch_linear(a, stream) == 0 ? FQ_OK : FQ_ERR_LAUNCH;
 }
 

@@ -82,7 +82,7 @@ def run(m, n, k, x_kind, y_kind, seed, bias=True, xs_one=False, ws_one=False, **
 SIZES = [(1, 1, 1), (1, 16, 64), (1, 4096, 512), (1, 1000, 1155), (2, 33, 17), (3, 257, 100), (7, 64, 4096), (16, 128, 256),
          (17, 130, 384), (20, 512, 1024), (31, 48, 63), (33, 16, 2048), (64, 64, 64), (65, 300, 127), (100, 31, 129),
          (128, 256, 128), (129, 257, 255), (200, 96, 3456), (255, 511, 40), (256, 256, 512), (300, 700, 130), (513, 384, 384),
-         (1000, 130, 1155), (1201, 257, 1155), (2049, 129, 96), (700, 1100, 640)]
+         (16, 64, 4000), (15, 70, 4288), (2, 40, 30000), (64, 8200, 96), (30, 16400, 200), (5, 16385, 80), (1000, 130, 1155), (1201, 257, 1155), (2049, 129, 96), (700, 1100, 640)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
