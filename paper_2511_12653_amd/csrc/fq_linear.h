@@ -9,7 +9,8 @@ namespace fq {
 constexpr long long kLinearMostK = 131071;       // k * 128 * 128 < 2^31
 constexpr long long kCodePitch = 128;            // rows of codes in the workspace: a multiple of this, zeros behind k
 
-constexpr long long kFewLds = 64 << 10;          // most codes of x in the LDS of a block of few tokens
+constexpr int kFewLds = 150 << 10;               // most LDS of a block of few tokens
+constexpr int kFewMostN = 16 * 256;              // most channels there: a block to a compute unit
 
 struct LinearArgs {
     const int8_t *x;           // codes
@@ -26,7 +27,8 @@ struct LinearArgs {
     int y16;                   // 1: y is FP16
     int y_vec;                 // 1: rows of y begin on 16-byte boundaries
     int x16, x_vec;            // of raw, 1: FP16; rows begin on 16-byte boundaries
-    int aligned;               // 1: rows of x and w begin on 16-byte boundaries, k is a multiple of 16, pitches are at most 2^22
+    int w_fits;                // 1: rows of w begin on 16-byte boundaries, k is a multiple of 16, the pitch is at most 2^22
+    int aligned;               // 1: so do those of x
 };
 
 struct QuantizeArgs {

@@ -91,6 +91,7 @@ fq_status run(const fq_linear &d, void *workspace, size_t ws_bytes, void *stream
     a.m = (int)d.m; a.n = (int)d.n; a.k = a.kx = (int)d.k;
     const size_t xb = size_of(d.x_dtype), yb = size_of(d.y_dtype);
     const bool x_vec = aligned(d.x, 16) && (size_t)d.ldx * xb % 16 == 0;
+    a.w_fits = aligned(a.w, 16) && a.ldw % 16 == 0 && a.ldw <= kMostPitch && a.k % 16 == 0;
     bool x_aligned = x_vec && a.ldx <= kMostPitch;
     if (d.x_dtype != FQ_I8) {
         if (!workspace || ws_bytes < ws.bytes) return FQ_ERR_WORKSPACE;
@@ -111,7 +112,7 @@ fq_status run(const fq_linear &d, void *workspace, size_t ws_bytes, void *stream
         }
     }
     a.y_vec = aligned(a.y, 16) && (size_t)a.ldy * yb % 16 == 0;
-    a.aligned = x_aligned && aligned(a.w, 16) && a.ldw % 16 == 0 && a.ldw <= kMostPitch && a.k % 16 == 0;
+    a.aligned = x_aligned && a.w_fits;
     return launch_linear(a, stream) == 0 ? FQ_OK : FQ_ERR_LAUNCH;
 }
 
