@@ -9,12 +9,13 @@ namespace fq {
 constexpr long long kLinearMostK = 131071;       // k * 128 * 128 < 2^31
 constexpr long long kCodePitch = 128;            // rows of codes in the workspace: a multiple of this, zeros behind k
 
+constexpr long long kMostPitch = 1 << 22;        // of rows of codes that the tiles take: 256 of them have 32-bit offsets
 constexpr int kFewLds = 150 << 10;               // most LDS of a block of few tokens
 constexpr int kFewMostN = 16 * 256;              // most channels there: a block to a compute unit
 
 struct LinearArgs {
-    const int8_t *x;           // codes
-    const void *raw;           // instead of x: values that the kernel quantizes itself (see linear_quantizes)
+    const int8_t *x;           // codes, in rows that fit (see w_fits)
+    const void *raw;           // instead of x: values for the kernel of few tokens
     const float *xs;
     const int8_t *w;
     const float *ws;
@@ -22,13 +23,12 @@ struct LinearArgs {
     void *y;
     long long ldx, ldw, ldy;
     int m, n, k;
-    int kx;                    // codes of a row of x that may be read: k, or up to the pitch where zeros lie behind k
+    int kx, kw;                // codes of a row of x and w that the tiles read: whole 16; k, or more where zeros lie behind k
     int xs_step, ws_step;
+    int x16, x_vec;            // of raw, 1: FP16; rows on 16-byte boundaries
     int y16;                   // 1: y is FP16
     int y_vec;                 // 1: rows of y begin on 16-byte boundaries
-    int x16, x_vec;            // of raw, 1: FP16; rows begin on 16-byte boundaries
-    int w_fits;                // 1: rows of w begin on 16-byte boundaries, k is a multiple of 16, the pitch is at most 2^22
-    int aligned;               // 1: so do those of x
+    int w_fits;                // 1: rows of w begin on 16-byte boundaries, k is a multiple of 16, the pitch is at most kMostPitch
 };
 
 struct QuantizeArgs {
@@ -36,14 +36,22 @@ struct QuantizeArgs {
     long long ldx;
     int m, k;
     int x16;                   // 1: x is FP16
-    int vec;                   // 1: rows of x begin on 16-byte boundaries
     int8_t *q;                 // [m][pitch]
     float *s;                  // [m]
     long long pitch;
 };
 
-bool linear_quantizes(const LinearArgs &a);      // whether the kernel for these sizes takes values of x
+struct AlignArgs {
+    const int8_t *from;
+    int8_t *to;                // [rows][pitch]
+    long long rows, ld, pitch;
+    int k;
+};
+
+bool linear_few(const LinearArgs &a, int size);   // whether x with elements of so many bytes may be given as raw (or as x)
+bool linear_rows(const LinearArgs &a);            // whether x may be given as raw for its short rows (w has to fit)
 int launch_quantize_rows(const QuantizeArgs &a, void *stream);
+int launch_align_rows(const AlignArgs &a, void *stream);
 int launch_linear(const LinearArgs &a, void *stream);
 
 }  // namespace fq

@@ -18,32 +18,60 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
-// Values [at, at + 8) of a row of k; zeros behind its end.
-template <typename T> __device__ __forceinline__ void load8(const T *row, int at, int k, bool vec, float *v)
+// L lanes have a row, V vectors of eight values each: vectors l, l + L, l + 2 L, ... to lane l.  All of them are asked for at
+// once, by loads that no lane branches round (any address will do; lanes without eight values take the row's first, which
+// leaves its greatest magnitude as it is, and with k < 8 all take `spare`, 32 bytes of no matter what).  An odd end is fetched
+// value by value.
+template <typename T> struct Eight { i32x4 w[sizeof(T) / 2]; };
+template <typename T> struct Values { typedef T type __attribute__((ext_vector_type(8))); };
+
+template <typename T> __device__ __forceinline__ Eight<T> ask8(const T *row, int at, int k, const void *spare)
 {
-    if (vec && at + 8 <= k) {
-        if constexpr (sizeof(T) == 2) {
-            const f16x8 h = *(const FQ_GLOBAL f16x8 *)(row + at);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = (float)h[e];
-        } else {
-            const f32x4 a = *(const FQ_GLOBAL f32x4 *)(row + at), b = *(const FQ_GLOBAL f32x4 *)(row + at + 4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[e + 4] = b[e]; }
-        }
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = at + e < k ? (float)ld_global(row + at + e) : 0.0f;
+    Eight<T> r;
+    const T *p = k >= 8 ? row + (at + 8 <= k ? at : 0) : (const T *)spare;
+    __builtin_memcpy(&r, (const FQ_GLOBAL T *)p, sizeof r);
+    return r;
 }
 
-// Greatest magnitude of eight values, as bits (magnitudes order like their bits: NaN, infinity, numbers).
-__device__ __forceinline__ unsigned most8(const float *v)
+template <typename T> __device__ __forceinline__ void odd_end(Eight<T> &r, const T *row, int at, int k)
 {
-    unsigned most = 0;
+    if (k % 8 == 0 || at + 8 <= k) return;
+    typename Values<T>::type h = (typename Values<T>::type)(T)0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) most = max(most, __builtin_bit_cast(unsigned, v[e]) & 0x7FFFFFFFu);
+    for (int e = 0; e < 8; ++e)
+        if (at + e < k) h[e] = ld_global(row + at + e);
+    r = __builtin_bit_cast(Eight<T>, h);
+}
+
+// Greatest magnitude of the vectors, as the bits of a float (magnitudes order like their bits: numbers, infinity, NaN).
+template <typename T, int V> __device__ __forceinline__ unsigned most_of(const Eight<T> (&r)[V])
+{
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    unsigned most = 0;
+    if constexpr (sizeof(T) == 2) {
+        u16x2 both = (u16x2)(unsigned short)0;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) both = __builtin_elementwise_max(both, __builtin_bit_cast(u16x2, r[j].w[0][e] & 0x7FFF7FFF));
+        const unsigned short half = both[0] > both[1] ? both[0] : both[1];
+        most = __builtin_bit_cast(unsigned, (float)__builtin_bit_cast(_Float16, half));
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most = max(most, (unsigned)r[j].w[e / 4][e % 4] & 0x7FFFFFFFu);
+    }
     return most;
+}
+
+// The greatest of the 16 lanes' values that a row of the DPP unit holds, in all of them.
+__device__ __forceinline__ unsigned max16(unsigned v)
+{
+    v = dpp_max<0xB1, 0xf>(v);
+    v = dpp_max<0x4E, 0xf>(v);
+    v = dpp_max<0x141, 0xf>(v);
+    return dpp_max<0x140, 0xf>(v);
 }
 
 struct RowScale {
@@ -62,89 +90,91 @@ __device__ __forceinline__ RowScale row_scale(unsigned most)
 // Codes of eight values.  x * (1 / s) is within 127 * 2^-22.4 of the quotient x / s, so unless it lies that near to a
 // half (a few vectors of a row) it rounds to the same integer.  Adding 1.5 * 2^23 rounds it, to even, and leaves the code in
 // the low byte.  No code leaves [-127, 127]: no |x| is over 127 * s * (1 + 2^-24).
-__device__ __forceinline__ u32x2 codes8(const float *v, RowScale r)
+template <typename T> __device__ __forceinline__ u32x2 codes8(const Eight<T> &r, RowScale scale, bool none)
 {
     constexpr float kMagic = 0x1.8p23f;
+    const auto v = __builtin_bit_cast(typename Values<T>::type, r);
     unsigned b[8];
     float near = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float t = v[e] * r.inverse, f = t + kMagic;
+        const float t = (float)v[e] * scale.inverse, f = t + kMagic;
         b[e] = __builtin_bit_cast(unsigned, f);
         near = __builtin_fmaxf(near, __builtin_fabsf(t - (f - kMagic)));
     }
     if (near > 0.49995f) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) b[e] = __builtin_bit_cast(unsigned, v[e] / r.s + kMagic);
+        for (int e = 0; e < 8; ++e) b[e] = __builtin_bit_cast(unsigned, (float)v[e] / scale.s + kMagic);
     }
     const auto pack = [](unsigned p, unsigned q, unsigned s, unsigned t) {
         return __builtin_amdgcn_perm(__builtin_amdgcn_perm(t, s, 0x0c0c0400u), __builtin_amdgcn_perm(q, p, 0x0c0c0400u), 0x05040100u);
     };
     u32x2 w = u32x2{pack(b[0], b[1], b[2], b[3]), pack(b[4], b[5], b[6], b[7])};
-    if (r.inverse == 0.0f) w = (u32x2)0u;
+    if (none || scale.inverse == 0.0f) w = (u32x2)0u;
     return w;
 }
 
-// THREADS of a block have a row, HELD vectors of eight each: read once, kept in registers.  Longer rows are read again
-// for the codes.
-template <typename T, int THREADS, int HELD>
+// A row to L lanes.  Rows of more than 8 * L * V values are read again for the codes.
+template <typename T, int L, int V>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs a)
 {
     __shared__ unsigned top[4];
-    const int at = threadIdx.x % THREADS;
-    const long long row = (long long)blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS;
-    if (THREADS < 256 && row >= a.m) return;
-    const T *x = (const T *)a.x + row * a.ldx;
-    float v[HELD][8];
-    unsigned most = 0;
+    const int at = threadIdx.x % L * 8;
+    const long long row = (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
+    const T *x = (const T *)a.x + min(row, (long long)a.m - 1) * a.ldx;
+    Eight<T> raw[V];
 #pragma unroll
-    for (int j = 0; j < HELD; ++j) load8(x, (j * THREADS + at) * 8, a.k, a.vec, v[j]);
+    for (int j = 0; j < V; ++j) raw[j] = ask8(x, j * L * 8 + at, a.k, a.q);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int j = 0; j < HELD; ++j) most = max(most, most8(v[j]));
-    for (int i = (HELD * THREADS + at) * 8; i < a.k; i += THREADS * 8) {
-        float more[8];
-        load8(x, i, a.k, a.vec, more);
-        most = max(most, most8(more));
+    for (int j = 0; j < V; ++j) odd_end(raw[j], x, j * L * 8 + at, a.k);
+    unsigned most = most_of(raw);
+    for (int i = V * L * 8 + at; i < a.k; i += L * 8) {
+        Eight<T> more[1] = {ask8(x, i, a.k, a.q)};
+        odd_end(more[0], x, i, a.k);
+        most = max(most, most_of(more));
     }
-    most = wave_max(most);
-    if (THREADS == 256) {
+    most = L == 16 ? max16(most) : wave_max(most);
+    if (L == 256) {
         if ((threadIdx.x & 63) == 0) top[threadIdx.x >> 6] = most;
         __syncthreads();
         most = max(max(top[0], top[1]), max(top[2], top[3]));
     }
     const RowScale r = row_scale(most);
+    if (row >= a.m) return;
     if (at == 0) st_global(a.s + row, r.s);
     int8_t *q = a.q + row * a.pitch;
 #pragma unroll
-    for (int j = 0; j < HELD; ++j) {
-        const int i = (j * THREADS + at) * 8;
-        if (i < a.pitch) *(FQ_GLOBAL u32x2 *)(q + i) = codes8(v[j], r);
+    for (int j = 0; j < V; ++j) {
+        const int i = j * L * 8 + at;
+        if (i < a.pitch) *(FQ_GLOBAL u32x2 *)(q + i) = codes8(raw[j], r, i >= a.k);
     }
-    for (int i = (HELD * THREADS + at) * 8; i < a.pitch; i += THREADS * 8) {
-        float more[8];
-        load8(x, i, a.k, a.vec, more);
-        *(FQ_GLOBAL u32x2 *)(q + i) = codes8(more, r);
+    for (int i = V * L * 8 + at; i < a.pitch; i += L * 8) {
+        Eight<T> more = ask8(x, i, a.k, a.q);
+        odd_end(more, x, i, a.k);
+        *(FQ_GLOBAL u32x2 *)(q + i) = codes8(more, r, i >= a.k);
     }
 }
 
 // ---------------------------------------------------------------------------------------------
-// 16 codes at any address.
-__device__ __forceinline__ i32x4 load16(const int8_t *p)
+// Rows of codes at any address, laid out anew for the tiles: on 16-byte boundaries, zeros behind k.  A thread moves 16.
+__global__ __launch_bounds__(256) void align_rows_kernel(AlignArgs a)
 {
-    i32x4 r;
-    __builtin_memcpy(&r, (const FQ_GLOBAL int8_t *)p, 16);
-    return r;
-}
-
-// 16 codes of a row of k from l on; zeros behind its end.
-__device__ __forceinline__ i32x4 load16(const int8_t *row, int l, int k)
-{
+    const unsigned each = (unsigned)(a.pitch / 16);
+    const unsigned long long i = (unsigned long long)blockIdx.x * 256 + threadIdx.x;
+    const long long row = (long long)(i / each);
+    const int l = (int)(i % each) * 16;
+    if (row >= a.rows) return;
+    const int8_t *from = a.from + row * a.ld + l;
     i32x4 r = {0, 0, 0, 0};
-    if (l + 16 <= k) return load16(row + l);
+    if (l + 16 <= a.k) {
+        __builtin_memcpy(&r, (const FQ_GLOBAL int8_t *)from, 16);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 16; ++j)
-        if (l + j < k) r[j / 4] |= (int)((unsigned)(unsigned char)ld_global(row + l + j) << (8 * (j % 4)));
-    return r;
+        for (int j = 0; j < 16; ++j)
+            if (l + j < a.k) r[j / 4] |= (int)((unsigned)(unsigned char)ld_global(from + j) << (8 * (j % 4)));
+    }
+    *(FQ_GLOBAL i32x4 *)(a.to + row * a.pitch + l) = r;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -182,13 +212,13 @@ __device__ __forceinline__ void load_lds(i32x4 buffer, unsigned off, int8_t *to)
 
 template <int N, int WAVES> struct Staging {                    // N wavefront loads of a panel per wavefront and step
     unsigned off[N];
-    i32x4 held[N];
 
-    __device__ __forceinline__ void place(long long ld, int lane, int wave)
+    // (shift: where in 16 bytes the first row begins; a row's loads begin at the boundary in front of it)
+    __device__ __forceinline__ void place(long long ld, int lane, int wave, unsigned shift = 0)
     {
 #pragma unroll
         for (int j = 0; j < N; ++j)
-            off[j] = (unsigned)((j * WAVES + wave) * 8 + lane / 8) * (unsigned)ld + (unsigned)((lane % 8) ^ (lane / 8)) * 16;
+            off[j] = (((unsigned)((j * WAVES + wave) * 8 + lane / 8) * (unsigned)ld + shift) & ~15u) + (unsigned)((lane % 8) ^ (lane / 8)) * 16;
     }
     // Load J of codes [at, at + kDepth) of the panel's rows into LDS; lanes with `none` fetch zeros.
     __device__ __forceinline__ void fetch(const Panel &p, int at, int j, int8_t *to, int wave, bool none)
@@ -197,22 +227,6 @@ template <int N, int WAVES> struct Staging {                    // N wavefront l
         const uint64_t from = (uint64_t)(p.at + at);
         const i32x4 r = {(int)from, (int)(from >> 32) & 0xFFFF, (int)(p.bytes - (unsigned)at), 0x00027000};
         load_lds(r, none ? kNowhere : off[j], to + (j * WAVES + wave) * 1024);
-    }
-    // The same by way of registers, for rows at any address.
-    __device__ __forceinline__ void request(const int8_t *base, long long ld, int row0, int rows, int at, int k, int lane, int wave)
-    {
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int row = min(row0 + (j * WAVES + wave) * 8 + lane / 8, rows - 1);
-            const int8_t *from = base + (long long)row * ld;
-            const int l = at + ((lane % 8) ^ (lane / 8)) * 16;
-            held[j] = at + kDepth <= k ? load16(from + l) : load16(from, l, k);
-        }
-    }
-    __device__ __forceinline__ void put(int8_t *to, int lane, int wave)
-    {
-#pragma unroll
-        for (int j = 0; j < N; ++j) *(i32x4 *)(to + (j * WAVES + wave) * 1024 + lane * 16) = held[j];
     }
 };
 
@@ -251,6 +265,32 @@ __device__ __forceinline__ void store8(const LinearArgs &a, long long i, int j, 
         if (j + e < a.n) st_global(to + e, y[e]);
 }
 
+// The same of 4 channels.
+__device__ __forceinline__ void store4(const LinearArgs &a, long long i, int j, const float *y)
+{
+    if (a.y16) {
+        _Float16 *to = (_Float16 *)a.y + i * a.ldy + j;
+        typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+        const f16x4 v = {(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
+        if (a.y_vec && j + 4 <= a.n) {
+            *(FQ_GLOBAL f16x4 *)to = v;
+            return;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (j + e < a.n) st_global(to + e, v[e]);
+        return;
+    }
+    float *to = (float *)a.y + i * a.ldy + j;
+    if (a.y_vec && j + 4 <= a.n) {
+        *(FQ_GLOBAL f32x4 *)to = f32x4{y[0], y[1], y[2], y[3]};
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (j + e < a.n) st_global(to + e, y[e]);
+}
+
 // Tile of a block.  Blocks go to the eight XCDs in turn: each gets neighbouring tiles, in groups kGroup token tiles
 // high, so that what its L2 holds of x and w serves many of them.
 constexpr int kXcds = 8, kGroup = 4;
@@ -270,13 +310,13 @@ template <int LEFT> __device__ __forceinline__ void loads_and_barrier()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(LEFT) : "memory");
 }
 
-template <int BM, int BN, int WM, int WN, int STAGES, bool ALIGNED>
+template <int BM, int BN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
 {
     constexpr int WAVES = WM * WN, TM = BM / WM / 32, TN = BN / WN / 32;
     constexpr int kPitch = TN * 32 + 4;                         // of the sums in LDS
     constexpr int kStage = (BM + BN) * kDepth, kLoads = (BM + BN) / 8 / WAVES;
-    static_assert(STAGES >= 2 && STAGES <= 4 && (STAGES == 2 || ALIGNED), "stages");
+    static_assert(STAGES >= 2 && STAGES <= 4, "stages");
     static_assert(WAVES * 32 * kPitch * 4 <= 2 * kStage, "the sums of a wavefront's 32 tokens fit in its share");
     // (separate arrays: the compiler then knows that a write of one leaves the others alone)
     __shared__ __attribute__((aligned(1024))) int8_t stage0[kStage], stage1[kStage], stage2[STAGES > 2 ? kStage : 16], stage3[STAGES > 3 ? kStage : 16];
@@ -295,11 +335,9 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
 
     Staging<BN / 8 / WAVES, WAVES> w;
     Staging<BM / 8 / WAVES, WAVES> x;
-    const Panel pw = panel(a.w, a.ldw, n0, BN, a.n - n0, a.k), px = panel(a.x, a.ldx, m0, BM, a.m - m0, a.kx);
-    if constexpr (ALIGNED) {
-        w.place(a.ldw, lane, wave);
-        x.place(a.ldx, lane, wave);
-    }
+    const Panel pw = panel(a.w, a.ldw, n0, BN, a.n - n0, a.kw), px = panel(a.x, a.ldx, m0, BM, a.m - m0, a.kx);
+    w.place(a.ldw, lane, wave);
+    x.place(a.ldx, lane, wave);
     const int steps = (a.k + kDepth - 1) / kDepth;
     const int mine16 = ((lane % 8) ^ (lane / 8)) * 16;          // where in a step this lane's 16 codes lie
     // Loads [from, to) of the kLoads of a step.
@@ -314,25 +352,10 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
         }
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto ask_slowly = [&](int step) {
-        if (step >= steps) return;
-        w.request(a.w, a.ldw, n0, a.n, step * kDepth, a.k, lane, wave);
-        x.request(a.x, a.ldx, m0, a.m, step * kDepth, a.k, lane, wave);
-        __builtin_amdgcn_sched_barrier(0);
-    };
     // The codes of step `step` are in LDS for all; those of the STAGES - 2 steps behind it may be on their way.
-    auto have = [&](auto sure, int step, int8_t *to) {
-        if constexpr (!ALIGNED) {
-            if (step < steps) {
-                w.put(to, lane, wave);
-                x.put(to + BN * kDepth, lane, wave);
-            }
-            __syncthreads();
-        } else if (sure || step + STAGES - 2 < steps) {
-            loads_and_barrier<(STAGES - 2) * kLoads>();
-        } else {
-            loads_and_barrier<0>();
-        }
+    auto have = [&](auto sure, int step) {
+        if (sure || step + STAGES - 2 < steps) loads_and_barrier<(STAGES - 2) * kLoads>();
+        else loads_and_barrier<0>();
     };
     i32x16 sum[TN][TM];
 #pragma unroll
@@ -360,7 +383,7 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
         for (int p = 0; p < TM * TN; ++p) {
             const int j = p / TM, i = p % TM, at = q * TM * TN + p;
             sum[j][i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(c.w[j], c.x[i], sum[j][i], 0, 0, 0);
-            if constexpr (ALIGNED && STAGES > 2 && q < 3) {
+            if constexpr (STAGES > 2 && q < 3) {
                 __builtin_amdgcn_sched_barrier(0);
                 ask(sure, step, into, at * kLoads / kOf, (at + 1) * kLoads / kOf);
             }
@@ -379,27 +402,23 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
         constexpr std::integral_constant<int, i + 1> ahead{};
         constexpr std::integral_constant<int, i + STAGES - 1> last{};
         const int8_t *from = stage(i);
-        int8_t *next = stage(ahead), *into = stage(last);
-        if constexpr (!ALIGNED) ask_slowly(step + 1);
-        else if constexpr (STAGES == 2) ask(all, step + 1, into, 0, kLoads);
+        const int8_t *next = stage(ahead);
+        int8_t *into = stage(last);
+        if constexpr (STAGES == 2) ask(all, step + 1, into, 0, kLoads);
         read(from, 1, then);
         multiply(all, k0, now, step + STAGES - 1, into);
         read(from, 2, now);
         multiply(all, k1, then, step + STAGES - 1, into);
         read(from, 3, then);
         multiply(all, k2, now, step + STAGES - 1, into);
-        have(all, step + 1, next);
+        have(all, step + 1);
         read(next, 0, now);
         multiply(all, k3, then, 0, nullptr);
     };
-    if constexpr (ALIGNED) {
-        ask(maybe, 0, stage0, 0, kLoads);
-        if constexpr (STAGES > 2) ask(maybe, 1, stage1, 0, kLoads);
-        if constexpr (STAGES > 3) ask(maybe, 2, stage2, 0, kLoads);
-    } else {
-        ask_slowly(0);
-    }
-    have(maybe, 0, stage0);
+    ask(maybe, 0, stage0, 0, kLoads);
+    if constexpr (STAGES > 2) ask(maybe, 1, stage1, 0, kLoads);
+    if constexpr (STAGES > 3) ask(maybe, 2, stage2, 0, kLoads);
+    have(maybe, 0);
     read(stage0, 0, now);
     int step = 0;
     auto round = [&](auto all) {
@@ -464,21 +483,27 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
 // wavefront has kRing steps of w of its own in LDS or on their way there, so it waits for nobody; the layout is that of the
 // tiles above.  x lies in LDS as a whole: fetched in front of w, and with X FP16 or FP32 turned into codes by the block while
 // w is still coming.
+// Rows that do not begin on 16-byte boundaries (SHIFTED: of w or x) are fetched from the boundary in front of them on.  A step then
+// is 112 codes, and the 16 of a lane are cut out of two neighbouring 16 bytes; the last quarter of the second product has
+// zeros for x.
 constexpr int kFewWaves = 8, kRing = 4;
 
 struct FewLds {                                                 // where things lie, in bytes behind the rings
-    int raw_pitch, raw, code_pitch, codes, total;
+    int use, steps, pieces, raw_pitch, raw, code_pitch, codes, total;
 };
 
-__host__ __device__ constexpr FewLds few_lds(int m, int k, int size)
+__host__ __device__ constexpr FewLds few_lds(int m, int k, int size, bool shifted)
 {
     FewLds l = {};
-    const int ring = kFewWaves * kRing * 16 * kDepth;
-    l.raw = ring;
-    l.raw_pitch = (k * size + 1023) / 1024 * 1024 + 16;          // (rows of 16 lanes begin in different banks)
-    l.code_pitch = size > 1 ? (k + kDepth - 1) / kDepth * kDepth + 16 : l.raw_pitch;
+    l.use = shifted ? kDepth - 16 : kDepth;
+    l.steps = (k + l.use - 1) / l.use;
+    l.raw = kFewWaves * kRing * 16 * kDepth;
+    // (of a row of x: values as they lie in memory from a 16-byte boundary on, or codes with zeros to the end of the last step)
+    l.pieces = ((size > 1 ? k * size + 15 : l.steps * l.use) + 1023) / 1024;
+    l.raw_pitch = l.pieces * 1024 + 16;                          // (rows of 16 lanes begin in different banks)
+    l.code_pitch = size > 1 ? l.steps * l.use + 32 - (l.steps * l.use % 32 == 0 ? 16 : 0) : l.raw_pitch;
     l.codes = size > 1 ? l.raw + m * l.raw_pitch : l.raw;
-    l.total = l.codes + m * l.code_pitch;
+    l.total = l.codes + m * l.code_pitch + 32;                   // (a shifted last step reads 16 codes more)
     return l;
 }
 
@@ -490,16 +515,36 @@ template <int LEFT> __device__ __forceinline__ void loads_but()
 
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }
 
-template <typename X>
+// Bytes [o, o + 16) of 32.
+__device__ __forceinline__ i32x4 cut16(i32x4 low, i32x4 high, int o)
+{
+    const auto pick = [](int which, int no, int yes) { return which ? yes : no; };
+    int t[7], e[5];
+#pragma unroll
+    for (int j = 0; j < 3; ++j) {
+        t[j] = pick(o & 4, low[j], low[j + 1]);
+        t[j + 4] = pick(o & 4, high[j], high[j + 1]);
+    }
+    t[3] = pick(o & 4, low[3], high[0]);
+#pragma unroll
+    for (int j = 0; j < 5; ++j) e[j] = pick(o & 8, t[j], t[j + 2]);
+    i32x4 r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[j] = (int)__builtin_amdgcn_alignbyte((unsigned)e[j + 1], (unsigned)e[j], (unsigned)o & 3u);
+    return r;
+}
+
+template <typename X, bool SHIFTED>
 __global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs a)
 {
     constexpr int WAVES = kFewWaves, kPitch = 17;                // (of 16 channels' sums in LDS)
     constexpr bool kQuantize = sizeof(X) > 1;
+    constexpr int kUse = SHIFTED ? kDepth - 16 : kDepth;
     extern __shared__ __attribute__((aligned(1024))) int8_t lds[];
     __shared__ int sums[16 * kPitch];
     __shared__ unsigned top[16];
     __shared__ float scales[16];
-    const FewLds at = few_lds(a.m, a.k, sizeof(X));
+    const FewLds at = few_lds(a.m, a.k, sizeof(X), SHIFTED);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n0 = (int)blockIdx.x * 16;
     // this thread's output: asked for first, used last
@@ -514,27 +559,29 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs a
     if (threadIdx.x < 16 * kPitch) sums[threadIdx.x] = 0;
     if (threadIdx.x < 16) top[threadIdx.x] = 0;
 
-    // x: 1 KiB of a row to a load, zeros behind its end
-    const int row_bytes = a.k * (int)sizeof(X), pieces = (row_bytes + 1023) / 1024;
-    const int8_t *xb = kQuantize ? (const int8_t *)a.raw : a.x;
-    for (int i = wave; i < a.m * pieces; i += WAVES) {
-        const int row = i / pieces, from = i % pieces * 1024;
-        const uint64_t p = (uint64_t)(xb + (long long)row * a.ldx * (int)sizeof(X) + from);
-        const i32x4 r = {(int)p, (int)(p >> 32) & 0xFFFF, row_bytes - from, 0x00027000};
+    // x: 1 KiB of a row to a load, zeros behind the 16 bytes with its end
+    auto row_of_x = [&](int row) { return (uint64_t)(kQuantize ? (const int8_t *)a.raw : a.x) + (uint64_t)row * (uint64_t)a.ldx * sizeof(X); };
+    for (int i = wave; i < a.m * at.pieces; i += WAVES) {
+        const int row = i / at.pieces, from = i % at.pieces * 1024;
+        const uint64_t begins = row_of_x(row), p = (begins & ~15ull) + from;
+        const int bytes = max(0, ((int)(begins & 15) + a.k * (int)sizeof(X) + 15) / 16 * 16 - from);
+        const i32x4 r = {(int)p, (int)(p >> 32) & 0xFFFF, bytes, 0x00027000};
         load_lds(r, (unsigned)lane * 16, lds + at.raw + row * at.raw_pitch + from);
     }
     // w
-    const int steps = (a.k + kDepth - 1) / kDepth, each = (steps + WAVES - 1) / WAVES;
-    const int begin = min(steps, wave * each), end = min(steps, begin + each);
+    const int each = (at.steps + WAVES - 1) / WAVES;
+    const int begin = min(at.steps, wave * each), end = min(at.steps, begin + each);
     int8_t *const ring = lds + wave * (kRing * 16 * kDepth);
-    const Panel pw = panel(a.w, a.ldw, n0, 16, a.n - n0, a.k);
+    const int8_t *const w0 = a.w + (long long)n0 * a.ldw;
+    const int shift0 = SHIFTED ? (int)((uint64_t)w0 & 15) : 0;
+    const Panel pw = {w0 - shift0, ((unsigned)(min(16, a.n - n0) - 1) * (unsigned)a.ldw + (unsigned)(shift0 + a.k) + 15) / 16 * 16};
     Staging<2, 1> w;
-    w.place(a.ldw, lane, 0);
+    w.place(a.ldw, lane, 0, (unsigned)shift0);
     auto ask = [&](int step) {
         if (step >= end) return;
         int8_t *to = ring + (step - begin) % kRing * (16 * kDepth);
-        w.fetch(pw, step * kDepth, 0, to, 0, false);
-        w.fetch(pw, step * kDepth, 1, to, 0, false);
+        w.fetch(pw, step * kUse, 0, to, 0, false);
+        w.fetch(pw, step * kUse, 1, to, 0, false);
     };
 #pragma unroll
     for (int j = 0; j < kRing; ++j) ask(begin + j);
@@ -551,50 +598,55 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs a
 
     if constexpr (kQuantize) {
         // (row, part) pairs go round the wavefronts
-        constexpr int kEach = 8;
         const int parts = max(1, WAVES / a.m), span = ((a.k + parts - 1) / parts + 511) / 512 * 512;
-        auto values = [&](int row, int from, float *v) {
-            const X *p = (const X *)(lds + at.raw + row * at.raw_pitch) + from;
+        auto values = [&](const X *p, bool whole, int from) {
+            if (!SHIFTED || (whole && from + 8 <= a.k)) return *(const Eight<X> *)__builtin_assume_aligned(p + from, 16);
+            typename Values<X>::type v;
 #pragma unroll
-            for (int e = 0; e < kEach; ++e) v[e] = (float)p[e];
+            for (int e = 0; e < 8; ++e) v[e] = from + e < a.k ? p[from + e] : (X)0;
+            return __builtin_bit_cast(Eight<X>, v);
         };
+        const int padded = at.steps * kUse;
         for (int i = wave; i < a.m * parts; i += WAVES) {
-            const int row = i / parts, from = i % parts * span;
+            const int row = i / parts, from = i % parts * span, shift = (int)(row_of_x(row) & 15);
+            const X *p = (const X *)(lds + at.raw + row * at.raw_pitch + shift);
             unsigned most = 0;
-            for (int l = from + lane * kEach; l < min(from + span, a.k); l += 64 * kEach) {
-                float v[kEach];
-                values(row, l, v);
-                most = max(most, most8(v));
+            for (int l = from + lane * 8; l < min(from + span, a.k); l += 512) {
+                const Eight<X> v[1] = {values(p, shift == 0, l)};
+                most = max(most, most_of(v));
             }
             most = wave_max(most);
             if (lane == 0) atomicMax(&top[row], most);
         }
         lds_barrier();
         for (int i = wave; i < a.m * parts; i += WAVES) {
-            const int row = i / parts, from = i % parts * span;
+            const int row = i / parts, from = i % parts * span, shift = (int)(row_of_x(row) & 15);
+            const X *p = (const X *)(lds + at.raw + row * at.raw_pitch + shift);
             const RowScale r = row_scale(top[row]);
             if (lane == 0) scales[row] = r.s;
-            for (int l = from + lane * kEach; l < min(from + span, steps * kDepth); l += 64 * kEach) {
-                float v[kEach];
-                if (l < a.k) values(row, l, v);
-                else
-#pragma unroll
-                    for (int e = 0; e < kEach; ++e) v[e] = 0.0f;
-                *(u32x2 *)(lds + at.codes + row * at.code_pitch + l) = codes8(v, r);
-            }
+            // (the last part also fills up the last step)
+            const int to = i % parts == parts - 1 ? padded : min(from + span, padded);
+            for (int l = from + lane * 8; l < to; l += 512)
+                *(u32x2 *)(lds + at.codes + row * at.code_pitch + l) = codes8(values(p, shift == 0, min(l, a.k)), r, l >= a.k);
         }
         lds_barrier();
     }
 
     const int8_t *x = lds + at.codes + min(lane % 16, a.m - 1) * at.code_pitch + lane / 16 * 16;
+    const int shift = SHIFTED ? (int)((uint64_t)(w0 + (long long)(lane % 16) * a.ldw) & 15) : 0;
     i32x4 sum = (i32x4)0;
     for (int step = begin; step < end; ++step) {
         arrived(min(kRing - 1, end - 1 - step));
         const int8_t *from = ring + (step - begin) % kRing * (16 * kDepth) + lane % 16 * kDepth;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const i32x4 cw = *(const i32x4 *)(from + ((4 * s + lane / 16) ^ (lane % 8)) * 16);
-            const i32x4 cx = *(const i32x4 *)(x + step * kDepth + 64 * s);
+            const int c = 4 * s + lane / 16;
+            i32x4 cw = *(const i32x4 *)(from + (c ^ (lane % 8)) * 16);
+            i32x4 cx = *(const i32x4 *)(x + step * kUse + 64 * s);
+            if (SHIFTED) {
+                cw = cut16(cw, *(const i32x4 *)(from + (((c + 1) & 7) ^ (lane % 8)) * 16), shift);
+                if (c == 7) cx = (i32x4)0;
+            }
             sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(cw, cx, sum, 0, 0, 0);
         }
         if (step + kRing < end) {
@@ -614,29 +666,154 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs a
     else st_global((float *)a.y + (long long)out_m * a.ldy + out_n, y);
 }
 
+// Whether all rows of x and w begin on 16-byte boundaries and consist of whole 16 values.
+bool few_fits(const LinearArgs &a) { return a.w_fits && (!a.raw || a.x_vec); }
+
 template <typename X> int launch_few(const LinearArgs &a, void *stream)
 {
-    const int lds = few_lds(a.m, a.k, sizeof(X)).total;
-    linear_few_kernel<X><<<((unsigned)a.n + 15) / 16, kFewWaves * 64, (size_t)lds, (hipStream_t)stream>>>(a);
+    const unsigned blocks = ((unsigned)a.n + 15) / 16;
+    const size_t lds = (size_t)few_lds(a.m, a.k, sizeof(X), !few_fits(a)).total;
+    if (few_fits(a)) linear_few_kernel<X, false><<<blocks, kFewWaves * 64, lds, (hipStream_t)stream>>>(a);
+    else linear_few_kernel<X, true><<<blocks, kFewWaves * 64, lds, (hipStream_t)stream>>>(a);
+    return (int)hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------------------------
+// Short rows, many tokens: x is read once and its codes never leave the compute unit.  A block has TOK * 16 tokens.  It turns
+// them into codes in LDS, a row to 16 lanes, V vectors each, with all of a wavefront's rows requested before the first is
+// looked at; then every wavefront multiplies all of them by 16 * CH channels at a time.  w, small enough to stay in the L2s,
+// goes from there into registers, whole rows of it: the first before x is quantized, the next as the last are used up.
+constexpr int kRowsWaves = 8, kRowsMostK = 512;
+
+template <typename X, int TOK, int CH, int V>
+__global__ __launch_bounds__(kRowsWaves * 64) void linear_rows_kernel(LinearArgs a)
+{
+    constexpr int WAVES = kRowsWaves, kRows = TOK * 16, kPasses = (kRows + 4 * WAVES - 1) / (4 * WAVES), kSteps = V * 2;
+    __shared__ __attribute__((aligned(16))) int8_t codes[kRows * (kSteps * 64 + 16)];
+    __shared__ float scales[kRows];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m0 = (int)blockIdx.x * kRows, steps = (a.k + 63) / 64, pitch = steps * 64 + 16;
+
+    auto row_of = [&](int r) { return (r * WAVES + wave) * 4 + lane / 16; };
+    auto row_of_x = [&](int r) { return (const X *)a.raw + (long long)min(m0 + row_of(r), a.m - 1) * a.ldx; };
+    Eight<X> raw[kPasses][V];
+#pragma unroll
+    for (int r = 0; r < kPasses; ++r)
+        if ((r * WAVES + wave) * 4 < kRows)
+#pragma unroll
+            for (int j = 0; j < V; ++j) raw[r][j] = ask8(row_of_x(r), (j * 16 + lane % 16) * 8, a.k, a.w);
+    __builtin_amdgcn_sched_barrier(0);
+    const int tiles = (a.n + 16 * CH - 1) / (16 * CH);
+    i32x4 cw[kSteps][CH];
+    auto load_w = [&](int tile, int step) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int8_t *row = a.w + (long long)min((tile * CH + c) * 16 + lane % 16, a.n - 1) * a.ldw;
+            cw[step][c] = ld_global((const i32x4 *)(row + min(step * 64 + lane / 16 * 16, a.kw - 16)));      // (behind k the codes of x are 0)
+        }
+    };
+    if (wave < tiles)
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j)
+            if (j < steps) load_w(wave, j);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int r = 0; r < kPasses; ++r) {
+        if ((r * WAVES + wave) * 4 >= kRows) continue;
+#pragma unroll
+        for (int j = 0; j < V; ++j) odd_end(raw[r][j], row_of_x(r), (j * 16 + lane % 16) * 8, a.k);
+        const RowScale scale = row_scale(max16(most_of(raw[r])));
+        if (lane % 16 == 0) scales[row_of(r)] = scale.s;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const int l = (j * 16 + lane % 16) * 8;
+            if (l < steps * 64) *(u32x2 *)(codes + row_of(r) * pitch + l) = codes8(raw[r][j], scale, l >= a.k);
+        }
+    }
+    __syncthreads();
+
+    const int8_t *x = codes + lane % 16 * pitch + lane / 16 * 16;
+    for (int tile = wave; tile < tiles; tile += WAVES) {
+        i32x4 sum[CH][TOK];
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int t = 0; t < TOK; ++t) sum[c][t] = (i32x4)0;
+#pragma unroll
+        for (int j = 0; j < kSteps; ++j) {
+            if (j >= steps) continue;
+#pragma unroll
+            for (int t = 0; t < TOK; ++t) {
+                const i32x4 cx = *(const i32x4 *)(x + t * 16 * pitch + j * 64);
+#pragma unroll
+                for (int c = 0; c < CH; ++c) sum[c][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(cw[j][c], cx, sum[c][t], 0, 0, 0);
+            }
+            if (tile + WAVES < tiles) load_w(tile + WAVES, j);
+        }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int n = (tile * CH + c) * 16 + lane / 16 * 4;
+            float ws[4], bias[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = min(n + e, a.n - 1);
+                ws[e] = ld_global(a.ws + (long long)j * a.ws_step);
+                bias[e] = a.bias ? ld_global(a.bias + j) : 0.0f;
+            }
+            if (n >= a.n) continue;
+#pragma unroll
+            for (int t = 0; t < TOK; ++t) {
+                const int m = m0 + t * 16 + lane % 16;
+                const float xs = scales[t * 16 + lane % 16];
+                float y[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    y[e] = (float)sum[c][t][e] * (xs * ws[e]);
+                    if (a.bias) y[e] += bias[e];
+                }
+                if (m < a.m) store4(a, m, n, y);
+            }
+        }
+    }
+}
+
+template <typename X, int TOK, int CH> int launch_rows_of(const LinearArgs &a, void *stream)
+{
+    const unsigned blocks = (unsigned)(((long long)a.m + TOK * 16 - 1) / (TOK * 16));
+    if (a.k <= 256) linear_rows_kernel<X, TOK, CH, 2><<<blocks, kRowsWaves * 64, 0, (hipStream_t)stream>>>(a);
+    else linear_rows_kernel<X, TOK, CH, 4><<<blocks, kRowsWaves * 64, 0, (hipStream_t)stream>>>(a);
     return (int)hipGetLastError();
 }
 
 template <int BM, int BN, int WM, int WN, int STAGES> int launch_tiles(const LinearArgs &a, void *stream)
 {
     const unsigned blocks = (unsigned)(((long long)a.m + BM - 1) / BM * (((long long)a.n + BN - 1) / BN));
-    if (a.aligned) linear_tile_kernel<BM, BN, WM, WN, STAGES, true><<<blocks, WM * WN * 64, 0, (hipStream_t)stream>>>(a);
-    else linear_tile_kernel<BM, BN, WM, WN, 2, false><<<blocks, WM * WN * 64, 0, (hipStream_t)stream>>>(a);
+    linear_tile_kernel<BM, BN, WM, WN, STAGES><<<blocks, WM * WN * 64, 0, (hipStream_t)stream>>>(a);
     return (int)hipGetLastError();
 }
 
 }  // namespace
 
+int launch_align_rows(const AlignArgs &a, void *stream)
+{
+    const unsigned long long pieces = (unsigned long long)a.rows * (unsigned long long)(a.pitch / 16);
+    align_rows_kernel<<<(unsigned)((pieces + 255) / 256), 256, 0, (hipStream_t)stream>>>(a);
+    return (int)hipGetLastError();
+}
+
+template <typename T, int L, int V> static int quantize_rows_by(const QuantizeArgs &a, void *stream)
+{
+    quantize_rows_kernel<T, L, V><<<(unsigned)(((long long)a.m + 256 / L - 1) / (256 / L)), 256, 0, (hipStream_t)stream>>>(a);
+    return (int)hipGetLastError();
+}
+
+// Short rows share a wavefront: what a row costs beside its values is then paid once for four.
 template <typename T> static int quantize_rows(const QuantizeArgs &a, void *stream)
 {
-    if (a.k <= 512) quantize_rows_kernel<T, 64, 1><<<((unsigned)a.m + 3) / 4, 256, 0, (hipStream_t)stream>>>(a);
-    else if (a.k <= 2048) quantize_rows_kernel<T, 64, 4><<<((unsigned)a.m + 3) / 4, 256, 0, (hipStream_t)stream>>>(a);
-    else quantize_rows_kernel<T, 256, 4><<<(unsigned)a.m, 256, 0, (hipStream_t)stream>>>(a);
-    return (int)hipGetLastError();
+    if (a.k <= 128) return quantize_rows_by<T, 16, 1>(a, stream);
+    if (a.k <= 512) return quantize_rows_by<T, 16, 4>(a, stream);
+    if (a.k <= 2048) return quantize_rows_by<T, 64, 4>(a, stream);
+    return quantize_rows_by<T, 256, 4>(a, stream);
 }
 
 int launch_quantize_rows(const QuantizeArgs &a, void *stream)
@@ -644,30 +821,21 @@ int launch_quantize_rows(const QuantizeArgs &a, void *stream)
     return a.x16 ? quantize_rows<_Float16>(a, stream) : quantize_rows<float>(a, stream);
 }
 
-// Up to 16 tokens whose x fits into LDS beside the rings; rows of x and w on 16-byte boundaries and of whole 16 bytes.
-static bool takes_few(const LinearArgs &a, int size, bool x_fits)
-{
-    return a.k > 0 && a.m <= 16 && a.w_fits && x_fits && (long long)a.k * 4 * a.m < (1 << 20) &&
-           few_lds(a.m, a.k, size).total <= kFewLds && a.n <= kFewMostN;
-}
-
-bool linear_quantizes(const LinearArgs &a) { return takes_few(a, a.x16 ? 2 : 4, a.x_vec && a.k % 16 == 0); }
-
 // The tiles, and what a step of 128 codes of a block takes: at least `wait`, and `work` for each block that a compute unit
 // holds at once (`resident` of them at most); `ends` for what is in front of the first step and behind the last (us).
 struct Tile {
-    int m, n, stages, resident;
+    int m, n, resident;
     double wait, work, ends;
     int (*launch)(const LinearArgs &, void *);
 };
 
 static const Tile kTiles[] = {
-    {256, 256, 2, 1, 1.80, 1.80, 2.0, launch_tiles<256, 256, 2, 4, 2>},
-    {256, 128, 3, 1, 0.70, 0.98, 2.0, launch_tiles<256, 128, 4, 2, 3>},
-    {128, 128, 2, 2, 0.80, 0.56, 2.0, launch_tiles<128, 128, 2, 2, 2>},
-    {128, 128, 4, 1, 0.46, 0.56, 2.5, launch_tiles<128, 128, 2, 2, 4>},
-    {64, 64, 4, 2, 0.19, 0.21, 1.0, launch_tiles<64, 64, 2, 2, 4>},
-    {32, 64, 4, 3, 0.19, 0.12, 1.0, launch_tiles<32, 64, 1, 2, 4>},
+    {256, 256, 1, 1.80, 1.80, 2.0, launch_tiles<256, 256, 2, 4, 2>},
+    {256, 128, 1, 0.70, 0.98, 2.0, launch_tiles<256, 128, 4, 2, 3>},
+    {128, 128, 2, 0.80, 0.56, 2.0, launch_tiles<128, 128, 2, 2, 2>},
+    {128, 128, 1, 0.46, 0.56, 2.5, launch_tiles<128, 128, 2, 2, 4>},
+    {64, 64, 2, 0.19, 0.21, 1.0, launch_tiles<64, 64, 2, 2, 4>},
+    {32, 64, 3, 0.19, 0.12, 1.0, launch_tiles<32, 64, 1, 2, 4>},
 };
 
 static double tile_time(const LinearArgs &a, const Tile &t)
@@ -683,25 +851,40 @@ static double tile_time(const LinearArgs &a, const Tile &t)
     return time;
 }
 
+// Whether the kernel of few tokens takes x of this element size: it fits into LDS beside the rings.
+bool linear_few(const LinearArgs &a, int size)
+{
+    return a.k > 0 && a.m <= 16 && (a.n <= kFewMostN || !a.w_fits) && a.ldw <= kMostPitch && (long long)a.k * size * a.m <= kFewLds &&
+           few_lds(a.m, a.k, size, true).total <= kFewLds;
+}
+
+// Few channels, or the product of 16 tokens takes longer than a trip of their codes to memory.  us, codes by a kernel of their
+// own and tiles / this: 19200 x 128 x 384 14.8 / 11.0, 288000 x 128 x 128 69.5 / 49.4, 2048 x 256 x 256 7.4 / 6.3, 1024 x 128 x 128
+// 7.4 / 4.6; 5000 x 384 x 384 9.4 / 10.1, 1024 x 512 x 512 7.8 / 13.3.
+bool linear_rows(const LinearArgs &a)
+{
+    return a.k >= 16 && a.k <= kRowsMostK && a.m >= 1024 && (long long)a.n * a.k <= (1 << 16);
+}
+
+template <typename X, int TOK> static int launch_rows_by(const LinearArgs &a, void *stream)
+{
+    return a.n <= 16 * kRowsWaves ? launch_rows_of<X, TOK, 1>(a, stream) : launch_rows_of<X, TOK, 2>(a, stream);
+}
+
+// 32 tokens to a block while they are that few that longer blocks leave compute units without one, else 80.
+template <typename X> static int launch_rows(const LinearArgs &a, void *stream)
+{
+    return a.m <= 32 * kComputeUnits ? launch_rows_by<X, 2>(a, stream) : launch_rows_by<X, 5>(a, stream);
+}
+
 int launch_linear(const LinearArgs &a, void *stream)
 {
-    if (a.raw) return a.x16 ? launch_few<_Float16>(a, stream) : launch_few<float>(a, stream);
-    if (takes_few(a, 1, a.aligned)) return launch_few<int8_t>(a, stream);
-#ifdef FQ_V
-    if (FQ_V == 1) return launch_tiles<256, 256, 2, 4, 2>(a, stream);
-    if (FQ_V == 2) return launch_tiles<256, 128, 4, 2, 3>(a, stream);
-    if (FQ_V == 3) return launch_tiles<128, 128, 2, 2, 2>(a, stream);
-    if (FQ_V == 4) return launch_tiles<128, 128, 2, 2, 4>(a, stream);
-    if (FQ_V == 5) return launch_tiles<64, 64, 2, 2, 4>(a, stream);
-    if (FQ_V == 6) return launch_tiles<64, 128, 1, 4, 3>(a, stream);
-    if (FQ_V == 14) return launch_tiles<32, 64, 1, 2, 4>(a, stream);
-    if (FQ_V == 15) return launch_tiles<32, 128, 1, 4, 4>(a, stream);
-    if (FQ_V == 16) return launch_tiles<32, 64, 1, 2, 3>(a, stream);
-#endif
+    if (a.raw && a.m <= 16) return a.x16 ? launch_few<_Float16>(a, stream) : launch_few<float>(a, stream);
+    if (a.raw) return a.x16 ? launch_rows<_Float16>(a, stream) : launch_rows<float>(a, stream);
+    if (linear_few(a, 1)) return launch_few<int8_t>(a, stream);
     int best = 0;
     double least = 0.0;
     for (int i = 0; i < (int)(sizeof kTiles / sizeof kTiles[0]); ++i) {
-        if (!a.aligned && kTiles[i].stages > 2 && kTiles[i].m != 64) continue;   // (64 x 64: launched with two)
         const double t = tile_time(a, kTiles[i]);
         if (least == 0.0 || t < least) { least = t; best = i; }
     }

@@ -8,7 +8,6 @@ namespace fq {
 namespace {
 
 constexpr size_t kAlign = 256;
-constexpr long long kMostPitch = 1 << 22;        // 256 rows of it have 32-bit offsets
 
 size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
@@ -35,20 +34,31 @@ bool overlap(const Rows &a, const Rows &b)
     return true;
 }
 
+// Whether the tiles take rows of codes as they lie.
+bool fits(const void *p, long long ld, long long k)
+{
+    return aligned(p, 16) && ld % 16 == 0 && ld <= kMostPitch && k % 16 == 0;
+}
+
+// [codes of x][scales of x][codes of w], each only where it is needed: x is quantized or laid out anew, w laid out anew.
 struct Workspace {
     long long pitch = 0;             // of a row of codes
-    size_t scales_off = 0, bytes = kAlign;
+    size_t scales = 0, w = 0, bytes = kAlign;
 };
 
 Workspace workspace_of(const fq_linear &d)
 {
-    Workspace w;
-    if (d.x_dtype == FQ_I8) return w;
-    w.pitch = (d.k + kCodePitch - 1) / kCodePitch * kCodePitch;
-    w.scales_off = round_up((size_t)d.m * (size_t)w.pitch, kAlign);
-    w.bytes = w.scales_off + round_up((size_t)d.m * sizeof(float), kAlign);
-    if (w.bytes < kAlign) w.bytes = kAlign;
-    return w;
+    Workspace at;
+    at.pitch = (d.k + kCodePitch - 1) / kCodePitch * kCodePitch;
+    if (d.m == 0 || d.n == 0 || d.k == 0) at.pitch = 0;
+    size_t end = 0;
+    if (d.x_dtype != FQ_I8 || !fits(d.x, d.ldx, d.k)) end += round_up((size_t)d.m * (size_t)at.pitch, kAlign);
+    at.scales = end;
+    if (d.x_dtype != FQ_I8) end += round_up((size_t)d.m * sizeof(float), kAlign);
+    at.w = end;
+    if (!fits(d.w, d.ldw, d.k)) end += round_up((size_t)d.n * (size_t)at.pitch, kAlign);
+    if (end > at.bytes) at.bytes = end;
+    return at;
 }
 
 bool pitch_fits(long long rows, long long pitch, long long width)
@@ -82,37 +92,53 @@ fq_status run(const fq_linear &d, void *workspace, size_t ws_bytes, void *stream
 {
     const fq_status st = validate(d);
     if (st != FQ_OK || d.m == 0 || d.n == 0) return st;
-    const Workspace ws = workspace_of(d);
+    const Workspace at = workspace_of(d);
+    const bool quantize = d.x_dtype != FQ_I8, x_fits = !quantize && fits(d.x, d.ldx, d.k), w_fits = fits(d.w, d.ldw, d.k);
+    if (!x_fits || !w_fits) {
+        if (!workspace || ws_bytes < at.bytes) return FQ_ERR_WORKSPACE;
+        if (!aligned(workspace, kAlign)) return FQ_ERR_ALIGN;
+    }
     LinearArgs a;
     std::memset(&a, 0, sizeof a);
     a.x = (const int8_t *)d.x; a.xs = d.xs; a.ldx = d.ldx; a.xs_step = d.xs_step;
     a.w = d.w; a.ws = d.ws; a.ldw = d.ldw; a.ws_step = d.ws_step;
     a.bias = d.bias; a.y = d.y; a.ldy = d.ldy; a.y16 = d.y_dtype == FQ_F16;
-    a.m = (int)d.m; a.n = (int)d.n; a.k = a.kx = (int)d.k;
-    const size_t xb = size_of(d.x_dtype), yb = size_of(d.y_dtype);
-    const bool x_vec = aligned(d.x, 16) && (size_t)d.ldx * xb % 16 == 0;
-    a.w_fits = aligned(a.w, 16) && a.ldw % 16 == 0 && a.ldw <= kMostPitch && a.k % 16 == 0;
-    bool x_aligned = x_vec && a.ldx <= kMostPitch;
-    if (d.x_dtype != FQ_I8) {
-        if (!workspace || ws_bytes < ws.bytes) return FQ_ERR_WORKSPACE;
-        if (!aligned(workspace, kAlign)) return FQ_ERR_ALIGN;
-        x_aligned = true;
-        a.x16 = d.x_dtype == FQ_F16;
-        a.x_vec = x_vec;
-        if (linear_quantizes(a)) {
-            a.raw = d.x;
-        } else {
-            QuantizeArgs q;
-            std::memset(&q, 0, sizeof q);
-            q.x = d.x; q.ldx = d.ldx; q.m = a.m; q.k = a.k; q.x16 = a.x16; q.vec = x_vec;
-            q.q = (int8_t *)workspace; q.s = (float *)((char *)workspace + ws.scales_off); q.pitch = ws.pitch;
-            if (launch_quantize_rows(q, stream) != 0) return FQ_ERR_LAUNCH;
-            a.x = q.q; a.xs = q.s; a.ldx = ws.pitch; a.xs_step = 1;
-            a.kx = (int)ws.pitch;
-        }
+    a.m = (int)d.m; a.n = (int)d.n; a.k = a.kx = a.kw = (int)d.k;
+    a.y_vec = aligned(a.y, 16) && (size_t)a.ldy * size_of(d.y_dtype) % 16 == 0;
+    a.w_fits = w_fits;
+    a.x16 = d.x_dtype == FQ_F16;
+    a.x_vec = aligned(d.x, 16) && (size_t)d.ldx * size_of(d.x_dtype) % 16 == 0;
+    if (quantize && linear_few(a, (int)size_of(d.x_dtype))) {
+        a.raw = d.x;
+        return launch_linear(a, stream) == 0 ? FQ_OK : FQ_ERR_LAUNCH;
     }
-    a.y_vec = aligned(a.y, 16) && (size_t)a.ldy * yb % 16 == 0;
-    a.aligned = x_aligned && a.w_fits;
+    int8_t *const codes = (int8_t *)workspace;
+    if (quantize && linear_rows(a)) {
+        a.raw = d.x;
+    } else if (quantize) {
+        QuantizeArgs q;
+        std::memset(&q, 0, sizeof q);
+        q.x = d.x; q.ldx = d.ldx; q.m = a.m; q.k = a.k; q.x16 = a.x16;
+        q.q = codes; q.s = (float *)(codes + at.scales); q.pitch = at.pitch;
+        if (launch_quantize_rows(q, stream) != 0) return FQ_ERR_LAUNCH;
+        a.xs = q.s;
+        a.xs_step = 1;
+    } else if (!x_fits && a.k > 0) {
+        const AlignArgs r = {a.x, codes, d.m, d.ldx, at.pitch, a.k};
+        if (launch_align_rows(r, stream) != 0) return FQ_ERR_LAUNCH;
+    }
+    if (!x_fits && !a.raw) {
+        a.x = codes;
+        a.ldx = at.pitch;
+        a.kx = (int)at.pitch;
+    }
+    if (!w_fits && a.k > 0 && !linear_few(a, 1)) {
+        const AlignArgs r = {a.w, codes + at.w, d.n, d.ldw, at.pitch, a.k};
+        if (launch_align_rows(r, stream) != 0) return FQ_ERR_LAUNCH;
+        a.w = r.to;
+        a.ldw = at.pitch;
+        a.kw = (int)at.pitch;
+    }
     return launch_linear(a, stream) == 0 ? FQ_OK : FQ_ERR_LAUNCH;
 }
 

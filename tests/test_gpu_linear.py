@@ -82,13 +82,23 @@ def run(m, n, k, x_kind, y_kind, seed, bias=True, xs_one=False, ws_one=False, **
 SIZES = [(1, 1, 1), (1, 16, 64), (1, 4096, 512), (1, 1000, 1155), (2, 33, 17), (3, 257, 100), (7, 64, 4096), (16, 128, 256),
          (17, 130, 384), (20, 512, 1024), (31, 48, 63), (33, 16, 2048), (64, 64, 64), (65, 300, 127), (100, 31, 129),
          (128, 256, 128), (129, 257, 255), (200, 96, 3456), (255, 511, 40), (256, 256, 512), (300, 700, 130), (513, 384, 384),
-         (16, 64, 4000), (15, 70, 4288), (2, 40, 30000), (64, 8200, 96), (30, 16400, 200), (5, 16385, 80), (1000, 130, 1155), (1201, 257, 1155), (2049, 129, 96), (700, 1100, 640)]
+         (16, 64, 4000), (15, 70, 4288), (2, 40, 30000), (64, 8200, 96), (30, 16400, 200), (5, 16385, 80), (1024, 16, 16), (1029, 130, 300), (1100, 300, 511), (1027, 512, 512), (1200, 700, 64), (4000, 33, 65),
+         (1050, 385, 384), (1100, 120, 500), (9000, 40, 100), (8200, 250, 256), (1000, 130, 1155), (1201, 257, 1155), (2049, 129, 96), (700, 1100, 640)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
 @pytest.mark.parametrize("x_kind,y_kind", [("f16", "f16"), ("f32", "f32"), ("i8", "f16")])
 def test_sizes(m, n, k, x_kind, y_kind):
     run(m, n, k, x_kind, y_kind, seed=m * 7919 + n * 31 + k)
+
+
+@pytest.mark.parametrize("m", [1, 3, 16])
+@pytest.mark.parametrize("k", [1, 15, 16, 100, 111, 112, 113, 127, 224, 225, 895, 896, 897, 1000, 2047, 4001])
+@pytest.mark.parametrize("x_kind", ["f16", "f32", "i8"])
+def test_few_tokens_with_rows_off_the_grid(m, k, x_kind):
+    """Rows of w and x that begin anywhere in 16 bytes, around the steps that such rows are cut into."""
+    for front in range(0, 16, 5):
+        run(m, 50, k, x_kind, "f32", seed=k + front, w_pitch=k + front % 3, x_pitch=k + front % 2, fronts=(front, front, 0))
 
 
 @pytest.mark.parametrize("m", [1, 5, 40, 300])
