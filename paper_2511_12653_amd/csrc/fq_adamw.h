@@ -34,7 +34,8 @@ struct AdamwStep {
     const float *grad_scale;
 };
 
-// table: the n descriptors, and behind them (at `first`) their first grid blocks.  rows: rows of a grid block.
+// table: the n descriptors, and behind them (at `first`) their first grid blocks; or, with no `first`, a descriptor for each
+// grid block.  rows: rows of a grid block, 1 or 2 (1 without `first`).
 int launch_adamw(const AdamwTensor *table, const unsigned *first, int n, const AdamwStep &s, unsigned blocks, int rows,
                  void *stream);
 

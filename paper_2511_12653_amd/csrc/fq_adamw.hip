@@ -63,21 +63,22 @@ __device__ __forceinline__ unsigned halves_max(unsigned v)
     return (unsigned)__builtin_amdgcn_readlane((int)v, kSumLane);
 }
 
-__device__ __forceinline__ unsigned random_bits(unsigned place, unsigned key)
+constexpr unsigned kPlace = 0x9E3779B1u;          // x = place * kPlace + key is what is mixed
+
+__device__ __forceinline__ unsigned mix(unsigned x)
 {
-    unsigned x = place * 0x9E3779B1u + key;
     x = (x ^ (x >> 16)) * 0x6A09E667u;
     x = (x ^ (x >> 15)) * 0xBB67AE85u;
     return x ^ (x >> 16);
 }
 
-// The e4m3 value at or below a (0 <= a <= 448) raised by (bits + 1/2) / 2^16 of the step between codes: adding that
+// The e4m3 value at or below a (0 <= a <= 448) raised by (u + 1/2) / 2^16 of the step between codes: adding that
 // to the 20 mantissa bits that a code lacks, and cutting them off.  Below 2^-6 the steps stay those of the binade
-// above, where adding 2^-6 puts a.
-__device__ __forceinline__ float round_code(float a, unsigned bits)
+// above, where adding 2^-6 puts a.  more: 16 u + 8.
+__device__ __forceinline__ float round_code(float a, unsigned more)
 {
     const float low = a < 0x1p-6f ? 0x1p-6f : 0.0f;
-    const unsigned z = (__builtin_bit_cast(unsigned, a + low) + (bits * 16u + 8u)) & 0xFFF00000u;
+    const unsigned z = (__builtin_bit_cast(unsigned, a + low) + more) & 0xFFF00000u;
     return __builtin_bit_cast(float, z) - low;
 }
 
@@ -133,66 +134,92 @@ __device__ __forceinline__ void step_rows(const AdamwTensor &t, const AdamwStep 
         const long long block = ((long long)chunk * ROWS + r) * (kAdamwRowElems / kStateBlock) + wave;
         const long long i = block * kStateBlock + 4 * lane, left = t.n - i;
         if (block * kStateBlock >= t.n) continue;
-        float m[4], v[4], root[4], p[4];
-        if (F8) {
-            unpack4(m8[r], m);
-            unpack4(v8[r], v);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const float g = (float)g4[r][j] * gs;
-            const float m0 = F8 ? m[j] * ms[r] : mf[r][j];
-            const float r0 = F8 ? v[j] * vs[r] : 0.0f;
-            const float v0 = F8 ? r0 * r0 : vf[r][j];
-            const float m1 = s.beta1 * m0 + s.one_minus_beta1 * g;
-            const float v1 = s.beta2 * v0 + (s.one_minus_beta2 * g) * g;
-            const bool fine = __builtin_fabsf(v1) < __builtin_inff();
-            m[j] = fine ? m1 : m0;
-            v[j] = fine ? v1 : v0;
-            root[j] = __builtin_sqrtf(v[j]);
-            const float below = root[j] * s.root_factor + s.eps;
-            const float p0 = (float)p4[r][j];
-            const float p1 = p0 * keep - lrc * (m[j] / below);
-            p[j] = fine ? p1 : p0;
-        }
-        P4 pn;
-        f16x4 copy;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            pn[j] = (P)p[j];
-            copy[j] = (_Float16)p[j];
-        }
-        store4<P>(t.p, i, vec, left, pn);
-        if (t.p16) store4<_Float16>(t.p16, i, vec, left, copy);
-        if (!F8) {
+        if constexpr (!F8) {
+            P4 pn;
+            f16x4 copy;
             f32x4 mn, vn;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { mn[j] = m[j]; vn[j] = v[j]; }
+            for (int j = 0; j < 4; ++j) {
+                const float g = (float)g4[r][j] * gs, m0 = mf[r][j], v0 = vf[r][j], p0 = (float)p4[r][j];
+                const float m1 = s.beta1 * m0 + s.one_minus_beta1 * g;
+                const float v1 = s.beta2 * v0 + (s.one_minus_beta2 * g) * g;
+                const bool fine = __builtin_fabsf(v1) < __builtin_inff();
+                mn[j] = fine ? m1 : m0;
+                vn[j] = fine ? v1 : v0;
+                const float p1 = p0 * keep - lrc * (m1 / (__builtin_sqrtf(v1) * s.root_factor + s.eps));
+                const float p = fine ? p1 : p0;
+                pn[j] = (P)p;
+                copy[j] = (_Float16)p;
+            }
+            store4<P>(t.p, i, vec, left, pn);
+            if (t.p16) store4<_Float16>(t.p16, i, vec, left, copy);
             store4<float>(t.m, i, vec, left, mn);
             store4<float>(t.v, i, vec, left, vn);
             continue;
         }
-        // exponents (biased) of the least powers of two that reach the greatest |m| / 1.75 and v / 1.53125: the
-        // mantissas of 448 = 1.75 * 2^8 and of 448^2 = 1.53125 * 2^17
-        unsigned am = 0, av = 0;
+        // What bounds this is the arithmetic (about 70 instructions an element; with exact root and quotient, a guard
+        // per element and four products to a hash it was 114, 57 us for 20 million FP16 elements).
+        float m[4], v[4];
+        unsigned both;
+        auto moments = [&](bool guarded) {
+            unpack4(m8[r], m);
+            unpack4(v8[r], v);
+            unsigned am = 0, av = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            am = max(am, __builtin_bit_cast(unsigned, m[j]) & 0x7FFFFFFFu);
-            av = max(av, __builtin_bit_cast(unsigned, v[j]) & 0x7FFFFFFFu);
-        }
-        const unsigned both = halves_max(((am + 0x1FFFFFu) >> 23) | ((av + 0x3BFFFFu) >> 23) << 16);
+            for (int j = 0; j < 4; ++j) {
+                const float g = (float)g4[r][j] * gs, m0 = m[j] * ms[r], r0 = v[j] * vs[r], v0 = r0 * r0;
+                m[j] = s.beta1 * m0 + s.one_minus_beta1 * g;
+                v[j] = s.beta2 * v0 + (s.one_minus_beta2 * g) * g;
+                if (guarded && !(__builtin_fabsf(v[j]) < __builtin_inff())) {
+                    m[j] = m0;
+                    v[j] = v0;
+                }
+                am = max(am, __builtin_bit_cast(unsigned, m[j]) & 0x7FFFFFFFu);
+                av = max(av, __builtin_bit_cast(unsigned, v[j]) & 0x7FFFFFFFu);
+            }
+            // exponents (biased) of the least powers of two that reach the greatest |m| / 1.75 and v / 1.53125: the
+            // mantissas of 448 = 1.75 * 2^8 and of 448^2 = 1.53125 * 2^17
+            both = halves_max(((am + 0x1FFFFFu) >> 23) | ((av + 0x3BFFFFu) >> 23) << 16);
+        };
+        moments(false);
+        const bool odd = both >> 16 >= 255u;                    // some v is not finite
+        if (odd) moments(true);
         const int em = max((int)(both & 0xFFFFu) - 127 - 8, -126);
         const int e2 = max((int)(both >> 16) - 127 - 17, -126);
         const int ev = (e2 + 1) >> 1;
-        const float down_m = power_of_two(-em), down_v = power_of_two(-ev);
+        const float down_m = power_of_two(-em), down_v = power_of_two(-2 * ev), up = power_of_two(ev) * s.root_factor;
+        // A root over 2^72 times smaller than the block's greatest is lost in its units.  Beside eps it does not matter,
+        // unless the greatest is large or eps tiny.
+        const bool careful = odd || !(up * 0x1p-62f <= s.eps * 0x1p-26f);
+        const unsigned place = (t.place + (unsigned)i) * kPlace + s.key;
         float cm[4], cv[4];
+        P4 pn;
+        f16x4 copy;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const unsigned bits = random_bits(t.place + (unsigned)i + (unsigned)j, s.key);
-            cm[j] = __builtin_copysignf(round_code(__builtin_fabsf(m[j]) * down_m, bits & 0xFFFFu), m[j]);
-            const float c = round_code(root[j] * down_v, bits >> 16);
-            cv[j] = v[j] > 0.0f && c == 0.0f ? 0x1p-9f : c;
+            const unsigned bits = mix(place + (unsigned)j * kPlace);
+            // the root in units of the scale: at most 448 (one rounding more would make a code that is none), and never 0
+            // under the quotient
+            const float root = __builtin_amdgcn_fmed3f(__builtin_amdgcn_sqrtf(v[j] * down_v), 0x1p-64f, 448.0f);
+            const float p0 = (float)p4[r][j];
+            float p = p0 * keep - lrc * (m[j] * __builtin_amdgcn_rcpf(root * up + s.eps));
+            if (careful) {
+                p = p0 * keep - lrc * (m[j] / (__builtin_sqrtf(v[j]) * s.root_factor + s.eps));
+                if (odd) {                                       // (a gradient that was not finite leaves no trace in m and v)
+                    float m0[4], v0[4];
+                    unpack4(m8[r], m0);
+                    unpack4(v8[r], v0);
+                    const float g = (float)g4[r][j] * gs, r0 = v0[j] * vs[r], v1 = s.beta2 * (r0 * r0) + (s.one_minus_beta2 * g) * g;
+                    if (!(__builtin_fabsf(v1) < __builtin_inff())) p = p0;
+                }
+            }
+            pn[j] = (P)p;
+            copy[j] = (_Float16)p;
+            cm[j] = __builtin_copysignf(round_code(__builtin_fabsf(m[j]) * down_m, (bits & 0xFFFFu) << 4 | 8u), m[j]);
+            cv[j] = __builtin_fmaxf(round_code(root, (bits >> 12 & 0xFFFF0u) | 8u), v[j] > 0.0f ? 0x1p-9f : 0.0f);
         }
+        store4<P>(t.p, i, vec, left, pn);
+        if (t.p16) store4<_Float16>(t.p16, i, vec, left, copy);
         store4<unsigned char>(t.m, i, vec, left, __builtin_bit_cast(u8x4, pack4(cm)));
         store4<unsigned char>(t.v, i, vec, left, __builtin_bit_cast(u8x4, pack4(cv)));
         if (lane == 0) {
@@ -228,10 +255,11 @@ __device__ __forceinline__ AdamwTensor descriptor(const AdamwTensor *p)
     return t;
 }
 
-template <int ROWS>
+// FIND: the table has a descriptor per tensor, else one per grid block.
+template <int ROWS, bool FIND>
 __global__ __launch_bounds__(kAdamwThreads) void adamw_kernel(const AdamwTensor *table, const unsigned *first, unsigned n, AdamwStep s)
 {
-    const unsigned which = __builtin_amdgcn_readfirstlane(find_tensor(first, n, blockIdx.x));
+    const unsigned which = FIND ? __builtin_amdgcn_readfirstlane(find_tensor(first, n, blockIdx.x)) : blockIdx.x;
     const AdamwTensor t = descriptor(table + which);
     const float gs = s.grad_scale ? ld_uniform(s.grad_scale) : 1.0f;
     const unsigned chunk = blockIdx.x - t.first;
@@ -252,10 +280,9 @@ __global__ __launch_bounds__(kAdamwThreads) void adamw_kernel(const AdamwTensor 
 int launch_adamw(const AdamwTensor *table, const unsigned *first, int n, const AdamwStep &s, unsigned blocks, int rows,
                  void *stream)
 {
-    if (rows == 1)
-        adamw_kernel<1><<<blocks, kAdamwThreads, 0, (hipStream_t)stream>>>(table, first, (unsigned)n, s);
-    else
-        adamw_kernel<4><<<blocks, kAdamwThreads, 0, (hipStream_t)stream>>>(table, first, (unsigned)n, s);
+    if (!first) adamw_kernel<1, false><<<blocks, kAdamwThreads, 0, (hipStream_t)stream>>>(table, first, (unsigned)n, s);
+    else if (rows == 1) adamw_kernel<1, true><<<blocks, kAdamwThreads, 0, (hipStream_t)stream>>>(table, first, (unsigned)n, s);
+    else adamw_kernel<2, true><<<blocks, kAdamwThreads, 0, (hipStream_t)stream>>>(table, first, (unsigned)n, s);
     return (int)hipGetLastError();
 }
 
