@@ -3,7 +3,8 @@
 `workloads` generates seeded synthetic inputs (numpy only).  The GPU entry points live in
 `binding` (thin ctypes marshalling onto the C-ABI library built from csrc/); it is imported
 on first use and raises if the compiled library is missing -- there is no CPU fallback.
-`fake_quantize` (module `autograd`) wraps the forward and backward calls in a torch.autograd Function.
+`fake_quantize` (module `autograd`) wraps the forward and backward calls in a torch.autograd Function, `linear_int8` (module
+`linear`) the int8 linear layer, `AdamW` (module `optim`) the multi-tensor AdamW step in a torch.optim.Optimizer.
 """
 from . import workloads  # noqa: F401
 
@@ -15,10 +16,13 @@ _API = ("fq_forward", "fq_backward", "fq_multi_tensor", "fq_workspace_bytes", "f
         "FQ_F16", "FQ_F32", "FQ_FLAG_NO_DX", "FQ_FLAG_TWO_PASS", "FQ_FLAG_NO_POLL", "FQ_MODE_FORWARD", "FQ_MODE_BACKWARD")
 
 
+_FRONT_DOORS = {"fake_quantize": "autograd", "linear_int8": "linear", "AdamW": "optim"}
+
+
 def __getattr__(name):
-    if name == "fake_quantize":
-        from .autograd import fake_quantize
-        return fake_quantize
+    if name in _FRONT_DOORS:
+        import importlib
+        return getattr(importlib.import_module(__name__ + "." + _FRONT_DOORS[name]), name)
     if name == "binding" or name in _API:
         import importlib
         mod = importlib.import_module(__name__ + ".binding")

@@ -142,15 +142,11 @@ class FqDistill(ctypes.Structure):
 
 def _device_of(tensors):
     """The one GPU that all given tensors are on."""
-    device = None
-    for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise ValueError("tensors must be on the GPU (no CPU fallback)")
-        if device is not None and t.device != device:
-            raise ValueError("tensors are on different GPUs")
-        device = t.device
+    devices = {t.get_device() for t in tensors if t is not None}
+    if -1 in devices:
+        raise ValueError("tensors must be on the GPU (no CPU fallback)")
+    if len(devices) > 1:
+        raise ValueError("tensors are on different GPUs")
 
 
 class FqParam(ctypes.Structure):

@@ -1,0 +1,114 @@
+"""Torch front door to the multi-tensor AdamW step: `AdamW(params, ...)`, a torch.optim.Optimizer whose step() is one
+fq_adamw_step call (one launch) per parameter group.
+
+Marshalling only.  The moments are float32, or float8_e4m3fn codes with a scale per 256 elements (`states="float8"`, a quarter
+of the memory, rounded stochastically).  There is no CPU path: CPU parameters raise.
+"""
+import torch
+
+from . import binding as fq
+
+_DTYPES = (torch.float16, torch.float32)
+
+
+class _Plan:
+    """A plan of the library with its workspace and the tensors whose addresses it holds."""
+
+    def __init__(self, key, params, device):
+        self.key, self.params = key, params
+        self.workspace = torch.empty(fq.fq_adamw_workspace_bytes(params), dtype=torch.uint8, device=device)
+        self.handle = fq.fq_adamw_create(params, self.workspace)
+
+    def __del__(self):
+        if getattr(self, "handle", None):
+            fq.fq_adamw_destroy(self.handle)
+
+
+class AdamW(torch.optim.Optimizer):
+    """Decoupled weight decay Adam over float16 and float32 parameters on one GPU.
+
+    states: "float32" or "float8".  seed: of the stochastic rounding of float8 states.  A group may override lr, betas, eps,
+    weight_decay and states, and may bring `copies`: one float16 tensor (or None) per float32 parameter, which receives
+    its new values.  Elements whose gradient is not finite are left as they are.  All parameters of a group share
+    its step count; one without a gradient is skipped.
+    """
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, states="float32", seed=0):
+        self._plans = {}
+        super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay, states=states, seed=seed, step=0,
+                                      copies=None))
+
+    def add_param_group(self, group):
+        super().add_param_group(group)
+        group = self.param_groups[-1]
+        if group["states"] not in ("float32", "float8"):
+            raise ValueError("states must be float32 or float8, not %r" % (group["states"],))
+        for p in group["params"]:
+            if not p.is_cuda:
+                raise RuntimeError("AdamW runs on the GPU only (no CPU fallback)")
+            if p.dtype not in _DTYPES or not p.is_contiguous():
+                raise TypeError("parameters must be contiguous float16 or float32")
+        if group["copies"] is not None and len(group["copies"]) != len(group["params"]):
+            raise ValueError("copies must hold a tensor or None for each parameter")
+        # (groups round differently: each has its own part of the seeds)
+        group["seed"] = int(group["seed"]) + ((len(self.param_groups) - 1) << 32)
+
+    def _state_of(self, p, group):
+        state = self.state[p]
+        if not state:
+            if group["states"] == "float8":
+                blocks = (p.numel() + 255) // 256
+                for name in ("m", "v"):
+                    state[name] = torch.zeros(p.shape, dtype=torch.float8_e4m3fn, device=p.device)
+                    state[name + "_scale"] = torch.zeros(blocks, device=p.device)
+            else:
+                for name in ("m", "v"):
+                    state[name] = torch.zeros(p.shape, device=p.device)
+        return state
+
+    def _plan(self, index, group):
+        chosen = [(p, self._state_of(p, group), c)
+                  for p, c in zip(group["params"], group["copies"] or [None] * len(group["params"])) if p.grad is not None]
+        if not chosen:
+            return None
+        # All that the plan's table is made of.  Gradients are often other tensors in every step: then it is made anew.
+        key = (group["weight_decay"],) + tuple(
+            (p.numel(), p.dtype, p.data_ptr(), p.grad.dtype, p.grad.stride(), p.grad.data_ptr(), c is not None and c.data_ptr())
+            + tuple(t.data_ptr() for t in s.values()) for p, s, c in chosen)
+        plan = self._plans.get(index)
+        if plan is None or plan.key != key:
+            if any(p.grad.is_sparse or not p.grad.is_contiguous() for p, _, _ in chosen):
+                raise TypeError("gradients must be dense and contiguous")
+            params = [fq.FqParam.from_torch(p.detach(), p.grad, s["m"], s["v"], s.get("m_scale"), s.get("v_scale"), p16=c,
+                                            weight_decay=group["weight_decay"]) for p, s, c in chosen]
+            plan = self._plans[index] = _Plan(key, params, chosen[0][0].device)
+        return plan
+
+    @torch.no_grad()
+    def step(self, closure=None, grad_scale=None):
+        """grad_scale: one float32 on the GPU that all gradients are multiplied by, or None."""
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for index, group in enumerate(self.param_groups):
+            group["step"] += 1
+            if not group["params"]:
+                continue
+            with torch.cuda.device(group["params"][0].device):
+                plan = self._plan(index, group)
+                if plan is not None:
+                    beta1, beta2 = group["betas"]
+                    fq.fq_adamw_step(plan.handle, fq.FqAdamW(group["lr"], beta1, beta2, group["eps"], group["step"], group["seed"],
+                                                             grad_scale))
+        return loss
+
+    def load_state_dict(self, state_dict):
+        super().load_state_dict(state_dict)
+        # The base class turns the states into the parameters' type.  They are codes, scales and floats: put back as saved.
+        saved = [i for g in state_dict["param_groups"] for i in g["params"]]
+        own = [p for g in self.param_groups for p in g["params"]]
+        for i, p in zip(saved, own):
+            if i in state_dict["state"]:
+                self.state[p] = {k: v.to(p.device, copy=True) for k, v in state_dict["state"][i].items()}
+        self._plans = {}
