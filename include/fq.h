@@ -368,9 +368,11 @@ void fq_adamw_destroy(fq_adamw_plan *plan);
  * with round-half-to-even and the correctly rounded quotient, as in fq_forward.  A row whose greatest magnitude is under
  * 127 * FLT_MIN has scale and codes 0; a row with a NaN or an infinity makes its row of y NaN.
  * A 1x1 convolution is this with positions for tokens, a larger kernel with unfolded patches.
- * Rows may lie any distance apart (ldx, ldw, ldy, in elements) and at any address that their type allows; nothing of x or w
- * outside the rows is read.  Fastest where the rows of x (FQ_I8) and w begin on 16-byte boundaries and k is a multiple of
- * 16.  One to three launches.  The workspace need not be initialised and may be shared by calls that do not overlap in time.
+ * Rows may lie any distance apart (ldx, ldw, ldy, in elements) and at any address that their type allows.  x and w are read in
+ * whole 16 bytes: what lies between two rows, and the rest of the 16 bytes in which the first begins and the last ends, may be
+ * read and has no effect.  Fastest where the rows of x (FQ_I8) and w begin on 16-byte boundaries and k is a multiple of 16:
+ * others are laid out anew in the workspace first (whose size therefore depends on the pointers), but for w with up to 16
+ * tokens.  One to three launches.  The workspace need not be initialised and may be shared by calls that do not overlap in time.
  */
 typedef struct fq_linear {
     int64_t m, n, k;                  /* tokens, output channels, values per token; any may be 0; k <= 131071 */

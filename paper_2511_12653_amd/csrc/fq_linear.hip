@@ -184,9 +184,12 @@ __global__ __launch_bounds__(256) void align_rows_kernel(AlignArgs a)
 //
 // 128 codes of every row of the tile make a step; LDS holds STAGES of them.  While the matrix cores work on one, the loads of
 // the STAGES - 1 next go straight from memory into the others.  A load instruction fills 1 KiB of LDS in lane order, eight rows; which
-// 16 codes a lane fetches is free, and lane 8 r + c fetches those at c ^ r, so that eight lanes that read the same 16 codes of
-// eight neighbouring rows find them in eight different places of the banks.
+// 16 codes a lane fetches is free.  LDS answers 16 lanes at a time, from 64 banks: 16 places of 16 bytes, two rows of them.  So
+// the codes at 16 c of row r lie at place c ^ (r / 2 % 8) of it: 16 neighbouring rows have theirs in 16 places.  (At
+// c ^ (r % 8) half of the cycles that LDS worked were conflicts.  The times are the same: not LDS bounds these kernels.)
 constexpr int kDepth = 128;                                     // codes of a row per step
+
+__device__ __forceinline__ int place_of(int chunk, int row) { return chunk ^ (row / 2 & 7); }      // (its own inverse in chunk)
 constexpr unsigned kNowhere = 0x7FFFFFF0u;                      // beyond the end of any buffer: reads as zeros
 
 #define FQ_LDS __attribute__((address_space(3)))
@@ -218,7 +221,8 @@ template <int N, int WAVES> struct Staging {                    // N wavefront l
     {
 #pragma unroll
         for (int j = 0; j < N; ++j)
-            off[j] = (((unsigned)((j * WAVES + wave) * 8 + lane / 8) * (unsigned)ld + shift) & ~15u) + (unsigned)((lane % 8) ^ (lane / 8)) * 16;
+            off[j] = (((unsigned)((j * WAVES + wave) * 8 + lane / 8) * (unsigned)ld + shift) & ~15u) +
+                     (unsigned)place_of(lane % 8, (j * WAVES + wave) * 8 + lane / 8) * 16;
     }
     // Load J of codes [at, at + kDepth) of the panel's rows into LDS; lanes with `none` fetch zeros.
     __device__ __forceinline__ void fetch(const Panel &p, int at, int j, int8_t *to, int wave, bool none)
@@ -339,7 +343,8 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
     w.place(a.ldw, lane, wave);
     x.place(a.ldx, lane, wave);
     const int steps = (a.k + kDepth - 1) / kDepth;
-    const int mine16 = ((lane % 8) ^ (lane / 8)) * 16;          // where in a step this lane's 16 codes lie
+    static_assert(WAVES % 2 == 0, "a wavefront's loads differ by multiples of 16 rows");
+    const int mine16 = place_of(lane % 8, wave * 8 + lane / 8) * 16;     // where in a step this lane's 16 codes lie
     // Loads [from, to) of the kLoads of a step.
     auto ask = [&](auto sure, int step, int8_t *into, int from, int to) {
         if (!sure && step >= steps) return;
@@ -367,7 +372,7 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
     struct Codes { i32x4 w[TN], x[TM]; } now, then;
     auto read = [&](const int8_t *from, int s, Codes &c) {
         const int8_t *fw = from + (wn + lane % 32) * kDepth, *fx = from + (BN + wm + lane % 32) * kDepth;
-        const int at = ((2 * s + lane / 32) ^ (lane % 8)) * 16;
+        const int at = place_of(2 * s + lane / 32, lane % 32) * 16;
 #pragma unroll
         for (int j = 0; j < TN; ++j) c.w[j] = *(const i32x4 *)(fw + j * 32 * kDepth + at);
 #pragma unroll
@@ -641,10 +646,10 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs a
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const int c = 4 * s + lane / 16;
-            i32x4 cw = *(const i32x4 *)(from + (c ^ (lane % 8)) * 16);
+            i32x4 cw = *(const i32x4 *)(from + place_of(c, lane % 16) * 16);
             i32x4 cx = *(const i32x4 *)(x + step * kUse + 64 * s);
             if (SHIFTED) {
-                cw = cut16(cw, *(const i32x4 *)(from + (((c + 1) & 7) ^ (lane % 8)) * 16), shift);
+                cw = cut16(cw, *(const i32x4 *)(from + place_of((c + 1) & 7, lane % 16) * 16), shift);
                 if (c == 7) cx = (i32x4)0;
             }
             sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(cw, cx, sum, 0, 0, 0);
