@@ -27,7 +27,6 @@ struct LinearArgs {
     int xs_step, ws_step;
     int x16, x_vec;            // of raw, 1: FP16; rows on 16-byte boundaries
     int y16;                   // 1: y is FP16
-    int y_vec;                 // 1: rows of y begin on 16-byte boundaries
     int w_fits;                // 1: rows of w begin on 16-byte boundaries, k is a multiple of 16, the pitch is at most kMostPitch
 };
 

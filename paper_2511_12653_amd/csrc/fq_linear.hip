@@ -87,9 +87,10 @@ __device__ __forceinline__ RowScale row_scale(unsigned most)
     return {s, 1.0f / s};
 }
 
-// Codes of eight values.  x * (1 / s) is within 127 * 2^-22.4 of the quotient x / s, so unless it lies that near to a
-// half (a few vectors of a row) it rounds to the same integer.  Adding 1.5 * 2^23 rounds it, to even, and leaves the code in
-// the low byte.  No code leaves [-127, 127]: no |x| is over 127 * s * (1 + 2^-24).
+// Codes of eight values.  x * (1 / s) is within 127 * 2^-23 of the quotient x / s as it is rounded, so unless it lies that near
+// to a half (a few vectors of a row) it rounds to the same integer.  Adding 1.5 * 2^23 rounds it, to even, and leaves the code
+// in the low byte; the product is not rounded before (one instruction, FP16 operands and all).  No code leaves
+// [-127, 127]: no |x| is over 127 * s * (1 + 2^-24).
 template <typename T> __device__ __forceinline__ u32x2 codes8(const Eight<T> &r, RowScale scale, bool none)
 {
     constexpr float kMagic = 0x1.8p23f;
@@ -98,9 +99,9 @@ template <typename T> __device__ __forceinline__ u32x2 codes8(const Eight<T> &r,
     float near = 0.0f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const float t = (float)v[e] * scale.inverse, f = t + kMagic;
+        const float f = __builtin_fmaf((float)v[e], scale.inverse, kMagic);
         b[e] = __builtin_bit_cast(unsigned, f);
-        near = __builtin_fmaxf(near, __builtin_fabsf(t - (f - kMagic)));
+        near = __builtin_fmaxf(near, __builtin_fabsf(__builtin_fmaf((float)v[e], scale.inverse, kMagic - f)));
     }
     if (near > 0.49995f) {
 #pragma unroll
@@ -241,58 +242,24 @@ __device__ __forceinline__ void lanes_in_step()
     __builtin_amdgcn_wave_barrier();
 }
 
-// y of 8 channels from j on, of token i.
-__device__ __forceinline__ void store8(const LinearArgs &a, long long i, int j, const float *y)
+// N neighbouring channels of a token, `left` of which there are (WHOLE: all).  Vector stores take any address.
+template <bool HALF, bool WHOLE, int N> __device__ __forceinline__ void store_channels(char *at, const float *y, int left)
 {
-    if (a.y16) {
-        _Float16 *to = (_Float16 *)a.y + i * a.ldy + j;
-        f16x8 v;
+    typedef typename std::conditional<HALF, _Float16, float>::type T;
+    typedef T V __attribute__((ext_vector_type(HALF ? N : 4)));
+    if (WHOLE || left >= N) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (_Float16)y[e];
-        if (a.y_vec && j + 8 <= a.n) {
-            *(FQ_GLOBAL f16x8 *)to = v;
-            return;
+        for (int p = 0; p < (HALF ? 1 : N / 4); ++p) {
+            V v;
+#pragma unroll
+            for (int e = 0; e < (HALF ? N : 4); ++e) v[e] = (T)y[p * 4 + e];
+            __builtin_memcpy((FQ_GLOBAL char *)at + p * sizeof v, &v, sizeof v);
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (j + e < a.n) st_global(to + e, v[e]);
-        return;
-    }
-    float *to = (float *)a.y + i * a.ldy + j;
-    if (a.y_vec && j + 8 <= a.n) {
-        *(FQ_GLOBAL f32x4 *)to = f32x4{y[0], y[1], y[2], y[3]};
-        *(FQ_GLOBAL f32x4 *)(to + 4) = f32x4{y[4], y[5], y[6], y[7]};
         return;
     }
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (j + e < a.n) st_global(to + e, y[e]);
-}
-
-// The same of 4 channels.
-__device__ __forceinline__ void store4(const LinearArgs &a, long long i, int j, const float *y)
-{
-    if (a.y16) {
-        _Float16 *to = (_Float16 *)a.y + i * a.ldy + j;
-        typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-        const f16x4 v = {(_Float16)y[0], (_Float16)y[1], (_Float16)y[2], (_Float16)y[3]};
-        if (a.y_vec && j + 4 <= a.n) {
-            *(FQ_GLOBAL f16x4 *)to = v;
-            return;
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (j + e < a.n) st_global(to + e, v[e]);
-        return;
-    }
-    float *to = (float *)a.y + i * a.ldy + j;
-    if (a.y_vec && j + 4 <= a.n) {
-        *(FQ_GLOBAL f32x4 *)to = f32x4{y[0], y[1], y[2], y[3]};
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (j + e < a.n) st_global(to + e, y[e]);
+    for (int e = 0; e < N; ++e)
+        if (e < left) st_global((T *)at + e, (T)y[e]);
 }
 
 // Tile of a block.  Blocks go to the eight XCDs in turn: each gets neighbouring tiles, in groups kGroup token tiles
@@ -367,6 +334,25 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
     for (int j = 0; j < TN; ++j)
 #pragma unroll
         for (int i = 0; i < TM; ++i) sum[j][i] = (i32x16)0;
+    // What the end needs, asked for at the begin where there are registers for it.  A lane ends with channels n_lane to n_lane + 7
+    // of tokens m_lane + kTokens * (0, 1, ...).
+    constexpr int kLanes = TN * 32 / 8, kTokens = 64 / kLanes, kRows = 32 / kTokens;      // lanes of a token, tokens at once, times
+    constexpr bool kEarly = TM * TN <= 4;
+    const int n_lane = n0 + wn + lane % kLanes * 8, m_lane = m0 + wm + lane / kLanes;
+    float ws[8], bias[8], xs[TM * kRows];
+    auto ask_scales = [&] {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int j = min(n_lane + e, a.n - 1);
+            ws[e] = ld_global(a.ws + (long long)j * a.ws_step);
+            bias[e] = a.bias ? ld_global(a.bias + j) : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < TM * kRows; ++i)
+            xs[i] = ld_global(a.xs + (long long)min(m_lane + i / kRows * 32 + i % kRows * kTokens, a.m - 1) * a.xs_step);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if constexpr (kEarly) ask_scales();
     // The codes of the next 32 are read from LDS before the products of these 32 are begun; so are the first of the next
     // step, behind the barrier, in front of the last products of this one.
     struct Codes { i32x4 w[TN], x[TM]; } now, then;
@@ -444,41 +430,42 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
 
     // 32 tokens at a time: the sums change places through LDS, so that a lane has 8 neighbouring channels of a token and
     // a store instruction whole lines.
-    constexpr int kLanes = TN * 32 / 8;                         // that hold a token
     int *const mine = (int *)(wave < WAVES / 2 ? stage0 : stage1) + (wave % (WAVES / 2)) * (32 * kPitch);
-    const int n = n0 + wn + lane % kLanes * 8;
-    float ws[8], bias[8];
+    if constexpr (!kEarly) ask_scales();
+    auto finish = [&](auto half, auto whole) {
+        const long long row_bytes = a.ldy * (half ? 2 : 4);
+        char *const y0 = (char *)a.y + (long long)m_lane * row_bytes + (long long)n_lane * (half ? 2 : 4);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int j = min(n + e, a.n - 1);
-        ws[e] = ld_global(a.ws + (long long)j * a.ws_step);
-        bias[e] = a.bias ? ld_global(a.bias + j) : 0.0f;
-    }
+        for (int i = 0; i < TM; ++i) {
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
+            for (int j = 0; j < TN; ++j)
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
+                for (int g = 0; g < 4; ++g)
+                    *(i32x4 *)(mine + (lane % 32) * kPitch + j * 32 + g * 8 + lane / 32 * 4) =
+                        i32x4{sum[j][i][4 * g], sum[j][i][4 * g + 1], sum[j][i][4 * g + 2], sum[j][i][4 * g + 3]};
+            lanes_in_step();
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                *(i32x4 *)(mine + (lane % 32) * kPitch + j * 32 + g * 8 + lane / 32 * 4) =
-                    i32x4{sum[j][i][4 * g], sum[j][i][4 * g + 1], sum[j][i][4 * g + 2], sum[j][i][4 * g + 3]};
-        lanes_in_step();
+            for (int t = 0; t < kRows; ++t) {
+                const int row = i * 32 + t * kTokens;
+                const int *from = mine + (t * kTokens + lane / kLanes) * kPitch + lane % kLanes * 8;
+                const i32x4 low = *(const i32x4 *)from, high = *(const i32x4 *)(from + 4);
+                float y[8];
 #pragma unroll
-        for (int t = 0; t < 32; t += 64 / kLanes) {
-            const int row = t + lane / kLanes, m = m0 + wm + i * 32 + row;
-            const int *from = mine + row * kPitch + lane % kLanes * 8;
-            const i32x4 low = *(const i32x4 *)from, high = *(const i32x4 *)(from + 4);
-            if (m >= a.m || n >= a.n) continue;
-            const float xs = ld_global(a.xs + (long long)m * a.xs_step);
-            float y[8];
+                for (int e = 0; e < 8; ++e) y[e] = (float)(e < 4 ? low[e] : high[e - 4]) * (xs[i * kRows + t] * ws[e]);
+                if (a.bias)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                y[e] = (float)(e < 4 ? low[e] : high[e - 4]) * (xs * ws[e]);
-                if (a.bias) y[e] += bias[e];
+                    for (int e = 0; e < 8; ++e) y[e] += bias[e];
+                if (m_lane + row < a.m) store_channels<half, whole, 8>(y0 + row * row_bytes, y, a.n - n_lane);
             }
-            store8(a, m, n, y);
+            lanes_in_step();
         }
-        lanes_in_step();
+    };
+    if (n0 + wn + TN * 32 <= a.n) {
+        if (a.y16) finish(std::true_type{}, std::true_type{});
+        else finish(std::false_type{}, std::true_type{});
+    } else {
+        if (a.y16) finish(std::true_type{}, std::false_type{});
+        else finish(std::false_type{}, std::false_type{});
     }
 }
 
@@ -755,29 +742,41 @@ __global__ __launch_bounds__(kRowsWaves * 64) void linear_rows_kernel(LinearArgs
             }
             if (tile + WAVES < tiles) load_w(tile + WAVES, j);
         }
+        const int n = tile * CH * 16 + lane / 16 * 4;
+        float ws[CH][4], bias[CH][4];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int n = (tile * CH + c) * 16 + lane / 16 * 4;
-            float ws[4], bias[4];
+        for (int c = 0; c < CH; ++c)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int j = min(n + e, a.n - 1);
-                ws[e] = ld_global(a.ws + (long long)j * a.ws_step);
-                bias[e] = a.bias ? ld_global(a.bias + j) : 0.0f;
+                const int j = min(n + c * 16 + e, a.n - 1);
+                ws[c][e] = ld_global(a.ws + (long long)j * a.ws_step);
+                bias[c][e] = a.bias ? ld_global(a.bias + j) : 0.0f;
             }
-            if (n >= a.n) continue;
+        auto finish = [&](auto half, auto whole) {
 #pragma unroll
             for (int t = 0; t < TOK; ++t) {
                 const int m = m0 + t * 16 + lane % 16;
                 const float xs = scales[t * 16 + lane % 16];
-                float y[4];
+                char *const to = (char *)a.y + ((long long)m * a.ldy + n) * (half ? 2 : 4);
+                if (m >= a.m) continue;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    y[e] = (float)sum[c][t][e] * (xs * ws[e]);
-                    if (a.bias) y[e] += bias[e];
+                for (int c = 0; c < CH; ++c) {
+                    float y[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[e] = (float)sum[c][t][e] * (xs * ws[c][e]);
+                    if (a.bias)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[e] += bias[c][e];
+                    store_channels<half, whole, 4>(to + c * 16 * (half ? 2 : 4), y, a.n - n - c * 16);
                 }
-                if (m < a.m) store4(a, m, n, y);
             }
+        };
+        if ((tile + 1) * CH * 16 <= a.n) {
+            if (a.y16) finish(std::true_type{}, std::true_type{});
+            else finish(std::false_type{}, std::true_type{});
+        } else {
+            if (a.y16) finish(std::true_type{}, std::false_type{});
+            else finish(std::false_type{}, std::false_type{});
         }
     }
 }
@@ -786,6 +785,7 @@ template <typename X, int TOK, int CH> int launch_rows_of(const LinearArgs &a, v
 {
     const unsigned blocks = (unsigned)(((long long)a.m + TOK * 16 - 1) / (TOK * 16));
     if (a.k <= 256) linear_rows_kernel<X, TOK, CH, 2><<<blocks, kRowsWaves * 64, 0, (hipStream_t)stream>>>(a);
+    else if (a.k <= 384) linear_rows_kernel<X, TOK, CH, 3><<<blocks, kRowsWaves * 64, 0, (hipStream_t)stream>>>(a);
     else linear_rows_kernel<X, TOK, CH, 4><<<blocks, kRowsWaves * 64, 0, (hipStream_t)stream>>>(a);
     return (int)hipGetLastError();
 }
@@ -816,6 +816,8 @@ template <typename T, int L, int V> static int quantize_rows_by(const QuantizeAr
 template <typename T> static int quantize_rows(const QuantizeArgs &a, void *stream)
 {
     if (a.k <= 128) return quantize_rows_by<T, 16, 1>(a, stream);
+    if (a.k <= 256) return quantize_rows_by<T, 16, 2>(a, stream);
+    if (a.k <= 384) return quantize_rows_by<T, 16, 3>(a, stream);
     if (a.k <= 512) return quantize_rows_by<T, 16, 4>(a, stream);
     if (a.k <= 2048) return quantize_rows_by<T, 64, 4>(a, stream);
     return quantize_rows_by<T, 256, 4>(a, stream);
