@@ -26,7 +26,7 @@ struct LinearArgs {
     int kx, kw;                // codes of a row of x and w that the tiles read: whole 16; k, or more where zeros lie behind k
     int xs_step, ws_step;
     int x16, x_vec;            // of raw, 1: FP16; rows on 16-byte boundaries
-    int y16;                   // 1: y is FP16
+    int y16, y_lines;          // 1: y is FP16; its rows begin on 128-byte lines
     int w_fits;                // 1: rows of w begin on 16-byte boundaries, k is a multiple of 16, the pitch is at most kMostPitch
 };
 

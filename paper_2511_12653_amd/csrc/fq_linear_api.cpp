@@ -104,6 +104,7 @@ fq_status run(const fq_linear &d, void *workspace, size_t ws_bytes, void *stream
     a.w = d.w; a.ws = d.ws; a.ldw = d.ldw; a.ws_step = d.ws_step;
     a.bias = d.bias; a.y = d.y; a.ldy = d.ldy; a.y16 = d.y_dtype == FQ_F16;
     a.m = (int)d.m; a.n = (int)d.n; a.k = a.kx = a.kw = (int)d.k;
+    a.y_lines = aligned(a.y, 128) && (size_t)a.ldy * size_of(d.y_dtype) % 128 == 0;
     a.w_fits = w_fits;
     a.x16 = d.x_dtype == FQ_F16;
     a.x_vec = aligned(d.x, 16) && (size_t)d.ldx * size_of(d.x_dtype) % 16 == 0;
