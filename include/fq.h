@@ -303,7 +303,8 @@ fq_status fq_distill_loss_no_poll(const fq_distill *d, void *workspace, size_t w
  * own, with g = grad * *grad_scale:
  *   m <- beta1*m + (1-beta1)*g;   v <- beta2*v + ((1-beta2)*g)*g;   r = sqrt(v)
  *   p <- p*(1 - lr*weight_decay) - (lr/(1-beta1^step)) * (m / (r/sqrt(1-beta2^step) + eps)),   lr = lr * lr_scale
- * (root and quotient of the last line to 2 units in the last place; they go into p, and into the codes of r, alone).
+ * (the root is the correctly rounded one; the quotient of the last line, which goes into p alone, is right to 2 units in the
+ * last place).
  * An element whose new v is not finite (a gradient that is NaN or infinite, or whose (1-beta2)*g*g overflows) keeps m, v and p; so a
  * grad_scale of NaN or infinity leaves the whole list as it is.  The constants are evaluated in binary64 on the host and
  * rounded to binary32 once each.

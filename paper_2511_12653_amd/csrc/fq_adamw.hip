@@ -74,12 +74,13 @@ __device__ __forceinline__ unsigned mix(unsigned x)
 
 // The e4m3 value at or below a (0 <= a <= 448) raised by (u + 1/2) / 2^16 of the step between codes: adding that
 // to the 20 mantissa bits that a code lacks, and cutting them off.  Below 2^-6 the steps stay those of the binade
-// above, where adding 2^-6 puts a.  more: 16 u + 8.
-__device__ __forceinline__ float round_code(float a, unsigned more)
+// above, where adding 2^-6 puts a.  more: 16 u + 8.  near: the least distance, plus 2, of the sums from a multiple of 2^20 so far.
+__device__ __forceinline__ float round_code(float a, unsigned more, unsigned &near)
 {
     const float low = a < 0x1p-6f ? 0x1p-6f : 0.0f;
-    const unsigned z = (__builtin_bit_cast(unsigned, a + low) + more) & 0xFFF00000u;
-    return __builtin_bit_cast(float, z) - low;
+    const unsigned z = __builtin_bit_cast(unsigned, a + low) + more, far = (z + 2u) & 0xFFFFFu;
+    near = near < far ? near : far;
+    return __builtin_bit_cast(float, z & 0xFFF00000u) - low;
 }
 
 __device__ __forceinline__ unsigned pack4(const float *c)
@@ -157,8 +158,8 @@ __device__ __forceinline__ void step_rows(const AdamwTensor &t, const AdamwStep 
             store4<float>(t.v, i, vec, left, vn);
             continue;
         }
-        // What bounds this is the arithmetic (about 70 instructions an element; with exact root and quotient, a guard
-        // per element and four products to a hash it was 114, 57 us for 20 million FP16 elements).
+        // What bounds this is the arithmetic (about 75 instructions an element; with the compiler's root and quotient, a
+        // guard per element and four products to a hash it was 114: 20 million FP16 elements 53 us, now 43).
         float m[4], v[4];
         unsigned both;
         auto moments = [&](bool guarded) {
@@ -188,35 +189,43 @@ __device__ __forceinline__ void step_rows(const AdamwTensor &t, const AdamwStep 
         const int e2 = max((int)(both >> 16) - 127 - 17, -126);
         const int ev = (e2 + 1) >> 1;
         const float down_m = power_of_two(-em), down_v = power_of_two(-2 * ev), up = power_of_two(ev) * s.root_factor;
-        // A root over 2^72 times smaller than the block's greatest is lost in its units.  Beside eps it does not matter,
-        // unless the greatest is large or eps tiny.
-        const bool careful = odd || !(up * 0x1p-62f <= s.eps * 0x1p-26f);
         const unsigned place = (t.place + (unsigned)i) * kPlace + s.key;
         float cm[4], cv[4];
         P4 pn;
         f16x4 copy;
+        unsigned near = ~0u, nothing = 0;
+        // The root in units of the scale: the rounding of a scaled number is that of the number.
+        auto codes = [&](int j, float root) {
+            const unsigned bits = mix(place + (unsigned)j * kPlace);
+            cm[j] = __builtin_copysignf(round_code(__builtin_fabsf(m[j]) * down_m, (bits & 0xFFFFu) << 4 | 8u, nothing), m[j]);
+            cv[j] = __builtin_fmaxf(round_code(root, (bits >> 12 & 0xFFFF0u) | 8u, near), v[j] > 0.0f ? 0x1p-9f : 0.0f);
+        };
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const unsigned bits = mix(place + (unsigned)j * kPlace);
-            // the root in units of the scale: at most 448 (one rounding more would make a code that is none), and never 0
-            // under the quotient
-            const float root = __builtin_amdgcn_fmed3f(__builtin_amdgcn_sqrtf(v[j] * down_v), 0x1p-64f, 448.0f);
-            const float p0 = (float)p4[r][j];
-            float p = p0 * keep - lrc * (m[j] * __builtin_amdgcn_rcpf(root * up + s.eps));
-            if (careful) {
-                p = p0 * keep - lrc * (m[j] / (__builtin_sqrtf(v[j]) * s.root_factor + s.eps));
-                if (odd) {                                       // (a gradient that was not finite leaves no trace in m and v)
-                    float m0[4], v0[4];
-                    unpack4(m8[r], m0);
-                    unpack4(v8[r], v0);
-                    const float g = (float)g4[r][j] * gs, r0 = v0[j] * vs[r], v1 = s.beta2 * (r0 * r0) + (s.one_minus_beta2 * g) * g;
-                    if (!(__builtin_fabsf(v1) < __builtin_inff())) p = p0;
-                }
-            }
+            const float root = __builtin_amdgcn_sqrtf(v[j] * down_v);
+            const float p = (float)p4[r][j] * keep - lrc * (m[j] * __builtin_amdgcn_rcpf(root * up + s.eps));
             pn[j] = (P)p;
             copy[j] = (_Float16)p;
-            cm[j] = __builtin_copysignf(round_code(__builtin_fabsf(m[j]) * down_m, (bits & 0xFFFFu) << 4 | 8u), m[j]);
-            cv[j] = __builtin_fmaxf(round_code(root, (bits >> 12 & 0xFFFF0u) | 8u), v[j] > 0.0f ? 0x1p-9f : 0.0f);
+            codes(j, root);
+        }
+        // The hardware's root is one unit off at most.  Where that may make another code, which has to follow from the
+        // rounded root alone, it is worked out again; few wavefronts are.  So they are where the greatest v is large or eps tiny: a
+        // root over 2^62 times smaller than the greatest is lost in the units, which otherwise does not matter beside eps.
+        if (__builtin_expect(odd || !(up * 0x1p-62f <= s.eps * 0x1p-26f) || __ballot(near <= 4u), 0)) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float g = (float)g4[r][j] * gs, p0 = (float)p4[r][j];
+                float m0[4], v0[4];
+                unpack4(m8[r], m0);
+                unpack4(v8[r], v0);
+                const float r0 = v0[j] * vs[r], v1 = s.beta2 * (r0 * r0) + (s.one_minus_beta2 * g) * g;
+                const float root = __builtin_sqrtf(v[j]);
+                float p = p0 * keep - lrc * (m[j] / (root * s.root_factor + s.eps));
+                if (!(__builtin_fabsf(v1) < __builtin_inff())) p = p0;    // (a gradient that was not finite leaves no trace in m and v)
+                pn[j] = (P)p;
+                copy[j] = (_Float16)p;
+                codes(j, __builtin_sqrtf(v[j] * down_v));
+            }
         }
         store4<P>(t.p, i, vec, left, pn);
         if (t.p16) store4<_Float16>(t.p16, i, vec, left, copy);

@@ -148,5 +148,9 @@ def step(p, g, m, v, m_scale, v_scale, h, place, lr_scale=1.0, weight_decay=0.0,
         code = round_codes(np.maximum(value, 0.0), high)
         code = np.where(vb > 0, np.maximum(code, 2.0 ** -9), 0.0)
         out[name] = np.minimum(code, 448.0).reshape(-1)[:n]
+    # and the code of the binary32 root, which is the one to expect
+    a = np.sqrt(vb).astype(np.float64) * down(ev)
+    a = np.where(a < 2.0 ** -6, (a.astype(np.float32) + F32(2.0 ** -6)).astype(np.float64) - 2.0 ** -6, a)
+    out["v8"] = np.where(vb > 0, np.maximum(round_codes(a, high), 2.0 ** -9), 0.0).reshape(-1)[:n]
     out["m_scale"], out["v_scale"] = np.exp2(em.astype(np.float64)), np.exp2(ev.astype(np.float64))
     return out

@@ -188,6 +188,24 @@ def test_magnitudes(spread, f8):
     run([Tensor(rng, 2000, f8=f8, spread=spread), Tensor(rng, 500, f8=f8, spread=spread, fresh=True)], "spread %g" % spread, steps=3)
 
 
+@pytest.mark.parametrize("spread", [1e-12, 1e-3, 1.0, 1e9])
+def test_codes_follow_from_the_rounded_root(spread):
+    """Bit by bit over many elements and steps: a root that is one unit off changes one code in a hundred thousand."""
+    rng = np.random.Generator(np.random.Philox(12))
+    t = Tensor(rng, 1 << 20, g="f16" if spread == 1.0 else "f32", f8=True, spread=spread)
+    plan, ws = make_plan([t])
+    h = dict(HYPER)
+    hy = fq.FqAdamW(**h)
+    for i in range(3):
+        h["step"] = hy.step = 50 + i
+        want = t.reference(h, 0, None)
+        fq.fq_adamw_step(plan, hy)
+        torch.cuda.synchronize()
+        t.compare(want, "rounded root, step %d" % i)
+        assert np.array_equal(t.v.host(), want["v8"].astype(np.float32))
+    fq.fq_adamw_destroy(plan)
+
+
 @pytest.mark.parametrize("f8", [False, True])
 def test_fresh_states_zero_gradients_and_other_constants(f8):
     rng = np.random.Generator(np.random.Philox(7))
