@@ -115,10 +115,40 @@ template <typename T> __device__ __forceinline__ u32x2 codes8(const Eight<T> &r,
     return w;
 }
 
+// Rows of codes at any address, laid out anew for the tiles: on 16-byte boundaries, zeros behind k.  A thread moves 16.
+__device__ __forceinline__ void align_rows(const AlignArgs &a, unsigned block)
+{
+    const unsigned each = (unsigned)(a.pitch / 16);
+    const unsigned long long i = (unsigned long long)block * 256 + threadIdx.x;
+    const long long row = (long long)(i / each);
+    const int l = (int)(i % each) * 16;
+    if (row >= a.rows) return;
+    const int8_t *from = a.from + row * a.ld + l;
+    i32x4 r = {0, 0, 0, 0};
+    if (l + 16 <= a.k) {
+        __builtin_memcpy(&r, (const FQ_GLOBAL int8_t *)from, 16);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (l + j < a.k) r[j / 4] |= (int)((unsigned)(unsigned char)ld_global(from + j) << (8 * (j % 4)));
+    }
+    *(FQ_GLOBAL i32x4 *)(a.to + row * a.pitch + l) = r;
+}
+
+__global__ __launch_bounds__(256) void align_rows_kernel(AlignArgs a, unsigned blocks, AlignArgs other)
+{
+    if (blockIdx.x < blocks) align_rows(a, blockIdx.x);
+    else align_rows(other, blockIdx.x - blocks);
+}
+
 // A row to L lanes.  Rows of more than 8 * L * V values are read again for the codes.
 template <typename T, int L, int V>
-__global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs a)
+__global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs a, unsigned blocks, AlignArgs other)
 {
+    if (blockIdx.x >= blocks) {
+        align_rows(other, blockIdx.x - blocks);
+        return;
+    }
     __shared__ unsigned top[4];
     const int at = threadIdx.x % L * 8;
     const long long row = (long long)blockIdx.x * (256 / L) + threadIdx.x / L;
@@ -155,27 +185,6 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs a)
         odd_end(more, x, i, a.k);
         *(FQ_GLOBAL u32x2 *)(q + i) = codes8(more, r, i >= a.k);
     }
-}
-
-// ---------------------------------------------------------------------------------------------
-// Rows of codes at any address, laid out anew for the tiles: on 16-byte boundaries, zeros behind k.  A thread moves 16.
-__global__ __launch_bounds__(256) void align_rows_kernel(AlignArgs a)
-{
-    const unsigned each = (unsigned)(a.pitch / 16);
-    const unsigned long long i = (unsigned long long)blockIdx.x * 256 + threadIdx.x;
-    const long long row = (long long)(i / each);
-    const int l = (int)(i % each) * 16;
-    if (row >= a.rows) return;
-    const int8_t *from = a.from + row * a.ld + l;
-    i32x4 r = {0, 0, 0, 0};
-    if (l + 16 <= a.k) {
-        __builtin_memcpy(&r, (const FQ_GLOBAL int8_t *)from, 16);
-    } else {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (l + j < a.k) r[j / 4] |= (int)((unsigned)(unsigned char)ld_global(from + j) << (8 * (j % 4)));
-    }
-    *(FQ_GLOBAL i32x4 *)(a.to + row * a.pitch + l) = r;
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -804,33 +813,39 @@ template <int BM, int BN, int WM, int WN, int STAGES> int launch_tiles(const Lin
 
 }  // namespace
 
-int launch_align_rows(const AlignArgs &a, void *stream)
+static unsigned align_blocks(const AlignArgs &a)
 {
-    const unsigned long long pieces = (unsigned long long)a.rows * (unsigned long long)(a.pitch / 16);
-    align_rows_kernel<<<(unsigned)((pieces + 255) / 256), 256, 0, (hipStream_t)stream>>>(a);
+    return (unsigned)(((unsigned long long)a.rows * (unsigned long long)(a.pitch / 16) + 255) / 256);
+}
+
+int launch_align_rows(const AlignArgs &a, const AlignArgs &other, void *stream)
+{
+    const unsigned blocks = align_blocks(a);
+    align_rows_kernel<<<blocks + align_blocks(other), 256, 0, (hipStream_t)stream>>>(a, blocks, other);
     return (int)hipGetLastError();
 }
 
-template <typename T, int L, int V> static int quantize_rows_by(const QuantizeArgs &a, void *stream)
+template <typename T, int L, int V> static int quantize_rows_by(const QuantizeArgs &a, const AlignArgs &other, void *stream)
 {
-    quantize_rows_kernel<T, L, V><<<(unsigned)(((long long)a.m + 256 / L - 1) / (256 / L)), 256, 0, (hipStream_t)stream>>>(a);
+    const unsigned blocks = (unsigned)(((long long)a.m + 256 / L - 1) / (256 / L));
+    quantize_rows_kernel<T, L, V><<<blocks + align_blocks(other), 256, 0, (hipStream_t)stream>>>(a, blocks, other);
     return (int)hipGetLastError();
 }
 
 // Short rows share a wavefront: what a row costs beside its values is then paid once for four.
-template <typename T> static int quantize_rows(const QuantizeArgs &a, void *stream)
+template <typename T> static int quantize_rows(const QuantizeArgs &a, const AlignArgs &other, void *stream)
 {
-    if (a.k <= 128) return quantize_rows_by<T, 16, 1>(a, stream);
-    if (a.k <= 256) return quantize_rows_by<T, 16, 2>(a, stream);
-    if (a.k <= 384) return quantize_rows_by<T, 16, 3>(a, stream);
-    if (a.k <= 512) return quantize_rows_by<T, 16, 4>(a, stream);
-    if (a.k <= 2048) return quantize_rows_by<T, 64, 4>(a, stream);
-    return quantize_rows_by<T, 256, 4>(a, stream);
+    if (a.k <= 128) return quantize_rows_by<T, 16, 1>(a, other, stream);
+    if (a.k <= 256) return quantize_rows_by<T, 16, 2>(a, other, stream);
+    if (a.k <= 384) return quantize_rows_by<T, 16, 3>(a, other, stream);
+    if (a.k <= 512) return quantize_rows_by<T, 16, 4>(a, other, stream);
+    if (a.k <= 2048) return quantize_rows_by<T, 64, 4>(a, other, stream);
+    return quantize_rows_by<T, 256, 4>(a, other, stream);
 }
 
-int launch_quantize_rows(const QuantizeArgs &a, void *stream)
+int launch_quantize_rows(const QuantizeArgs &a, const AlignArgs &other, void *stream)
 {
-    return a.x16 ? quantize_rows<_Float16>(a, stream) : quantize_rows<float>(a, stream);
+    return a.x16 ? quantize_rows<_Float16>(a, other, stream) : quantize_rows<float>(a, other, stream);
 }
 
 // The tiles, and what a step of 128 codes of a block takes: at least `wait`, and `work` for each block that a compute unit

@@ -8,6 +8,7 @@ namespace fq {
 namespace {
 
 constexpr size_t kAlign = 256;
+constexpr long long kMostRows = 1LL << 23;       // of x to a launch: a grid has less than 2^32 threads, a row up to 256 of them
 
 size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
@@ -88,16 +89,10 @@ fq_status validate(const fq_linear &d)
     return FQ_OK;
 }
 
-fq_status run(const fq_linear &d, void *workspace, size_t ws_bytes, void *stream)
+fq_status run(const fq_linear &d, void *workspace, void *stream)
 {
-    const fq_status st = validate(d);
-    if (st != FQ_OK || d.m == 0 || d.n == 0) return st;
     const Workspace at = workspace_of(d);
     const bool quantize = d.x_dtype != FQ_I8, x_fits = !quantize && fits(d.x, d.ldx, d.k), w_fits = fits(d.w, d.ldw, d.k);
-    if (!x_fits || !w_fits) {
-        if (!workspace || ws_bytes < at.bytes) return FQ_ERR_WORKSPACE;
-        if (!aligned(workspace, kAlign)) return FQ_ERR_ALIGN;
-    }
     LinearArgs a;
     std::memset(&a, 0, sizeof a);
     a.x = (const int8_t *)d.x; a.xs = d.xs; a.ldx = d.ldx; a.xs_step = d.xs_step;
@@ -113,33 +108,55 @@ fq_status run(const fq_linear &d, void *workspace, size_t ws_bytes, void *stream
         return launch_linear(a, stream) == 0 ? FQ_OK : FQ_ERR_LAUNCH;
     }
     int8_t *const codes = (int8_t *)workspace;
+    AlignArgs w;
+    std::memset(&w, 0, sizeof w);
+    if (!w_fits && a.k > 0 && !linear_few(a, 1)) {
+        w = {a.w, codes + at.w, d.n, d.ldw, at.pitch, a.k};
+        a.w = w.to;
+        a.ldw = at.pitch;
+        a.kw = (int)at.pitch;
+    }
     if (quantize && linear_rows(a)) {
         a.raw = d.x;
+        if (w.rows && launch_align_rows(w, {}, stream) != 0) return FQ_ERR_LAUNCH;
     } else if (quantize) {
         QuantizeArgs q;
         std::memset(&q, 0, sizeof q);
         q.x = d.x; q.ldx = d.ldx; q.m = a.m; q.k = a.k; q.x16 = a.x16;
         q.q = codes; q.s = (float *)(codes + at.scales); q.pitch = at.pitch;
-        if (launch_quantize_rows(q, stream) != 0) return FQ_ERR_LAUNCH;
+        if (launch_quantize_rows(q, w, stream) != 0) return FQ_ERR_LAUNCH;
         a.xs = q.s;
         a.xs_step = 1;
-    } else if (!x_fits && a.k > 0) {
-        const AlignArgs r = {a.x, codes, d.m, d.ldx, at.pitch, a.k};
-        if (launch_align_rows(r, stream) != 0) return FQ_ERR_LAUNCH;
+    } else if (a.k > 0 && (!x_fits || w.rows)) {
+        const AlignArgs x = {a.x, codes, x_fits ? 0 : d.m, d.ldx, at.pitch, a.k};
+        if (launch_align_rows(x, w, stream) != 0) return FQ_ERR_LAUNCH;
     }
     if (!x_fits && !a.raw) {
         a.x = codes;
         a.ldx = at.pitch;
         a.kx = (int)at.pitch;
     }
-    if (!w_fits && a.k > 0 && !linear_few(a, 1)) {
-        const AlignArgs r = {a.w, codes + at.w, d.n, d.ldw, at.pitch, a.k};
-        if (launch_align_rows(r, stream) != 0) return FQ_ERR_LAUNCH;
-        a.w = r.to;
-        a.ldw = at.pitch;
-        a.kw = (int)at.pitch;
-    }
     return launch_linear(a, stream) == 0 ? FQ_OK : FQ_ERR_LAUNCH;
+}
+
+fq_status forward(const fq_linear &d, void *workspace, size_t ws_bytes, void *stream)
+{
+    const fq_status st = validate(d);
+    if (st != FQ_OK || d.m == 0 || d.n == 0) return st;
+    if (d.x_dtype != FQ_I8 || !fits(d.x, d.ldx, d.k) || !fits(d.w, d.ldw, d.k)) {
+        if (!workspace || ws_bytes < workspace_of(d).bytes) return FQ_ERR_WORKSPACE;
+        if (!aligned(workspace, kAlign)) return FQ_ERR_ALIGN;
+    }
+    for (long long row = 0; row < d.m; row += kMostRows) {
+        fq_linear part = d;
+        part.m = d.m - row < kMostRows ? d.m - row : kMostRows;
+        part.x = d.x ? (const char *)d.x + (size_t)(row * d.ldx) * size_of(d.x_dtype) : nullptr;
+        part.xs = d.xs ? d.xs + row * d.xs_step : nullptr;
+        part.y = (char *)d.y + (size_t)(row * d.ldy) * size_of(d.y_dtype);
+        const fq_status ran = run(part, workspace, stream);
+        if (ran != FQ_OK) return ran;
+    }
+    return FQ_OK;
 }
 
 }  // namespace
@@ -155,7 +172,7 @@ size_t fq_linear_workspace_bytes(const fq_linear *d)
 fq_status fq_linear_forward(const fq_linear *d, void *workspace, size_t ws_bytes, void *hip_stream)
 {
     if (!d) return FQ_ERR_NULL;
-    return fq::run(*d, workspace, ws_bytes, hip_stream);
+    return fq::forward(*d, workspace, ws_bytes, hip_stream);
 }
 
 }  // extern "C"

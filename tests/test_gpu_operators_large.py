@@ -33,6 +33,29 @@ def test_rows_gigabytes_apart(m, k):
     R.check_linear(yd.cpu().numpy(), y, off, True, "far")
 
 
+@pytest.mark.parametrize("k,n,codes", [(8, 3, False), (16, 16, False), (9, 5, True)])
+def test_more_rows_than_a_launch_takes(k, n, codes):
+    m = (1 << 23) + 21
+    H.say("linear, %d rows of %d" % (m, k))
+    gen = torch.Generator(device="cuda").manual_seed(k)
+    x = torch.randn((m, k), generator=gen, device="cuda").to(torch.float16)
+    q, s = x, None
+    if codes:
+        q = torch.randint(-127, 128, (m, k), generator=gen, device="cuda", dtype=torch.int8)
+        s = torch.rand(m, generator=gen, device="cuda") + 0.5
+    rng = np.random.Generator(np.random.Philox(n))
+    w = rng.integers(-127, 128, (n, k)).astype(np.int8)
+    ws, b = rng.uniform(1e-3, 2e-3, n).astype(np.float32), rng.standard_normal(n).astype(np.float32)
+    y = torch.full((m, n), 7.0, device="cuda")
+    d = fq.FqLinear.from_torch(q, H.dev(w), H.dev(ws), y, bias=H.dev(b), x_scale=s)
+    fq.fq_linear_forward(d, torch.empty(fq.fq_linear_workspace_bytes(d), dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    for part in (slice(0, 300), slice((1 << 23) - 150, m)):
+        xq, xs = (q[part].cpu().numpy(), s[part].cpu().numpy()) if codes else R.quantize_rows(x[part].cpu().numpy())
+        want, off = R.linear(xq, xs, w, ws, b, False)
+        R.check_linear(y[part].cpu().numpy(), want, off, False, "rows %d to %d" % (part.start, part.stop))
+
+
 def test_a_tensor_of_more_than_two_billion_elements():
     n = (1 << 31) + 777
     H.say("adamw, %d elements" % n)
