@@ -1,4 +1,15 @@
 // AdamW over a list of tensors in one launch, moments in FP32 or in FP8 (declared in include/fq.h).
+//
+//   m' = beta1 m + (1 - beta1) g,  v' = beta2 v + (1 - beta2) g^2,  p' = p (1 - lr wd) - lr / (1 - beta1^t) m' / (sqrt(v') /
+//   sqrt(1 - beta2^t) + eps)
+//
+// Every element is read and written once and depends on no other; in FP8 the 256 elements of a state block share a scale, which is known
+// when all their new moments are.  Hence a state block to a wavefront, four elements to a lane: the block's greatest moments are one
+// reduction in registers, and no LDS or barrier is needed.  A grid block has one tensor, so all branches on types are uniform.
+//
+// With FP32 states memory bounds it: 120 million elements 544 us, 6.2 TB/s.  In FP8 it is memory too where the elements have many
+// bytes (240 million, FP32 p, FP16 g and copy: 16 bytes each, 640 us, 6.0 TB/s), and arithmetic where they have few (20 million in FP16: 10
+// bytes each, 44 us, 4.5 TB/s).  Short lists cost the launch and a trip to memory or two (88 tensors, 0.4 million elements: 4.2 us).
 #include <hip/hip_fp16.h>
 
 #include "fq_adamw.h"

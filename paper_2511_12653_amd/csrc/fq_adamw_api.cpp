@@ -18,6 +18,7 @@ constexpr long long kAdamwOneRow = 1 << 21;
 // Up to so many grid blocks the table has a descriptor for each: the search for the block's tensor, a trip to memory in front
 // of all others, falls away (88 tensors, 436 blocks: the kernel 2.8 us at best, with the search 3.7).
 constexpr long long kAdamwBlockTable = 2048;
+constexpr long long kAdamwMostBlocks = 0xffffffffLL / kAdamwThreads;      // a grid has less than 2^32 threads
 
 struct Range {
     uintptr_t at;
@@ -80,7 +81,7 @@ fq_status shape_of(const fq_param *ps, int n, Shape &shape)
     const long long per = (long long)kAdamwRowElems * shape.rows;
     for (int i = 0; i < n; ++i) {
         shape.blocks += (ps[i].n + per - 1) / per;
-        if (shape.blocks > 0x7fffffffLL) return FQ_ERR_SHAPE;
+        if (shape.blocks > kAdamwMostBlocks) return FQ_ERR_SHAPE;
     }
     shape.by_block = shape.rows == 1 && shape.blocks <= kAdamwBlockTable;
     shape.entries = shape.by_block ? shape.blocks : n;

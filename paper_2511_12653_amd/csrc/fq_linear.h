@@ -11,7 +11,8 @@ constexpr long long kCodePitch = 128;            // rows of codes in the workspa
 
 constexpr long long kMostPitch = 1 << 22;        // of rows of codes that the tiles take: 256 of them have 32-bit offsets
 constexpr int kFewLds = 150 << 10;               // most LDS of a block of few tokens
-constexpr int kFewMostN = 16 * 256;              // most channels there: a block to a compute unit
+constexpr int kFewLdsOfTwo = 78 << 10;           // most of a block that leaves room for another
+constexpr int kFewMostN = 16 * 256;              // channels there of a block to a compute unit
 
 struct LinearArgs {
     const int8_t *x;           // codes, in rows that fit (see w_fits)

@@ -1,4 +1,12 @@
 // Int8 linear layer with a scale per token and per channel (declared in include/fq.h).
+//
+//   y_ij = (sum_k q_ik w_jk) * (xs_i * ws_j) + bias_j          the sum exact in 32 bits, the rest in binary32
+//   xs_i = max_k |x_ik| / 127,  q_ik = round(x_ik / xs_i)      where x comes in FP16 or FP32
+//
+// Up to 16 tokens: linear_few_kernel does all of it in one launch, bound by the stream of w.  Short rows and few channels:
+// linear_rows_kernel, one launch, bound by x and y.  All else: quantize_rows_kernel, bound by memory, and linear_tile_kernel, bound
+// by the matrix cores or, in few tiles, by what a compute unit can load.  Quantizing inside the tiles would do it again for every tile
+// of channels: n / 256 times.  Sizes below are m x n x k, tokens by channels by values of a row.
 #include <type_traits>
 
 #include "fq_device.h"
@@ -141,7 +149,13 @@ __global__ __launch_bounds__(256) void align_rows_kernel(AlignArgs a, unsigned b
     else align_rows(other, blockIdx.x - blocks);
 }
 
-// A row to L lanes.  Rows of more than 8 * L * V values are read again for the codes.
+// A row to L lanes, from the loads to the codes in their registers: x is read once.  (Rows of more than 8 * L * V values are read
+// again for the codes; the second time they come from the caches.)  Bound by memory: 8192 x 8192 FP16 31.4 us, 6.4 TB/s; 600 x 4096
+// 5.0 us, mostly the way to memory and back.  Short rows share a wavefront: what a row costs beside its values is paid
+// once for four (19200 x 384 5.6 us).
+//
+// The blocks behind the first `blocks` lay out w instead, where its rows begin at any address: 301 x 600 x 437 FP32 7.9 us
+// against 10.4 with a launch of its own for that.
 template <typename T, int L, int V>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs a, unsigned blocks, AlignArgs other)
 {
@@ -188,7 +202,13 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs a, unsi
 }
 
 // ---------------------------------------------------------------------------------------------
-// Product of a tile of BM tokens by BN channels.  BM / WM by BN / WN of it belong to a wavefront, which builds them from
+// Product of a tile of BM tokens by BN channels.  What bounds it, by tile: 256 x 256 the matrix cores, which are busy 65 % of the
+// cycles at a clock that their power holds down (8192 x 8192 x 8192 460 us, 2.39 POP/s; codes that are all zero are 12 to 25 % faster);
+// the smaller ones, taken where large ones leave compute units without work, what a compute unit can load, 40 to 50 bytes a cycle (17
+// x 64 x 4096, a block or two in all: 16 KiB of a 64 x 64 step in 0.15 us, 32 KiB of a 128 x 128 step in 0.37).  More stages, and codes
+// read from LDS a whole step ahead, change neither (5 % either way).
+//
+// BM / WM by BN / WN of it belong to a wavefront, which builds them from
 // 32 x 32 matrix instructions: lane l holds 16 codes of channel l % 32 and of token l % 32, and of the sums those of token
 // l % 32 and channels 8 g + 4 (l / 32) + 0..3, g = 0..3.
 //
@@ -484,7 +504,8 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
 }
 
 // ---------------------------------------------------------------------------------------------
-// Up to 16 tokens: what counts is to stream w once.  A block multiplies 16 channels by all tokens (lanes past the last
+// Up to 16 tokens: what counts is to stream w once (1 x 4096 x 4096 FP16 5.4 us a call, 16.8 MB of w, of which the launch
+// of an empty kernel is 1.7).  A block multiplies 16 channels by all tokens (lanes past the last
 // repeat it); its wavefronts share the codes of a row, a run of whole steps of 128 each, and their sums meet in LDS.  Every
 // wavefront has kRing steps of w of its own in LDS or on their way there, so it waits for nobody; the layout is that of the
 // tiles above.  x lies in LDS as a whole: fetched in front of w, and with X FP16 or FP32 turned into codes by the block while
@@ -685,7 +706,8 @@ template <typename X> int launch_few(const LinearArgs &a, void *stream)
 }
 
 // ---------------------------------------------------------------------------------------------
-// Short rows, many tokens: x is read once and its codes never leave the compute unit.  A block has TOK * 16 tokens.  It turns
+// Short rows, many tokens: x is read once and its codes never leave the compute unit (288000 x 128 x 128 FP16 49.4 us, 3.0 TB/s of x and
+// y; codes by a launch of their own and tiles 69.5).  A block has TOK * 16 tokens.  It turns
 // them into codes in LDS, a row to 16 lanes, V vectors each, with all of a wavefront's rows requested before the first is
 // looked at; then every wavefront multiplies all of them by 16 * CH channels at a time.  w, small enough to stay in the L2s,
 // goes from there into registers, whole rows of it: the first before x is quantized, the next as the last are used up.
@@ -832,7 +854,6 @@ template <typename T, int L, int V> static int quantize_rows_by(const QuantizeAr
     return (int)hipGetLastError();
 }
 
-// Short rows share a wavefront: what a row costs beside its values is then paid once for four.
 template <typename T> static int quantize_rows(const QuantizeArgs &a, const AlignArgs &other, void *stream)
 {
     if (a.k <= 128) return quantize_rows_by<T, 16, 1>(a, other, stream);
@@ -849,7 +870,15 @@ int launch_quantize_rows(const QuantizeArgs &a, const AlignArgs &other, void *st
 }
 
 // The tiles, and what a step of 128 codes of a block takes: at least `wait`, and `work` for each block that a compute unit
-// holds at once (`resident` of them at most); `ends` for what is in front of the first step and behind the last (us).
+// holds at once (`resident` of them at most); `ends` for what is in front of the first step and behind the last (us).  The tile
+// with the least sum is taken.  Measured, codes at aligned rows, us, the tiles in the order of the table (- : not in question):
+//   8192 x 8192 x 8192   461   483   565   582   856   1091
+//   2048 x 4096 x 4096  44.5  34.0  37.0  38.3  55.0   73.9
+//   19200 x 384 x 384   12.3   8.8   8.6  11.1  14.4   16.9
+//   600 x 4096 x 4096   41.2  23.1  27.0  17.0  21.6   26.9
+//   256 x 4096 x 4096      -     -     -  15.7  10.3   12.1
+//   446 x 503 x 6144       -     -     -  22.7  12.3   11.3
+//   20 x 16384 x 4096   40.3  22.2  26.2  15.0  12.8   12.5
 struct Tile {
     int m, n, resident;
     double wait, work, ends;
@@ -878,11 +907,15 @@ static double tile_time(const LinearArgs &a, const Tile &t)
     return time;
 }
 
-// Whether the kernel of few tokens takes x of this element size: it fits into LDS beside the rings.
+// Whether the kernel of few tokens takes x of this element size: it fits into LDS beside the rings, and all blocks are on the chip at
+// once, or w does not fit the tiles.  us, this / quantizing and tiles: 1 x 4096 x 4096 FP16 5.4 / 10.7, 16 x 4096 x 4096 8.9 / 11.0, 4 x 4096 x 8192
+// 10.5 / 16.2; two blocks to a compute unit: 1 x 8192 x 4096 8.4 / 11.0, 1 x 8192 x 64 4.6 / 7.6, codes 3 x 8192 x 2048 4.8 / 6.2; not at
+// once: 4 x 8192 x 4096 15.1 / 11.2, codes 16 x 16384 x 4096 20.7 / 12.4.
 bool linear_few(const LinearArgs &a, int size)
 {
-    return a.k > 0 && a.m <= 16 && (a.n <= kFewMostN || !a.w_fits) && a.ldw <= kMostPitch && (long long)a.k * size * a.m <= kFewLds &&
-           few_lds(a.m, a.k, size, true).total <= kFewLds;
+    if (a.k <= 0 || a.m > 16 || a.ldw > kMostPitch || (long long)a.k * size * a.m > kFewLds) return false;
+    const int lds = few_lds(a.m, a.k, size, true).total;
+    return lds <= kFewLds && (!a.w_fits || a.n <= (lds <= kFewLdsOfTwo ? 2 : 1) * kFewMostN);
 }
 
 // Few channels, or the product of 16 tokens takes longer than a trip of their codes to memory.  us, codes by a kernel of their

@@ -58,18 +58,30 @@ int launch_adamw(const AdamwTensor *t, const unsigned *first, int n, const Adamw
 bool linear_few(const LinearArgs &a, int size) { return a.k > 0 && a.m <= 16 && (long long)a.m * a.k * size < 40000; }
 bool linear_rows(const LinearArgs &a) { return a.k >= 16 && a.k <= 512 && a.m >= 1024; }
 
-int launch_quantize_rows(const QuantizeArgs &a, void *)
+static void check_aligned(const AlignArgs &a)
+{
+    CHECK(a.pitch % 128 == 0 && a.pitch >= a.k && a.ld >= a.k && a.rows > 0 && inside(a.to, (size_t)a.rows * (size_t)a.pitch));
+}
+
+int launch_quantize_rows(const QuantizeArgs &a, const AlignArgs &other, void *)
 {
     ++launches;
     CHECK(a.pitch % 128 == 0 && a.pitch >= a.k && inside(a.q, (size_t)a.m * (size_t)a.pitch) && inside(a.s, (size_t)a.m * 4));
     CHECK((char *)a.s >= (char *)a.q + (size_t)a.m * (size_t)a.pitch);
+    if (other.rows) {
+        check_aligned(other);
+        CHECK((char *)other.to >= (char *)(a.s + a.m));
+    }
     return 0;
 }
 
-int launch_align_rows(const AlignArgs &a, void *)
+int launch_align_rows(const AlignArgs &a, const AlignArgs &other, void *)
 {
     ++launches;
-    CHECK(a.pitch % 128 == 0 && a.pitch >= a.k && a.ld >= a.k && a.rows > 0 && inside(a.to, (size_t)a.rows * (size_t)a.pitch));
+    CHECK(a.rows || other.rows);
+    if (a.rows) check_aligned(a);
+    if (other.rows) check_aligned(other);
+    if (a.rows && other.rows) CHECK((char *)other.to >= (char *)a.to + (size_t)a.rows * (size_t)a.pitch);
     return 0;
 }
 
