@@ -34,8 +34,8 @@ def linear_int8(x, w, w_scale, bias=None, x_scale=None, out=None, out_dtype=None
             raise ValueError("out must have shape %s and the wanted type" % (shape,))
         y = out.view(rows, n)                       # (raises where the rows are no view of it)
     x2 = x.reshape(rows, k)
-    if k > 1 and x2.stride(1) != 1:
-        x2 = x2.contiguous()
+    if (k > 1 and x2.stride(1) != 1) or (rows > 1 and x2.stride(0) < k):
+        x2 = x2.contiguous()                        # (values apart, or an expanded x whose rows are the same memory)
     with torch.cuda.device(x.device):
         d = fq.FqLinear.from_torch(x2, w, w_scale, y, bias=bias, x_scale=x_scale)
         workspace = torch.empty(fq.fq_linear_workspace_bytes(d), dtype=torch.uint8, device=x.device)

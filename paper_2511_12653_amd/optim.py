@@ -18,6 +18,13 @@ class _Plan:
         self.key, self.params = key, params
         self.workspace = torch.empty(fq.fq_adamw_workspace_bytes(params), dtype=torch.uint8, device=device)
         self.handle = fq.fq_adamw_create(params, self.workspace)
+        self.stream = torch.cuda.current_stream()
+
+    def used_here(self):
+        """The workspace was allocated on another stream than the current one: it stays until that is done with it, too."""
+        stream = torch.cuda.current_stream()
+        if stream != self.stream:
+            self.workspace.record_stream(stream)
 
     def __del__(self):
         if getattr(self, "handle", None):
@@ -99,12 +106,27 @@ class AdamW(torch.optim.Optimizer):
                 plan = self._plan(index, group)
                 if plan is not None:
                     beta1, beta2 = group["betas"]
+                    plan.used_here()
                     fq.fq_adamw_step(plan.handle, fq.FqAdamW(group["lr"], beta1, beta2, group["eps"], group["step"], group["seed"],
                                                              grad_scale))
         return loss
 
+    def __setstate__(self, state):
+        super().__setstate__(state)
+        self._plans = {}                            # (plans belong to the tensors of the optimizer that was copied or pickled)
+
+    def state_dict(self):
+        """Without the copies, which are the program's own and follow from the parameters."""
+        packed = super().state_dict()
+        for group in packed["param_groups"]:
+            group["copies"] = None
+        return packed
+
     def load_state_dict(self, state_dict):
+        copies = [group["copies"] for group in self.param_groups]
         super().load_state_dict(state_dict)
+        for group, own in zip(self.param_groups, copies):
+            group["copies"] = own
         # The base class turns the states into the parameters' type.  They are codes, scales and floats: put back as saved.
         saved = [i for g in state_dict["param_groups"] for i in g["params"]]
         own = [p for g in self.param_groups for p in g["params"]]

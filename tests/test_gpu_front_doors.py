@@ -47,6 +47,14 @@ def test_linear_int8_shapes_and_strides(lead):
         assert linear_int8(codes, wd, wsd, x_scale=H.dev(s[:1]), out_dtype=torch.float32).dtype == torch.float32
 
 
+@pytest.mark.parametrize("rows", [3, 40])
+def test_linear_int8_of_an_expanded_tensor(rows):
+    _, w, ws, b = operands(48, 96, 4)
+    x = torch.randn(1, 96, device="cuda")
+    got = linear_int8(x.expand(rows, 96), H.dev(w), H.dev(ws), H.dev(b))
+    assert torch.equal(got, linear_int8(x, H.dev(w), H.dev(ws), H.dev(b)).expand(rows, 48))
+
+
 def test_linear_int8_refuses():
     _, w, ws, b = operands(8, 16, 2)
     x, wd, wsd, bd = torch.randn(4, 16, device="cuda"), H.dev(w), H.dev(ws), H.dev(b)
@@ -135,6 +143,52 @@ def test_adamw_steps_groups_and_restarts(states):
     for p, v in zip((a, b, c), ends):
         assert torch.equal(p, v)
     torch.optim.lr_scheduler.StepLR(again, 1)
+
+
+@pytest.mark.parametrize("states", ["float32", "float8"])
+def test_adamw_copies_stay_the_programs_own(states):
+    """A state that is loaded brings no copies with it and takes none away; an optimizer that was copied steps on its own."""
+    import copy as copying
+    torch.manual_seed(5)
+    p = torch.nn.Parameter(torch.randn(700, device="cuda"))
+    half = torch.zeros(700, device="cuda", dtype=torch.float16)
+    opt = AdamW([{"params": [p], "copies": [half]}], lr=1e-2, states=states)
+    p.grad = torch.randn(700, device="cuda")
+    opt.step()
+    saved = copying.deepcopy(opt.state_dict())
+    assert all(g["copies"] is None for g in saved["param_groups"])
+    opt.load_state_dict(saved)
+    opt.step()
+    assert torch.equal(half, p.detach().half())
+    twin_p, twin = copying.deepcopy((p, opt))
+    twin_p = twin.param_groups[0]["params"][0]
+    twin_p.grad = p.grad.clone()
+    opt.step()
+    twin.step()
+    assert torch.equal(twin_p, p) and torch.equal(twin.param_groups[0]["copies"][0], half)
+
+
+def test_adamw_on_another_stream():
+    """A plan that one stream made serves steps on another, and its memory is not given away while they run."""
+    torch.manual_seed(6)
+    start = torch.randn(1 << 20, device="cuda")
+    grad = torch.randn(1 << 20, device="cuda")
+    ends = []
+    for streams in ((None, None, None), (None, torch.cuda.Stream(), torch.cuda.Stream())):
+        p = torch.nn.Parameter(start.clone())
+        opt = AdamW([p], lr=1e-2)
+        p.grad = grad.clone()
+        before = torch.cuda.current_stream()
+        for stream in streams:
+            stream = stream or torch.cuda.current_stream()
+            stream.wait_stream(before)
+            with torch.cuda.stream(stream):
+                opt.step()
+            before = stream
+        opt._plans.clear()
+        torch.cuda.current_stream().wait_stream(before)
+        ends.append(p.detach().clone())
+    assert torch.equal(ends[0], ends[1])
 
 
 def test_adamw_refuses():
