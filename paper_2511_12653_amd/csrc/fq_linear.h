@@ -49,7 +49,8 @@ struct AlignArgs {
 };
 
 bool linear_few(const LinearArgs &a, int size);   // whether x with elements of so many bytes may be given as raw (or as x)
-bool linear_rows(const LinearArgs &a);            // whether x may be given as raw for its short rows (w has to fit)
+bool linear_rows(const LinearArgs &a);            // whether x may be given as raw for its short rows
+bool linear_rows_as_they_lie(const LinearArgs &a);     // whether w then is best read so; else its rows are laid out anew first
 // (`other`: rows of codes to lay out anew by the same launch; none if it has no rows)
 int launch_quantize_rows(const QuantizeArgs &a, const AlignArgs &other, void *stream);
 int launch_align_rows(const AlignArgs &a, const AlignArgs &other, void *stream);

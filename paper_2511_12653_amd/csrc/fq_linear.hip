@@ -706,12 +706,30 @@ template <typename X> int launch_few(const LinearArgs &a, void *stream)
 }
 
 // ---------------------------------------------------------------------------------------------
-// Short rows, many tokens: x is read once and its codes never leave the compute unit (288000 x 128 x 128 FP16 49.4 us, 3.0 TB/s of x and
-// y; codes by a launch of their own and tiles 69.5).  A block has TOK * 16 tokens.  It turns
+// Short rows, many tokens: x is read once and its codes never leave the compute unit (288000 x 128 x 128 FP16 50.0 us, 2.9 TB/s of x and
+// y; codes by a launch of their own and tiles 58.5).  A block has TOK * 16 tokens.  It turns
 // them into codes in LDS, a row to 16 lanes, V vectors each, with all of a wavefront's rows requested before the first is
 // looked at; then every wavefront multiplies all of them by 16 * CH channels at a time.  w, small enough to stay in the L2s,
 // goes from there into registers, whole rows of it: the first before x is quantized, the next as the last are used up.
-constexpr int kRowsWaves = 8, kRowsMostK = 512;
+//
+// w may lie at any address: where k is no multiple of 16, its last codes are fetched as those of the 16 that end with the row, and the
+// codes of x are laid out for that (end_behind).  With many channels and few tokens, blockIdx.y shares the channels out: x, small then,
+// is quantized once for each.
+constexpr int kRowsWaves = 8, kRowsLeastK = 16, kRowsMostK = 512;
+
+// Codes l to l + 7 of a row of k, no multiple of 16, in lanes of which an even and the odd one behind it have 16; of the row's last k % 16 codes the
+// 16 end with them instead of beginning with them, zeros in front.
+__device__ __forceinline__ u32x2 end_behind(u32x2 c, int l, int k)
+{
+    const auto swap = [](unsigned v) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, false); };
+    const u32x2 o = u32x2{swap(c[0]), swap(c[1])};
+    const uint64_t own = __builtin_bit_cast(uint64_t, c), other = __builtin_bit_cast(uint64_t, o);
+    const uint64_t first = l & 8 ? other : own, second = l & 8 ? own : other;
+    const int by = 128 - k % 16 * 8;                            // bits, 8 to 120
+    const uint64_t low = by < 64 ? first << by : 0;
+    const uint64_t high = by < 64 ? second << by | first >> (64 - by) : first << (by - 64);
+    return (l & ~15) == (k & ~15) ? __builtin_bit_cast(u32x2, l & 8 ? high : low) : c;
+}
 
 template <typename X, int TOK, int CH, int V>
 __global__ __launch_bounds__(kRowsWaves * 64) void linear_rows_kernel(LinearArgs a)
@@ -737,13 +755,14 @@ __global__ __launch_bounds__(kRowsWaves * 64) void linear_rows_kernel(LinearArgs
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int8_t *row = a.w + (long long)min((tile * CH + c) * 16 + lane % 16, a.n - 1) * a.ldw;
-            cw[step][c] = ld_global((const i32x4 *)(row + min(step * 64 + lane / 16 * 16, a.kw - 16)));      // (behind k the codes of x are 0)
+            __builtin_memcpy(&cw[step][c], (const FQ_GLOBAL int8_t *)(row + min(step * 64 + lane / 16 * 16, a.k - 16)), 16);      // (behind k the codes of x are 0)
         }
     };
-    if (wave < tiles)
+    const int first = (int)blockIdx.y * WAVES + wave, stride = (int)gridDim.y * WAVES;
+    if (first < tiles)
 #pragma unroll
         for (int j = 0; j < kSteps; ++j)
-            if (j < steps) load_w(wave, j);
+            if (j < steps) load_w(first, j);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int r = 0; r < kPasses; ++r) {
@@ -752,16 +771,22 @@ __global__ __launch_bounds__(kRowsWaves * 64) void linear_rows_kernel(LinearArgs
         for (int j = 0; j < V; ++j) odd_end(raw[r][j], row_of_x(r), (j * 16 + lane % 16) * 8, a.k);
         const RowScale scale = row_scale(max16(most_of(raw[r])));
         if (lane % 16 == 0) scales[row_of(r)] = scale.s;
+        u32x2 c[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) c[j] = codes8(raw[r][j], scale, (j * 16 + lane % 16) * 8 >= a.k);
+        if (a.k % 16 != 0)
+#pragma unroll
+            for (int j = 0; j < V; ++j) c[j] = end_behind(c[j], (j * 16 + lane % 16) * 8, a.k);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const int l = (j * 16 + lane % 16) * 8;
-            if (l < steps * 64) *(u32x2 *)(codes + row_of(r) * pitch + l) = codes8(raw[r][j], scale, l >= a.k);
+            if (l < steps * 64) *(u32x2 *)(codes + row_of(r) * pitch + l) = c[j];
         }
     }
     __syncthreads();
 
     const int8_t *x = codes + lane % 16 * pitch + lane / 16 * 16;
-    for (int tile = wave; tile < tiles; tile += WAVES) {
+    for (int tile = first; tile < tiles; tile += stride) {
         i32x4 sum[CH][TOK];
 #pragma unroll
         for (int c = 0; c < CH; ++c)
@@ -776,7 +801,7 @@ __global__ __launch_bounds__(kRowsWaves * 64) void linear_rows_kernel(LinearArgs
 #pragma unroll
                 for (int c = 0; c < CH; ++c) sum[c][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(cw[j][c], cx, sum[c][t], 0, 0, 0);
             }
-            if (tile + WAVES < tiles) load_w(tile + WAVES, j);
+            if (tile + stride < tiles) load_w(tile + stride, j);
         }
         const int n = tile * CH * 16 + lane / 16 * 4;
         float ws[CH][4], bias[CH][4];
@@ -820,9 +845,11 @@ __global__ __launch_bounds__(kRowsWaves * 64) void linear_rows_kernel(LinearArgs
 template <typename X, int TOK, int CH> int launch_rows_of(const LinearArgs &a, void *stream)
 {
     const unsigned blocks = (unsigned)(((long long)a.m + TOK * 16 - 1) / (TOK * 16));
-    if (a.k <= 256) linear_rows_kernel<X, TOK, CH, 2><<<blocks, kRowsWaves * 64, 0, (hipStream_t)stream>>>(a);
-    else if (a.k <= 384) linear_rows_kernel<X, TOK, CH, 3><<<blocks, kRowsWaves * 64, 0, (hipStream_t)stream>>>(a);
-    else linear_rows_kernel<X, TOK, CH, 4><<<blocks, kRowsWaves * 64, 0, (hipStream_t)stream>>>(a);
+    const unsigned passes = (unsigned)(((long long)a.n + kRowsWaves * 16 * CH - 1) / (kRowsWaves * 16 * CH));
+    const dim3 grid(blocks, blocks < kComputeUnits ? min(passes, kComputeUnits / blocks) : 1);
+    if (a.k <= 256) linear_rows_kernel<X, TOK, CH, 2><<<grid, kRowsWaves * 64, 0, (hipStream_t)stream>>>(a);
+    else if (a.k <= 384) linear_rows_kernel<X, TOK, CH, 3><<<grid, kRowsWaves * 64, 0, (hipStream_t)stream>>>(a);
+    else linear_rows_kernel<X, TOK, CH, 4><<<grid, kRowsWaves * 64, 0, (hipStream_t)stream>>>(a);
     return (int)hipGetLastError();
 }
 
@@ -918,17 +945,28 @@ bool linear_few(const LinearArgs &a, int size)
     return lds <= kFewLds && (!a.w_fits || a.n <= (lds <= kFewLdsOfTwo ? 2 : 1) * kFewMostN);
 }
 
-// Few channels, or the product of 16 tokens takes longer than a trip of their codes to memory.  us, codes by a kernel of their
-// own and tiles / this: 19200 x 128 x 384 14.8 / 11.0, 288000 x 128 x 128 69.5 / 49.4, 2048 x 256 x 256 7.4 / 6.3, 1024 x 128 x 128
-// 7.4 / 4.6; 5000 x 384 x 384 9.4 / 10.1, 1024 x 512 x 512 7.8 / 13.3.
+// Work that a launch and a trip of the codes to memory would be much of, and x with few channels.  us, codes by a kernel of their own and
+// tiles / this: 348 x 37 x 16 5.8 / 3.5, 1000 x 1000 x 128 7.3 / 4.5, 100 x 8000 x 320 7.4 / 5.4, 1024 x 512 x 512 7.7 / 6.5; 2048 x 256 x 256 7.1 / 6.1,
+// 19200 x 128 x 384 14.5 / 10.6, 288000 x 128 x 128 58.5 / 50.0; not: 900 x 1100 x 512 FP32 8.5 / 10.9, 12032 x 2277 x 64 26.2 / 30.8, 2000 x 2000 x 384
+// 11.3 / 12.2.
 bool linear_rows(const LinearArgs &a)
 {
-    return a.k >= 16 && a.k <= kRowsMostK && a.m >= 1024 && (long long)a.n * a.k <= (1 << 16);
+    if (a.k < kRowsLeastK || a.k > kRowsMostK) return false;
+    return (a.m >= 1024 && (long long)a.n * a.k <= (1 << 16)) || ((double)a.m * a.n * a.k <= 0x1p28 && linear_rows_as_they_lie(a));
+}
+
+// Loads of 16 bytes that begin between words take twice the time, which is nothing for few.  us, w laid out and tiles (the last:
+// this kernel) / as it lies: 500 x 1000 x 63 7.6 / 5.1, 200 x 1000 x 127 7.4 / 6.4, 400 x 300 x 255 7.5 / 7.5, 200 x 300 x 511 8.5 / 12.7, 900 x 1100
+// x 127 7.9 / 8.3, 100000 x 64 x 255 29.2 / 33.4.
+bool linear_rows_as_they_lie(const LinearArgs &a)
+{
+    return ((uintptr_t)a.w | (uintptr_t)a.ldw) % 4 == 0 || (a.k <= 256 && (double)a.m * a.n * a.k <= 0x1p26);
 }
 
 template <typename X, int TOK> static int launch_rows_by(const LinearArgs &a, void *stream)
 {
-    return a.n <= 16 * kRowsWaves ? launch_rows_of<X, TOK, 1>(a, stream) : launch_rows_of<X, TOK, 2>(a, stream);
+    const long long pairs = ((long long)a.m + TOK * 16 - 1) / (TOK * 16) * (((long long)a.n + 32 * kRowsWaves - 1) / (32 * kRowsWaves));
+    return a.n <= 16 * kRowsWaves || pairs < kComputeUnits ? launch_rows_of<X, TOK, 1>(a, stream) : launch_rows_of<X, TOK, 2>(a, stream);
 }
 
 // 32 tokens to a block while they are that few that longer blocks leave compute units without one, else 80.

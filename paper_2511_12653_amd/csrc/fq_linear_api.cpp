@@ -110,13 +110,14 @@ fq_status run(const fq_linear &d, void *workspace, void *stream)
     int8_t *const codes = (int8_t *)workspace;
     AlignArgs w;
     std::memset(&w, 0, sizeof w);
-    if (!w_fits && a.k > 0 && !linear_few(a, 1)) {
+    const bool rows = quantize && linear_rows(a);
+    if (!w_fits && a.k > 0 && !(rows ? linear_rows_as_they_lie(a) : linear_few(a, 1))) {
         w = {a.w, codes + at.w, d.n, d.ldw, at.pitch, a.k};
         a.w = w.to;
         a.ldw = at.pitch;
         a.kw = (int)at.pitch;
     }
-    if (quantize && linear_rows(a)) {
+    if (rows) {
         a.raw = d.x;
         if (w.rows && launch_align_rows(w, {}, stream) != 0) return FQ_ERR_LAUNCH;
     } else if (quantize) {

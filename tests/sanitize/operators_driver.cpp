@@ -57,6 +57,7 @@ int launch_adamw(const AdamwTensor *t, const unsigned *first, int n, const Adamw
 
 bool linear_few(const LinearArgs &a, int size) { return a.k > 0 && a.m <= 16 && (long long)a.m * a.k * size < 40000; }
 bool linear_rows(const LinearArgs &a) { return a.k >= 16 && a.k <= 512 && a.m >= 1024; }
+bool linear_rows_as_they_lie(const LinearArgs &a) { return ((uintptr_t)a.w | (uintptr_t)a.ldw) % 4 == 0; }
 
 static void check_aligned(const AlignArgs &a)
 {
@@ -91,7 +92,8 @@ int launch_linear(const LinearArgs &a, void *)
     CHECK(a.m > 0 && a.n > 0 && a.y && (a.raw || a.k == 0 || a.x) && (a.raw || a.xs));
     if (a.raw && linear_few(a, a.x16 ? 2 : 4)) return 0;
     if (!a.raw && linear_few(a, 1)) return 0;
-    // the tiles (and the rows' kernel, of w) read whole 16 bytes of rows on 16-byte boundaries
+    if (a.raw && linear_rows(a) && linear_rows_as_they_lie(a)) return 0;       // reads inside the rows of w
+    // the tiles read whole 16 bytes of rows on 16-byte boundaries
     if (a.k > 0) CHECK((uintptr_t)a.w % 16 == 0 && a.ldw % 16 == 0 && a.kw % 16 == 0 && a.kw >= a.k && a.kw <= a.ldw && a.ldw <= kMostPitch);
     if (a.k > 0 && !a.raw) CHECK((uintptr_t)a.x % 16 == 0 && a.ldx % 16 == 0 && a.kx % 16 == 0 && a.kx >= a.k && a.kx <= a.ldx && a.ldx <= kMostPitch);
     return 0;

@@ -117,6 +117,21 @@ def test_pitches_and_alignments(m, n, k, x_pitch, w_pitch, y_pitch, fronts, x_ki
         y_pitch=add(y_pitch, max(0, n - 200)), fronts=fronts)
 
 
+@pytest.mark.parametrize("m,n", [(17, 3), (33, 300), (100, 1100), (260, 129)])
+@pytest.mark.parametrize("k", [16, 17, 24, 31, 33, 63, 64, 127, 136, 200, 256, 257, 300, 384, 399, 500, 511, 512, 513])
+@pytest.mark.parametrize("x_kind", ["f16", "f32"])
+def test_short_rows_of_any_length(m, n, k, x_kind):
+    """Short rows of x against rows of w that begin anywhere: on 16 bytes, on words, between them."""
+    for front, more in ((0, 0), (4, 4), (7, 3)):
+        run(m, n, k, x_kind, "f16", seed=k + front, w_pitch=k + more, x_pitch=k + more % 4, fronts=(front % 4, front, 0))
+
+
+@pytest.mark.parametrize("m,n,k", [(1500, 40, 250), (1030, 200, 300), (1025, 513, 127), (3000, 30, 511), (8200, 200, 77), (1024, 1100, 203)])
+@pytest.mark.parametrize("front", [0, 5])
+def test_short_rows_of_many_tokens(m, n, k, front):
+    run(m, n, k, "f16", "f32", seed=k + front, w_pitch=k + 4 * front, fronts=(0, front, front))
+
+
 def test_rows_of_y_in_the_gaps_of_x():
     """x and y as columns of one buffer."""
     rng = np.random.Generator(np.random.Philox(5))
