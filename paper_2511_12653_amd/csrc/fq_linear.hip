@@ -202,7 +202,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs a, unsi
 }
 
 // ---------------------------------------------------------------------------------------------
-// Product of a tile of BM tokens by BN channels.  What bounds it, by tile: 256 x 256 the matrix cores, which are busy 65 % of the
+// Product of a tile of BM tokens by BN channels.  What bounds it, by tile: 256 x 256 the matrix cores, which are busy 63 % of the
 // cycles at a clock that their power holds down (8192 x 8192 x 8192 460 us, 2.39 POP/s; codes that are all zero are 12 to 25 % faster);
 // the smaller ones, taken where large ones leave compute units without work, what a compute unit can load, 40 to 50 bytes a cycle (17
 // x 64 x 4096, a block or two in all: 16 KiB of a 64 x 64 step in 0.15 us, 32 KiB of a 128 x 128 step in 0.37).  More stages, and codes
