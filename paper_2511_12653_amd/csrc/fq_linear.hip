@@ -3,7 +3,7 @@
 //   y_ij = (sum_k q_ik w_jk) * (xs_i * ws_j) + bias_j          the sum exact in 32 bits, the rest in binary32
 //   xs_i = max_k |x_ik| / 127,  q_ik = round(x_ik / xs_i)      where x comes in FP16 or FP32
 //
-// Up to 16 tokens: linear_few_kernel does all of it in one launch, bound by the stream of w.  Short rows and few channels:
+// Few tokens: linear_few_kernel, which with up to 16 and room for them in LDS does all of it in one launch, bound by the stream of w.  Short rows and few channels:
 // linear_rows_kernel, one launch, bound by x and y.  All else: quantize_rows_kernel, bound by memory, and linear_tile_kernel, bound
 // by the matrix cores or, in few tiles, by what a compute unit can load.  Quantizing inside the tiles would do it again for every tile
 // of channels: n / 256 times.  Sizes below are m x n x k, tokens by channels by values of a row.
@@ -504,8 +504,8 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
 }
 
 // ---------------------------------------------------------------------------------------------
-// Up to 16 tokens: what counts is to stream w once (1 x 4096 x 4096 FP16 5.4 us a call, 16.8 MB of w, of which the launch
-// of an empty kernel is 1.7).  A block multiplies 16 channels by all tokens (lanes past the last
+// Few tokens: what counts is to stream w once (1 x 4096 x 4096 FP16 5.4 us a call, 16.8 MB of w, of which the launch
+// of an empty kernel is 1.7).  A block multiplies 16 channels by all tokens, up to 16 (lanes past the last
 // repeat it); its wavefronts share the codes of a row, a run of whole steps of 128 each, and their sums meet in LDS.  Every
 // wavefront has kRing steps of w of its own in LDS or on their way there, so it waits for nobody; the layout is that of the
 // tiles above.  x lies in LDS as a whole: fetched in front of w, and with X FP16 or FP32 turned into codes by the block while
@@ -513,7 +513,14 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
 // Rows that do not begin on 16-byte boundaries (SHIFTED: of w or x) are fetched from the boundary in front of them on.  A step then
 // is 112 codes, and the 16 of a lane are cut out of two neighbouring 16 bytes; the last quarter of the second product has
 // zeros for x.
+// Codes of x that leave no room in LDS, and those of more tokens (RINGED: 16, or 32 to a block and more along blockIdx.y), come
+// through the rings, too, step by step beside those of w.
 constexpr int kFewWaves = 8, kRing = 4;
+
+// What the rings hold: 16 rows of w, and with x in them 16 or 32 of x; three steps of the latter.
+constexpr int few_slot(int of_x) { return (16 + of_x) * kDepth; }
+constexpr int few_ring(int of_x) { return of_x > 16 ? kRing - 1 : kRing; }
+constexpr int few_ringed(int of_x) { return kFewWaves * few_ring(of_x) * few_slot(of_x); }
 
 struct FewLds {                                                 // where things lie, in bytes behind the rings
     int use, steps, pieces, raw_pitch, raw, code_pitch, codes, total;
@@ -561,34 +568,36 @@ __device__ __forceinline__ i32x4 cut16(i32x4 low, i32x4 high, int o)
     return r;
 }
 
-template <typename X, bool SHIFTED>
+template <typename X, bool SHIFTED, int RINGED = 0>
 __global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs a)
 {
-    constexpr int WAVES = kFewWaves, kPitch = 17;                // (of 16 channels' sums in LDS)
+    static_assert(!RINGED || sizeof(X) == 1, "values to quantize lie in LDS");
+    constexpr int WAVES = kFewWaves, kPitch = 17, kGroups = RINGED > 16 ? 2 : 1;      // (pitch of 16 channels' sums in LDS; 16 tokens each)
     constexpr bool kQuantize = sizeof(X) > 1;
-    constexpr int kUse = SHIFTED ? kDepth - 16 : kDepth;
+    constexpr int kUse = SHIFTED ? kDepth - 16 : kDepth, kDeep = few_ring(RINGED), kSlot = few_slot(RINGED), kLoads = kSlot / 1024;
     extern __shared__ __attribute__((aligned(1024))) int8_t lds[];
-    __shared__ int sums[16 * kPitch];
+    __shared__ int sums[kGroups * 16 * kPitch];
     __shared__ unsigned top[16];
     __shared__ float scales[16];
-    const FewLds at = few_lds(a.m, a.k, sizeof(X), SHIFTED);
+    const FewLds at = few_lds(RINGED ? 0 : a.m, a.k, sizeof(X), SHIFTED);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n0 = (int)blockIdx.x * 16;
+    const int m0 = RINGED ? (int)blockIdx.y * RINGED : 0;
     // this thread's output: asked for first, used last
-    const int out_m = threadIdx.x / 16, out_n = n0 + (int)threadIdx.x % 16;
-    const bool writes = out_m < a.m && out_n < a.n;
+    const int out_m = m0 + (int)threadIdx.x / 16, out_n = n0 + (int)threadIdx.x % 16;
+    const bool writes = out_m < a.m && out_n < a.n && (!RINGED || (int)threadIdx.x < RINGED * 16);
     float ws = 0.0f, bias = 0.0f, xs = 0.0f;
     if (writes) {
         ws = ld_global(a.ws + (long long)out_n * a.ws_step);
         if (a.bias) bias = ld_global(a.bias + out_n);
         if (!kQuantize) xs = ld_global(a.xs + (long long)out_m * a.xs_step);
     }
-    if (threadIdx.x < 16 * kPitch) sums[threadIdx.x] = 0;
+    for (int i = threadIdx.x; i < kGroups * 16 * kPitch; i += WAVES * 64) sums[i] = 0;
     if (threadIdx.x < 16) top[threadIdx.x] = 0;
 
     // x: 1 KiB of a row to a load, zeros behind the 16 bytes with its end
     auto row_of_x = [&](int row) { return (uint64_t)(kQuantize ? (const int8_t *)a.raw : a.x) + (uint64_t)row * (uint64_t)a.ldx * sizeof(X); };
-    for (int i = wave; i < a.m * at.pieces; i += WAVES) {
+    for (int i = wave; !RINGED && i < a.m * at.pieces; i += WAVES) {
         const int row = i / at.pieces, from = i % at.pieces * 1024;
         const uint64_t begins = row_of_x(row), p = (begins & ~15ull) + from;
         const int bytes = max(0, ((int)(begins & 15) + a.k * (int)sizeof(X) + 15) / 16 * 16 - from);
@@ -598,29 +607,37 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs a
     // w
     const int each = (at.steps + WAVES - 1) / WAVES;
     const int begin = min(at.steps, wave * each), end = min(at.steps, begin + each);
-    int8_t *const ring = lds + wave * (kRing * 16 * kDepth);
+    int8_t *const ring = lds + wave * (kDeep * kSlot);
     const int8_t *const w0 = a.w + (long long)n0 * a.ldw;
     const int shift0 = SHIFTED ? (int)((uint64_t)w0 & 15) : 0;
     const Panel pw = {w0 - shift0, ((unsigned)(min(16, a.n - n0) - 1) * (unsigned)a.ldw + (unsigned)(shift0 + a.k) + 15) / 16 * 16};
     Staging<2, 1> w;
     w.place(a.ldw, lane, 0, (unsigned)shift0);
+    const Panel px = panel(a.x, a.ldx, m0, kGroups * 16, a.m - m0, a.kx);
+    Staging<2 * kGroups, 1> rows;
+    if (RINGED) rows.place(a.ldx, lane, 0);
     auto ask = [&](int step) {
         if (step >= end) return;
-        int8_t *to = ring + (step - begin) % kRing * (16 * kDepth);
+        int8_t *to = ring + (step - begin) % kDeep * kSlot;
         w.fetch(pw, step * kUse, 0, to, 0, false);
         w.fetch(pw, step * kUse, 1, to, 0, false);
+        if (RINGED) {
+#pragma unroll
+            for (int j = 0; j < 2 * kGroups; ++j)
+                rows.fetch(px, step * kUse, j, to + 16 * kDepth, 0, step * kUse + place_of(lane % 8, j * 8 + lane / 8) * 16 >= a.kx);
+        }
     };
 #pragma unroll
-    for (int j = 0; j < kRing; ++j) ask(begin + j);
+    for (int j = 0; j < kDeep; ++j) ask(begin + j);
     // what is left on its way when x has come: the steps of w
     auto arrived = [&](int steps_left) {
-        if (steps_left >= 4) loads_but<8>();
-        else if (steps_left == 3) loads_but<6>();
-        else if (steps_left == 2) loads_but<4>();
-        else if (steps_left == 1) loads_but<2>();
+        if (steps_left >= 4) loads_but<4 * kLoads>();
+        else if (steps_left == 3) loads_but<3 * kLoads>();
+        else if (steps_left == 2) loads_but<2 * kLoads>();
+        else if (steps_left == 1) loads_but<kLoads>();
         else loads_but<0>();
     };
-    arrived(min(kRing, end - begin));
+    arrived(min(kDeep, end - begin));
     lds_barrier();
 
     if constexpr (kQuantize) {
@@ -661,33 +678,38 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs a
 
     const int8_t *x = lds + at.codes + min(lane % 16, a.m - 1) * at.code_pitch + lane / 16 * 16;
     const int shift = SHIFTED ? (int)((uint64_t)(w0 + (long long)(lane % 16) * a.ldw) & 15) : 0;
-    i32x4 sum = (i32x4)0;
+    i32x4 sum[kGroups];
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) sum[g] = (i32x4)0;
     for (int step = begin; step < end; ++step) {
-        arrived(min(kRing - 1, end - 1 - step));
-        const int8_t *from = ring + (step - begin) % kRing * (16 * kDepth) + lane % 16 * kDepth;
+        arrived(min(kDeep - 1, end - 1 - step));
+        const int8_t *from = ring + (step - begin) % kDeep * kSlot + lane % 16 * kDepth;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const int c = 4 * s + lane / 16;
             i32x4 cw = *(const i32x4 *)(from + place_of(c, lane % 16) * 16);
-            i32x4 cx = *(const i32x4 *)(x + step * kUse + 64 * s);
-            if (SHIFTED) {
-                cw = cut16(cw, *(const i32x4 *)(from + place_of((c + 1) & 7, lane % 16) * 16), shift);
-                if (c == 7) cx = (i32x4)0;
+            if (SHIFTED) cw = cut16(cw, *(const i32x4 *)(from + place_of((c + 1) & 7, lane % 16) * 16), shift);
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                i32x4 cx = *(const i32x4 *)(RINGED ? from + (g + 1) * 16 * kDepth + place_of(c, lane % 16) * 16 : x + step * kUse + 64 * s);
+                if (SHIFTED && c == 7) cx = (i32x4)0;
+                sum[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(cw, cx, sum[g], 0, 0, 0);
             }
-            sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(cw, cx, sum, 0, 0, 0);
         }
-        if (step + kRing < end) {
+        if (step + kDeep < end) {
             loads_but<63>();                                    // (the reads of this step are done)
-            ask(step + kRing);
+            ask(step + kDeep);
         }
     }
     // lane l has channels 4 (l / 16) to 4 (l / 16) + 3 of token l % 16
 #pragma unroll
-    for (int e = 0; e < 4; ++e) atomicAdd(sums + lane % 16 * kPitch + lane / 16 * 4 + e, sum[e]);
+    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) atomicAdd(sums + (g * 16 + lane % 16) * kPitch + lane / 16 * 4 + e, sum[g][e]);
     __syncthreads();
     if (!writes) return;
     if (kQuantize) xs = scales[out_m];
-    float y = (float)sums[out_m * kPitch + threadIdx.x % 16] * (xs * ws);
+    float y = (float)sums[threadIdx.x / 16 * kPitch + threadIdx.x % 16] * (xs * ws);
     if (a.bias) y += bias;
     if (a.y16) st_global((_Float16 *)a.y + (long long)out_m * a.ldy + out_n, (_Float16)y);
     else st_global((float *)a.y + (long long)out_m * a.ldy + out_n, y);
@@ -696,9 +718,25 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs a
 // Whether all rows of x and w begin on 16-byte boundaries and consist of whole 16 values.
 bool few_fits(const LinearArgs &a) { return a.w_fits && (!a.raw || a.x_vec); }
 
+// LDS of a block with x as a whole there, at any alignment; more than there is for more than 16 tokens.
+long long few_most(const LinearArgs &a, int size)
+{
+    return a.m > 16 || (long long)a.m * a.k * size > kFewLds ? kFewLds + 1 : few_lds(a.m, a.k, size, true).total;
+}
+
+template <int RINGED> int launch_ringed(const LinearArgs &a, unsigned blocks, void *stream)
+{
+    const dim3 grid(blocks, ((unsigned)a.m + RINGED - 1) / RINGED);
+    if (a.w_fits) linear_few_kernel<int8_t, false, RINGED><<<grid, kFewWaves * 64, few_ringed(RINGED), (hipStream_t)stream>>>(a);
+    else linear_few_kernel<int8_t, true, RINGED><<<grid, kFewWaves * 64, few_ringed(RINGED), (hipStream_t)stream>>>(a);
+    return (int)hipGetLastError();
+}
+
 template <typename X> int launch_few(const LinearArgs &a, void *stream)
 {
     const unsigned blocks = ((unsigned)a.n + 15) / 16;
+    if constexpr (sizeof(X) == 1)
+        if (few_most(a, 1) > kFewLds) return a.m <= 16 ? launch_ringed<16>(a, blocks, stream) : launch_ringed<32>(a, blocks, stream);
     const size_t lds = (size_t)few_lds(a.m, a.k, sizeof(X), !few_fits(a)).total;
     if (few_fits(a)) linear_few_kernel<X, false><<<blocks, kFewWaves * 64, lds, (hipStream_t)stream>>>(a);
     else linear_few_kernel<X, true><<<blocks, kFewWaves * 64, lds, (hipStream_t)stream>>>(a);
@@ -934,15 +972,18 @@ static double tile_time(const LinearArgs &a, const Tile &t)
     return time;
 }
 
-// Whether the kernel of few tokens takes x of this element size: it fits into LDS beside the rings, and all blocks are on the chip at
-// once, or w does not fit the tiles.  us, this / quantizing and tiles: 1 x 4096 x 4096 FP16 5.4 / 10.7, 16 x 4096 x 4096 8.9 / 11.0, 4 x 4096 x 8192
-// 10.5 / 16.2; two blocks to a compute unit: 1 x 8192 x 4096 8.4 / 11.0, 1 x 8192 x 64 4.6 / 7.6, codes 3 x 8192 x 2048 4.8 / 6.2; not at
-// once: 4 x 8192 x 4096 15.1 / 11.2, codes 16 x 16384 x 4096 20.7 / 12.4.
+// Whether the kernel of few tokens takes x of this element size: values fit into LDS beside the rings (codes need not), and all
+// blocks are on the chip at once, or there are at most 16 tokens and w does not fit the tiles.  us, this / quantizing and tiles: 1 x 4096 x 4096 FP16 5.4 / 10.7, 16 x 4096 x 4096 8.9 / 11.0, 4 x 4096 x 8192
+// 10.5 / 16.2; two blocks to a compute unit: 1 x 8192 x 4096 8.4 / 11.0, 1 x 8192 x 64 4.6 / 7.6, codes 3 x 8192 x 2048 4.8 / 6.2; codes
+// through the rings, x quantized by a launch of its own in both: 16 x 4096 x 14336 15.8 / 25.5, 32 x 4096 x 4096 8.3 / 11.3, 128 x 1024 x 2352
+// 6.9 / 9.7, 1000 x 128 x 4096 11.4 / 13.2, codes 224 x 503 x 6144 5.9 / 11.1, 33 x 16 x 16 4.4 / 4.4; not at once: 4 x 8192 x 4096 15.1 / 11.2, 1201
+// x 257 x 1155 14.0 / 10.2, codes 16 x 16384 x 4096 20.7 / 12.4, 446 x 503 x 6144 10.4 / 11.3.
 bool linear_few(const LinearArgs &a, int size)
 {
-    if (a.k <= 0 || a.m > 16 || a.ldw > kMostPitch || (long long)a.k * size * a.m > kFewLds) return false;
-    const int lds = few_lds(a.m, a.k, size, true).total;
-    return lds <= kFewLds && (!a.w_fits || a.n <= (lds <= kFewLdsOfTwo ? 2 : 1) * kFewMostN);
+    if (a.k <= 0 || a.ldw > kMostPitch) return false;
+    if (a.m > 16) return size == 1 && ((long long)a.m + 31) / 32 * (((long long)a.n + 15) / 16) <= kComputeUnits;
+    const long long lds = few_most(a, size);
+    return (lds <= kFewLds || size == 1) && (!a.w_fits || a.n <= (lds <= kFewLdsOfTwo ? 2 : 1) * kFewMostN);
 }
 
 // Work that a launch and a trip of the codes to memory would be much of, and x with few channels.  us, codes by a kernel of their own and

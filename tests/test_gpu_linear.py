@@ -132,6 +132,21 @@ def test_short_rows_of_many_tokens(m, n, k, front):
     run(m, n, k, "f16", "f32", seed=k + front, w_pitch=k + 4 * front, fronts=(0, front, front))
 
 
+@pytest.mark.parametrize("m", [1, 5, 16, 17, 32, 33, 64, 100])
+@pytest.mark.parametrize("k", [513, 1008, 2001, 9000, 12345, 20000])
+@pytest.mark.parametrize("x_kind", ["f16", "i8"])
+def test_few_tokens_with_long_rows(m, k, x_kind):
+    """Rows of x that leave no room in LDS, and more tokens than a block takes; w on 16 bytes and anywhere."""
+    for front, more in ((0, -k % 16), (6, 3)):
+        run(m, 37, k, x_kind, "f32", seed=k + front, w_pitch=k + more, x_pitch=k + (more if x_kind == "i8" else 0), fronts=(front if x_kind == "i8" else 0, front, 0))
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 20, 131071), (20, 4096, 640), (20, 4090, 639), (257, 464, 520), (8190, 16, 530)])
+@pytest.mark.parametrize("x_kind", ["f32", "i8"])
+def test_the_most_blocks_of_few_tokens(m, n, k, x_kind):
+    run(m, n, k, x_kind, "f16", seed=m + n)
+
+
 def test_rows_of_y_in_the_gaps_of_x():
     """x and y as columns of one buffer."""
     rng = np.random.Generator(np.random.Philox(5))
