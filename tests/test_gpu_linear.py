@@ -92,6 +92,17 @@ def test_sizes(m, n, k, x_kind, y_kind):
     run(m, n, k, x_kind, y_kind, seed=m * 7919 + n * 31 + k)
 
 
+@pytest.mark.parametrize("m,n,k", [(1419, 5415, 130), (3362, 2314, 256), (1671, 4647, 385), (5393, 1416, 513), (1420, 5478, 1155),
+                                   (5002, 772, 130), (712, 5462, 256), (5029, 773, 385), (5488, 708, 513), (706, 5456, 1155),
+                                   (1331, 5397, 130), (1288, 5379, 256), (1281, 5510, 385), (1282, 5498, 1030),
+                                   (514, 5473, 385), (5479, 513, 513), (5455, 517, 650), (580, 4913, 1030),
+                                   (4913, 265, 256), (554, 1259, 385), (1960, 267, 513), (2832, 146, 650),
+                                   (694, 1511, 256), (533, 775, 650), (1931, 135, 1030), (2048, 2304, 1024)])
+def test_tiles_of_every_size(m, n, k):
+    """One to ten steps of each tile, with ends that fill none."""
+    run(m, n, k, "f16" if (m + k) % 2 else "i8", "f32" if n % 2 else "f16", seed=m)
+
+
 @pytest.mark.parametrize("m", [1, 3, 16])
 @pytest.mark.parametrize("k", [1, 15, 16, 100, 111, 112, 113, 127, 224, 225, 895, 896, 897, 1000, 2047, 4001])
 @pytest.mark.parametrize("x_kind", ["f16", "f32", "i8"])
