@@ -372,7 +372,7 @@ void fq_adamw_destroy(fq_adamw_plan *plan);
  * Rows may lie any distance apart (ldx, ldw, ldy, in elements) and at any address that their type allows.  x and w are read in
  * whole 16 bytes: what lies between two rows, and the rest of the 16 bytes in which the first begins and the last ends, may be
  * read and has no effect.  Fastest where the rows of x (FQ_I8) and w begin on 16-byte boundaries and k is a multiple of 16:
- * others are laid out anew in the workspace first (whose size therefore depends on the pointers), but for w with few tokens or
+ * others are laid out anew in the workspace first (whose size therefore depends on the pointers), but with few tokens or
  * short rows.  One to three launches.  The workspace need not be initialised and may be shared by calls that do not overlap in time.
  */
 typedef struct fq_linear {

@@ -15,7 +15,7 @@ constexpr int kFewLdsOfTwo = 78 << 10;           // most of a block that leaves 
 constexpr int kFewMostN = 16 * 256;              // channels there of a block to a compute unit
 
 struct LinearArgs {
-    const int8_t *x;           // codes, in rows that fit (see w_fits)
+    const int8_t *x;           // codes, in rows that fit (see w_fits) but in the kernel of few tokens
     const void *raw;           // instead of x: values for the kernel of few tokens
     const float *xs;
     const int8_t *w;
@@ -28,6 +28,7 @@ struct LinearArgs {
     int xs_step, ws_step;
     int x16, x_vec;            // of raw, 1: FP16; rows on 16-byte boundaries
     int y16, y_lines;          // 1: y is FP16; its rows begin on 128-byte lines
+    int x_fits;                // 1: so do rows of x, where it is codes
     int w_fits;                // 1: rows of w begin on 16-byte boundaries, k is a multiple of 16, the pitch is at most kMostPitch
 };
 

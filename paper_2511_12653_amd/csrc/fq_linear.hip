@@ -514,7 +514,8 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
 // is 112 codes, and the 16 of a lane are cut out of two neighbouring 16 bytes; the last quarter of the second product has
 // zeros for x.
 // Codes of x that leave no room in LDS, and those of more tokens (RINGED: 16, or 32 to a block and more along blockIdx.y), come
-// through the rings, too, step by step beside those of w.
+// through the rings, too, step by step beside those of w, and may lie at any address like those (16 x 1000 x 1155 codes 4.3 us, laid
+// out anew first 7.5).
 constexpr int kFewWaves = 8, kRing = 4;
 
 // What the rings hold: 16 rows of w, and with x in them 16 or 32 of x; three steps of the latter.
@@ -568,6 +569,17 @@ __device__ __forceinline__ i32x4 cut16(i32x4 low, i32x4 high, int o)
     return r;
 }
 
+// The first n bytes of 16, zeros behind them.
+__device__ __forceinline__ i32x4 first16(i32x4 v, int n)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int bits = min(max(n - 4 * j, 0), 4) * 8;
+        v[j] &= (int)(unsigned)((1ull << bits) - 1);
+    }
+    return v;
+}
+
 template <typename X, bool SHIFTED, int RINGED = 0>
 __global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs a)
 {
@@ -613,9 +625,11 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs a
     const Panel pw = {w0 - shift0, ((unsigned)(min(16, a.n - n0) - 1) * (unsigned)a.ldw + (unsigned)(shift0 + a.k) + 15) / 16 * 16};
     Staging<2, 1> w;
     w.place(a.ldw, lane, 0, (unsigned)shift0);
-    const Panel px = panel(a.x, a.ldx, m0, kGroups * 16, a.m - m0, a.kx);
+    const int8_t *const x0 = a.x + (long long)m0 * a.ldx;
+    const int front = RINGED && SHIFTED ? (int)((uint64_t)x0 & 15) : 0;       // (0 where rows of x fit)
+    const Panel px = {x0 - front, ((unsigned)(min(kGroups * 16, a.m - m0) - 1) * (unsigned)a.ldx + (unsigned)(front + a.kx) + 15) / 16 * 16};
     Staging<2 * kGroups, 1> rows;
-    if (RINGED) rows.place(a.ldx, lane, 0);
+    if (RINGED) rows.place(a.ldx, lane, 0, (unsigned)front);
     auto ask = [&](int step) {
         if (step >= end) return;
         int8_t *to = ring + (step - begin) % kDeep * kSlot;
@@ -624,7 +638,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs a
         if (RINGED) {
 #pragma unroll
             for (int j = 0; j < 2 * kGroups; ++j)
-                rows.fetch(px, step * kUse, j, to + 16 * kDepth, 0, step * kUse + place_of(lane % 8, j * 8 + lane / 8) * 16 >= a.kx);
+                rows.fetch(px, step * kUse, j, to + 16 * kDepth, 0, a.x_fits && step * kUse + place_of(lane % 8, j * 8 + lane / 8) * 16 >= a.kx);
         }
     };
 #pragma unroll
@@ -692,6 +706,11 @@ __global__ __launch_bounds__(kFewWaves * 64) void linear_few_kernel(LinearArgs a
 #pragma unroll
             for (int g = 0; g < kGroups; ++g) {
                 i32x4 cx = *(const i32x4 *)(RINGED ? from + (g + 1) * 16 * kDepth + place_of(c, lane % 16) * 16 : x + step * kUse + 64 * s);
+                if (SHIFTED && RINGED && !a.x_fits) {
+                    const int8_t *more = from + (g + 1) * 16 * kDepth + place_of((c + 1) & 7, lane % 16) * 16;
+                    cx = first16(cut16(cx, *(const i32x4 *)more, (int)((uint64_t)(x0 + (long long)(g * 16 + lane % 16) * a.ldx) & 15)),
+                                 a.k - step * kUse - c * 16);
+                }
                 if (SHIFTED && c == 7) cx = (i32x4)0;
                 sum[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(cw, cx, sum[g], 0, 0, 0);
             }
@@ -727,7 +746,7 @@ long long few_most(const LinearArgs &a, int size)
 template <int RINGED> int launch_ringed(const LinearArgs &a, unsigned blocks, void *stream)
 {
     const dim3 grid(blocks, ((unsigned)a.m + RINGED - 1) / RINGED);
-    if (a.w_fits) linear_few_kernel<int8_t, false, RINGED><<<grid, kFewWaves * 64, few_ringed(RINGED), (hipStream_t)stream>>>(a);
+    if (a.w_fits && a.x_fits) linear_few_kernel<int8_t, false, RINGED><<<grid, kFewWaves * 64, few_ringed(RINGED), (hipStream_t)stream>>>(a);
     else linear_few_kernel<int8_t, true, RINGED><<<grid, kFewWaves * 64, few_ringed(RINGED), (hipStream_t)stream>>>(a);
     return (int)hipGetLastError();
 }
@@ -736,7 +755,7 @@ template <typename X> int launch_few(const LinearArgs &a, void *stream)
 {
     const unsigned blocks = ((unsigned)a.n + 15) / 16;
     if constexpr (sizeof(X) == 1)
-        if (few_most(a, 1) > kFewLds) return a.m <= 16 ? launch_ringed<16>(a, blocks, stream) : launch_ringed<32>(a, blocks, stream);
+        if (few_most(a, 1) > kFewLds || !a.x_fits) return a.m <= 16 ? launch_ringed<16>(a, blocks, stream) : launch_ringed<32>(a, blocks, stream);
     const size_t lds = (size_t)few_lds(a.m, a.k, sizeof(X), !few_fits(a)).total;
     if (few_fits(a)) linear_few_kernel<X, false><<<blocks, kFewWaves * 64, lds, (hipStream_t)stream>>>(a);
     else linear_few_kernel<X, true><<<blocks, kFewWaves * 64, lds, (hipStream_t)stream>>>(a);
@@ -980,7 +999,7 @@ static double tile_time(const LinearArgs &a, const Tile &t)
 // x 257 x 1155 14.0 / 10.2, codes 16 x 16384 x 4096 20.7 / 12.4, 446 x 503 x 6144 10.4 / 11.3.
 bool linear_few(const LinearArgs &a, int size)
 {
-    if (a.k <= 0 || a.ldw > kMostPitch) return false;
+    if (a.k <= 0 || a.ldw > kMostPitch || (size == 1 && !a.x_fits && a.ldx > kMostPitch)) return false;
     if (a.m > 16) return size == 1 && ((long long)a.m + 31) / 32 * (((long long)a.n + 15) / 16) <= kComputeUnits;
     const long long lds = few_most(a, size);
     return (lds <= kFewLds || size == 1) && (!a.w_fits || a.n <= (lds <= kFewLdsOfTwo ? 2 : 1) * kFewMostN);

@@ -100,6 +100,7 @@ fq_status run(const fq_linear &d, void *workspace, void *stream)
     a.bias = d.bias; a.y = d.y; a.ldy = d.ldy; a.y16 = d.y_dtype == FQ_F16;
     a.m = (int)d.m; a.n = (int)d.n; a.k = a.kx = a.kw = (int)d.k;
     a.y_lines = aligned(a.y, 128) && (size_t)a.ldy * size_of(d.y_dtype) % 128 == 0;
+    a.x_fits = x_fits || quantize;                   // (codes in the workspace fit)
     a.w_fits = w_fits;
     a.x16 = d.x_dtype == FQ_F16;
     a.x_vec = aligned(d.x, 16) && (size_t)d.ldx * size_of(d.x_dtype) % 16 == 0;
@@ -128,7 +129,10 @@ fq_status run(const fq_linear &d, void *workspace, void *stream)
         if (launch_quantize_rows(q, w, stream) != 0) return FQ_ERR_LAUNCH;
         a.xs = q.s;
         a.xs_step = 1;
+    } else if (!x_fits && linear_few(a, 1)) {
+        return launch_linear(a, stream) == 0 ? FQ_OK : FQ_ERR_LAUNCH;
     } else if (a.k > 0 && (!x_fits || w.rows)) {
+        a.x_fits = 1;
         const AlignArgs x = {a.x, codes, x_fits ? 0 : d.m, d.ldx, at.pitch, a.k};
         if (launch_align_rows(x, w, stream) != 0) return FQ_ERR_LAUNCH;
     }

@@ -152,6 +152,13 @@ def test_few_tokens_with_long_rows(m, k, x_kind):
         run(m, 37, k, x_kind, "f32", seed=k + front, w_pitch=k + more, x_pitch=k + (more if x_kind == "i8" else 0), fronts=(front if x_kind == "i8" else 0, front, 0))
 
 
+@pytest.mark.parametrize("m", [1, 15, 16, 17, 50])
+@pytest.mark.parametrize("k", [1, 7, 15, 16, 17, 96, 111, 112, 113, 128, 225, 800])
+@pytest.mark.parametrize("x_front,x_more,w_front,w_more", [(1, 1, 0, 0), (5, 3, 5, 3), (0, 13, 9, 0), (16, 0, 3, 2), (15, 16, 0, 16)])
+def test_few_tokens_of_codes_at_any_address(m, k, x_front, x_more, w_front, w_more):
+    run(m, 50, k, "i8", "f16", seed=k + m, x_pitch=k + x_more, w_pitch=k + w_more, fronts=(x_front, w_front, 0))
+
+
 @pytest.mark.parametrize("m,n,k", [(3, 20, 131071), (20, 4096, 640), (20, 4090, 639), (257, 464, 520), (8190, 16, 530)])
 @pytest.mark.parametrize("x_kind", ["f32", "i8"])
 def test_the_most_blocks_of_few_tokens(m, n, k, x_kind):
