@@ -954,7 +954,8 @@ int launch_quantize_rows(const QuantizeArgs &a, const AlignArgs &other, void *st
 }
 
 // The tiles, and what a step of 128 codes of a block takes: at least `wait`, and `work` for each block that a compute unit
-// holds at once (`resident` of them at most); `ends` for what is in front of the first step and behind the last (us).  The tile
+// holds at once (`resident` of them at most); in us.  What is in front of the first step and behind the last takes kEnds and the time of the
+// blocks' parts of y at 5 TB/s (with few steps the most of it: 11707 x 9600 x 272 89 us in 256 x 256, 45 of them for y).  The tile
 // with the least sum is taken.  Measured, codes at aligned rows, us, the tiles in the order of the table (- : not in question):
 //   8192 x 8192 x 8192   461   483   565   582   856   1091
 //   2048 x 4096 x 4096  44.5  34.0  37.0  38.3  55.0   73.9
@@ -963,30 +964,33 @@ int launch_quantize_rows(const QuantizeArgs &a, const AlignArgs &other, void *st
 //   256 x 4096 x 4096      -     -     -  15.7  10.3   12.1
 //   446 x 503 x 6144       -     -     -  22.7  12.3   11.3
 //   20 x 16384 x 4096   40.3  22.2  26.2  15.0  12.8   12.5
+//   12814 x 166 x 1040, FP32 y  23.3  15.6  13.8  11.7  -  14.7
 struct Tile {
     int m, n, resident;
-    double wait, work, ends;
+    double wait, work;
     int (*launch)(const LinearArgs &, void *);
 };
 
+constexpr double kEnds = 1.5, kStoreRate = 5e6;                  // us, bytes a us
+
 static const Tile kTiles[] = {
-    {256, 256, 1, 1.80, 1.80, 2.0, launch_tiles<256, 256, 2, 4, 2>},
-    {256, 128, 1, 0.70, 0.98, 2.0, launch_tiles<256, 128, 4, 2, 3>},
-    {128, 128, 2, 0.80, 0.56, 2.0, launch_tiles<128, 128, 2, 2, 2>},
-    {128, 128, 1, 0.46, 0.56, 2.5, launch_tiles<128, 128, 2, 2, 4>},
-    {64, 64, 2, 0.19, 0.21, 1.0, launch_tiles<64, 64, 2, 2, 4>},
-    {32, 64, 3, 0.19, 0.12, 1.0, launch_tiles<32, 64, 1, 2, 4>},
+    {256, 256, 1, 1.80, 1.80, launch_tiles<256, 256, 2, 4, 2>},
+    {256, 128, 1, 0.70, 0.98, launch_tiles<256, 128, 4, 2, 3>},
+    {128, 128, 2, 0.80, 0.56, launch_tiles<128, 128, 2, 2, 2>},
+    {128, 128, 1, 0.46, 0.56, launch_tiles<128, 128, 2, 2, 4>},
+    {64, 64, 2, 0.19, 0.21, launch_tiles<64, 64, 2, 2, 4>},
+    {32, 64, 3, 0.19, 0.12, launch_tiles<32, 64, 1, 2, 4>},
 };
 
 static double tile_time(const LinearArgs &a, const Tile &t)
 {
     const long long blocks = ((long long)a.m + t.m - 1) / t.m * (((long long)a.n + t.n - 1) / t.n);
     const long long once = (long long)kComputeUnits * t.resident, rounds = blocks / once, left = blocks % once;
-    const double steps = (double)((a.k + kDepth - 1) / kDepth);
-    double time = (double)rounds * (steps * (t.wait > t.resident * t.work ? t.wait : t.resident * t.work) + t.ends);
+    const double steps = (double)((a.k + kDepth - 1) / kDepth), store = (double)t.m * t.n * (a.y16 ? 2 : 4) / kStoreRate;
+    double time = (double)rounds * (steps * (t.wait > t.resident * t.work ? t.wait : t.resident * t.work) + kEnds + (double)once * store);
     if (left) {
         const double each = (double)((left + kComputeUnits - 1) / kComputeUnits) * t.work;
-        time += steps * (t.wait > each ? t.wait : each) + t.ends;
+        time += steps * (t.wait > each ? t.wait : each) + kEnds + (double)left * store;
     }
     return time;
 }
