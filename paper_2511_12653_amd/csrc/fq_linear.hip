@@ -273,7 +273,8 @@ __device__ __forceinline__ void lanes_in_step()
 
 // N neighbouring channels of a token, `left` of which there are (WHOLE: all).  Vector stores take any address.  LINES: the
 // lanes of this one instruction write whole lines, which then need not wait in the caches for the rest of them: 19200 x 384 x 384
-// of codes 10.2 -> 8.7 us, 8192 x 8192 x 8192 479 -> 470; for parts of lines it is the other way, 20000 x 1000 x 64 FP32 28.7 -> 48.9.
+// of codes 10.2 -> 8.7 us, 8192 x 8192 x 8192 479 -> 470, 12000 x 2048 x 600 FP32 44.8 -> 40.9; for parts of lines it is the other way, 20000 x
+// 1000 x 64 FP32 28.7 -> 48.9.
 template <bool HALF, bool WHOLE, bool LINES, int N> __device__ __forceinline__ void store_channels(char *at, const float *y, int left)
 {
     typedef typename std::conditional<HALF, _Float16, float>::type T;
@@ -366,16 +367,17 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
     for (int j = 0; j < TN; ++j)
 #pragma unroll
         for (int i = 0; i < TM; ++i) sum[j][i] = (i32x16)0;
-    // What the end needs, asked for at the begin where there are registers for it.  A lane ends with channels n_lane to n_lane + 7
-    // of tokens m_lane + kTokens * (0, 1, ...).
+    // What the end needs, asked for at the begin where there are registers for it.  A lane ends with eight channels of tokens m_lane +
+    // kTokens * (0, 1, ...): n_lane to n_lane + 3 and `apart` behind them, so that the lanes of a store have neighbouring 16 bytes
+    // (12000 x 2048 x 600 FP32 53.0 us with 32 bytes of a lane in two stores, 44.8 so).
     constexpr int kLanes = TN * 32 / 8, kTokens = 64 / kLanes, kRows = 32 / kTokens;      // lanes of a token, tokens at once, times
     constexpr bool kEarly = TM * TN <= 4;
-    const int n_lane = n0 + wn + lane % kLanes * 8, m_lane = m0 + wm + lane / kLanes;
+    const int apart = a.y16 ? 4 : kLanes * 4, at_lane = lane % kLanes * (a.y16 ? 8 : 4), n_lane = n0 + wn + at_lane, m_lane = m0 + wm + lane / kLanes;
     float ws[8], bias[8], xs[TM * kRows];
     auto ask_scales = [&] {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            const int j = min(n_lane + e, a.n - 1);
+            const int j = min(n_lane + e % 4 + e / 4 * apart, a.n - 1);
             ws[e] = ld_global(a.ws + (long long)j * a.ws_step);
             bias[e] = a.bias ? ld_global(a.bias + j) : 0.0f;
         }
@@ -479,23 +481,30 @@ __global__ __launch_bounds__(WM * WN * 64) void linear_tile_kernel(LinearArgs a)
 #pragma unroll
             for (int t = 0; t < kRows; ++t) {
                 const int row = i * 32 + t * kTokens;
-                const int *from = mine + (t * kTokens + lane / kLanes) * kPitch + lane % kLanes * 8;
-                const i32x4 low = *(const i32x4 *)from, high = *(const i32x4 *)(from + 4);
+                const int *from = mine + (t * kTokens + lane / kLanes) * kPitch + at_lane;
+                const i32x4 low = *(const i32x4 *)from, high = *(const i32x4 *)(from + apart);
                 float y[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] = (float)(e < 4 ? low[e] : high[e - 4]) * (xs[i * kRows + t] * ws[e]);
                 if (a.bias)
 #pragma unroll
                     for (int e = 0; e < 8; ++e) y[e] += bias[e];
-                if (m_lane + row < a.m) store_channels<half, whole, lines, 8>(y0 + row * row_bytes, y, a.n - n_lane);
+                if (m_lane + row >= a.m) continue;
+                if constexpr (half) {
+                    store_channels<true, whole, lines, 8>(y0 + row * row_bytes, y, a.n - n_lane);
+                } else {
+                    store_channels<false, whole, lines, 4>(y0 + row * row_bytes, y, a.n - n_lane);
+                    store_channels<false, whole, lines, 4>(y0 + row * row_bytes + apart * 4, y + 4, a.n - n_lane - apart);
+                }
             }
             lanes_in_step();
         }
     };
-    constexpr std::bool_constant<TN == 2> line{};               // 64 channels of FP16
+    constexpr std::bool_constant<TN == 2> line{};               // 64 channels of FP16, 32 of FP32
     if (n0 + wn + TN * 32 <= a.n) {
         if (a.y16 && line && a.y_lines) finish(sure, sure, line);
         else if (a.y16) finish(sure, sure, maybe);
+        else if (line && a.y_lines) finish(maybe, sure, line);
         else finish(maybe, sure, maybe);
     } else {
         if (a.y16) finish(sure, maybe, maybe);
@@ -767,7 +776,9 @@ template <typename X> int launch_few(const LinearArgs &a, void *stream)
 // y; codes by a launch of their own and tiles 58.5).  A block has TOK * 16 tokens.  It turns
 // them into codes in LDS, a row to 16 lanes, V vectors each, with all of a wavefront's rows requested before the first is
 // looked at; then every wavefront multiplies all of them by 16 * CH channels at a time.  w, small enough to stay in the L2s,
-// goes from there into registers, whole rows of it: the first before x is quantized, the next as the last are used up.
+// goes from there into registers, whole rows of it: the first before x is quantized, the next as the last are used up.  Which rows
+// make one matrix instruction's 16 is free: those with which a store's lanes have the longest runs, 4 * CH channels of a token to a
+// lane of FP16 (20000 x 1000 x 64 16.4 -> 14.8 us), 4 with the neighbouring lanes' behind them of FP32 (the other way 19.1 -> 22.9).
 //
 // w may lie at any address: where k is no multiple of 16, its last codes are fetched as those of the 16 that end with the row, and the
 // codes of x are laid out for that (end_behind).  With many channels and few tokens, blockIdx.y shares the channels out: x, small then,
@@ -808,10 +819,11 @@ __global__ __launch_bounds__(kRowsWaves * 64) void linear_rows_kernel(LinearArgs
     __builtin_amdgcn_sched_barrier(0);
     const int tiles = (a.n + 16 * CH - 1) / (16 * CH);
     i32x4 cw[kSteps][CH];
+    const int by_c = a.y16 ? 4 : 16, by_group = a.y16 ? 4 * CH : 4;
     auto load_w = [&](int tile, int step) {
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
-            const int8_t *row = a.w + (long long)min((tile * CH + c) * 16 + lane % 16, a.n - 1) * a.ldw;
+            const int8_t *row = a.w + (long long)min(tile * 16 * CH + lane % 16 / 4 * by_group + c * by_c + lane % 4, a.n - 1) * a.ldw;
             __builtin_memcpy(&cw[step][c], (const FQ_GLOBAL int8_t *)(row + min(step * 64 + lane / 16 * 16, a.k - 16)), 16);      // (behind k the codes of x are 0)
         }
     };
@@ -860,16 +872,14 @@ __global__ __launch_bounds__(kRowsWaves * 64) void linear_rows_kernel(LinearArgs
             }
             if (tile + stride < tiles) load_w(tile + stride, j);
         }
-        const int n = tile * CH * 16 + lane / 16 * 4;
-        float ws[CH][4], bias[CH][4];
+        const int n = tile * 16 * CH + lane / 16 * by_group;
+        float ws[CH * 4], bias[CH * 4];
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int j = min(n + c * 16 + e, a.n - 1);
-                ws[c][e] = ld_global(a.ws + (long long)j * a.ws_step);
-                bias[c][e] = a.bias ? ld_global(a.bias + j) : 0.0f;
-            }
+        for (int e = 0; e < CH * 4; ++e) {
+            const int j = min(n + e / 4 * by_c + e % 4, a.n - 1);
+            ws[e] = ld_global(a.ws + (long long)j * a.ws_step);
+            bias[e] = a.bias ? ld_global(a.bias + j) : 0.0f;
+        }
         auto finish = [&](auto half, auto whole) {
 #pragma unroll
             for (int t = 0; t < TOK; ++t) {
@@ -877,15 +887,17 @@ __global__ __launch_bounds__(kRowsWaves * 64) void linear_rows_kernel(LinearArgs
                 const float xs = scales[t * 16 + lane % 16];
                 char *const to = (char *)a.y + ((long long)m * a.ldy + n) * (half ? 2 : 4);
                 if (m >= a.m) continue;
+                float y[CH * 4];
 #pragma unroll
-                for (int c = 0; c < CH; ++c) {
-                    float y[4];
+                for (int e = 0; e < CH * 4; ++e) y[e] = (float)sum[e / 4][t][e % 4] * (xs * ws[e]);
+                if (a.bias)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) y[e] = (float)sum[c][t][e] * (xs * ws[c][e]);
-                    if (a.bias)
+                    for (int e = 0; e < CH * 4; ++e) y[e] += bias[e];
+                if constexpr (half) {
+                    store_channels<true, whole, false, CH * 4>(to, y, a.n - n);
+                } else {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) y[e] += bias[c][e];
-                    store_channels<half, whole, false, 4>(to + c * 16 * (half ? 2 : 4), y, a.n - n - c * 16);
+                    for (int c = 0; c < CH; ++c) store_channels<false, whole, false, 4>(to + c * 64, y + c * 4, a.n - n - c * 16);
                 }
             }
         };
