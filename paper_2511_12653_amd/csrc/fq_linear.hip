@@ -3,10 +3,10 @@
 //   y_ij = (sum_k q_ik w_jk) * (xs_i * ws_j) + bias_j          the sum exact in 32 bits, the rest in binary32
 //   xs_i = max_k |x_ik| / 127,  q_ik = round(x_ik / xs_i)      where x comes in FP16 or FP32
 //
-// Few tokens: linear_few_kernel, which with up to 16 and room for them in LDS does all of it in one launch, bound by the stream of w.  Short rows and few channels:
-// linear_rows_kernel, one launch, bound by x and y.  All else: quantize_rows_kernel, bound by memory, and linear_tile_kernel, bound
-// by the matrix cores or, in few tiles, by what a compute unit can load.  Quantizing inside the tiles would do it again for every tile
-// of channels: n / 256 times.  Sizes below are m x n x k, tokens by channels by values of a row.
+// Few tokens: linear_few_kernel, which with up to 16 and room for them in LDS does all of it in one launch, bound by the stream of w.
+// Short rows and few channels: linear_rows_kernel, one launch, bound by x and y.  All else: quantize_rows_kernel, bound by memory, and
+// linear_tile_kernel, bound by the matrix cores or, in few tiles, by what a compute unit can load.  Quantizing inside the tiles would do
+// it again for every tile of channels: n / 256 times.  Sizes below are m x n x k, tokens by channels by values of a row.
 #include <type_traits>
 
 #include "fq_device.h"
@@ -22,8 +22,6 @@ typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 // ---------------------------------------------------------------------------------------------
 // Codes and scale of a row of x.
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
 // L lanes have a row, V vectors of eight values each: vectors l, l + L, l + 2 L, ... to lane l.  All of them are asked for at
@@ -202,7 +200,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs a, unsi
 }
 
 // ---------------------------------------------------------------------------------------------
-// Product of a tile of BM tokens by BN channels.  What bounds it, by tile: 256 x 256 the matrix cores, which are busy 63 % of the
+// Product of a tile of BM tokens by BN channels.  What bounds it, by tile: 256 x 256 the matrix cores, which are busy 65 % of the
 // cycles at a clock that their power holds down (8192 x 8192 x 8192 460 us, 2.39 POP/s; codes that are all zero are 12 to 25 % faster);
 // the smaller ones, taken where large ones leave compute units without work, what a compute unit can load, 40 to 50 bytes a cycle (17
 // x 64 x 4096, a block or two in all: 16 KiB of a 64 x 64 step in 0.15 us, 32 KiB of a 128 x 128 step in 0.37).  More stages, and codes
@@ -763,8 +761,11 @@ template <int RINGED> int launch_ringed(const LinearArgs &a, unsigned blocks, vo
 template <typename X> int launch_few(const LinearArgs &a, void *stream)
 {
     const unsigned blocks = ((unsigned)a.n + 15) / 16;
+    // (32 tokens to a block where 16 would make more blocks than compute units.  us, 32 / 16 where they do not: 385 x 64 x 6448 codes 7.4 / 5.6,
+    // 32 x 2048 x 14336 10.2 / 8.2, 112 x 384 x 668 4.4 / 4.4.)
     if constexpr (sizeof(X) == 1)
-        if (few_most(a, 1) > kFewLds || !a.x_fits) return a.m <= 16 ? launch_ringed<16>(a, blocks, stream) : launch_ringed<32>(a, blocks, stream);
+        if (few_most(a, 1) > kFewLds || !a.x_fits)
+            return ((long long)a.m + 15) / 16 * blocks <= kComputeUnits || a.m <= 16 ? launch_ringed<16>(a, blocks, stream) : launch_ringed<32>(a, blocks, stream);
     const size_t lds = (size_t)few_lds(a.m, a.k, sizeof(X), !few_fits(a)).total;
     if (few_fits(a)) linear_few_kernel<X, false><<<blocks, kFewWaves * 64, lds, (hipStream_t)stream>>>(a);
     else linear_few_kernel<X, true><<<blocks, kFewWaves * 64, lds, (hipStream_t)stream>>>(a);
