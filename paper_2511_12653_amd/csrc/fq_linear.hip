@@ -26,15 +26,17 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
 // L lanes have a row, V vectors of eight values each: vectors l, l + L, l + 2 L, ... to lane l.  All of them are asked for at
 // once, by loads that no lane branches round (any address will do; lanes without eight values take the row's first, which
-// leaves its greatest magnitude as it is, and with k < 8 all take `spare`, 32 bytes of no matter what).  An odd end is fetched
-// value by value.
+// leaves its greatest magnitude as it is, and with k < 8, where a row need not have as many, all take zeros: with k = 0 they
+// are the row).  An odd end is fetched value by value.
 template <typename T> struct Eight { i32x4 w[sizeof(T) / 2]; };
 template <typename T> struct Values { typedef T type __attribute__((ext_vector_type(8))); };
 
-template <typename T> __device__ __forceinline__ Eight<T> ask8(const T *row, int at, int k, const void *spare)
+__constant__ const int kZeros[8] = {};
+
+template <typename T> __device__ __forceinline__ Eight<T> ask8(const T *row, int at, int k)
 {
     Eight<T> r;
-    const T *p = k >= 8 ? row + (at + 8 <= k ? at : 0) : (const T *)spare;
+    const T *p = k >= 8 ? row + (at + 8 <= k ? at : 0) : (const T *)kZeros;
     __builtin_memcpy(&r, (const FQ_GLOBAL T *)p, sizeof r);
     return r;
 }
@@ -167,13 +169,13 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs a, unsi
     const T *x = (const T *)a.x + min(row, (long long)a.m - 1) * a.ldx;
     Eight<T> raw[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) raw[j] = ask8(x, j * L * 8 + at, a.k, a.q);
+    for (int j = 0; j < V; ++j) raw[j] = ask8(x, j * L * 8 + at, a.k);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int j = 0; j < V; ++j) odd_end(raw[j], x, j * L * 8 + at, a.k);
     unsigned most = most_of(raw);
     for (int i = V * L * 8 + at; i < a.k; i += L * 8) {
-        Eight<T> more[1] = {ask8(x, i, a.k, a.q)};
+        Eight<T> more[1] = {ask8(x, i, a.k)};
         odd_end(more[0], x, i, a.k);
         most = max(most, most_of(more));
     }
@@ -193,7 +195,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs a, unsi
         if (i < a.pitch) *(FQ_GLOBAL u32x2 *)(q + i) = codes8(raw[j], r, i >= a.k);
     }
     for (int i = V * L * 8 + at; i < a.pitch; i += L * 8) {
-        Eight<T> more = ask8(x, i, a.k, a.q);
+        Eight<T> more = ask8(x, i, a.k);
         odd_end(more, x, i, a.k);
         *(FQ_GLOBAL u32x2 *)(q + i) = codes8(more, r, i >= a.k);
     }
@@ -816,7 +818,7 @@ __global__ __launch_bounds__(kRowsWaves * 64) void linear_rows_kernel(LinearArgs
     for (int r = 0; r < kPasses; ++r)
         if ((r * WAVES + wave) * 4 < kRows)
 #pragma unroll
-            for (int j = 0; j < V; ++j) raw[r][j] = ask8(row_of_x(r), (j * 16 + lane % 16) * 8, a.k, a.w);
+            for (int j = 0; j < V; ++j) raw[r][j] = ask8(row_of_x(r), (j * 16 + lane % 16) * 8, a.k);
     __builtin_amdgcn_sched_barrier(0);
     const int tiles = (a.n + 16 * CH - 1) / (16 * CH);
     i32x4 cw[kSteps][CH];
