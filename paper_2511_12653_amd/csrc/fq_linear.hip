@@ -1056,7 +1056,10 @@ template <typename X> static int launch_rows(const LinearArgs &a, void *stream)
 
 int launch_linear(const LinearArgs &a, void *stream)
 {
-    if (a.raw && a.m <= 16) return a.x16 ? launch_few<_Float16>(a, stream) : launch_few<float>(a, stream);
+    // (x given as raw for its short rows goes there also with 16 tokens or fewer: offsets into rows of w beyond kMostPitch need 64 bits, and
+    // blocks that are not all on the chip at once cost.  us, few tokens / short rows: 16 x 16384 x 512 17.4 / 6.0, 1 x 16384 x 64 6.5 / 4.1,
+    // 1 x 16384 x 512 6.6 / 5.7, 1 x 8208 x 512 5.2 / 5.4.)
+    if (a.raw && linear_few(a, a.x16 ? 2 : 4)) return a.x16 ? launch_few<_Float16>(a, stream) : launch_few<float>(a, stream);
     if (a.raw) return a.x16 ? launch_rows<_Float16>(a, stream) : launch_rows<float>(a, stream);
     if (linear_few(a, 1)) return launch_few<int8_t>(a, stream);
     int best = 0;
