@@ -8,7 +8,9 @@ namespace fq {
 namespace {
 
 constexpr size_t kAlign = 256;
-constexpr long long kMostRows = 1LL << 23;       // of x to a launch: a grid has less than 2^32 threads, a row up to 256 of them
+// What a launch takes, so that its grid has less than 2^32 threads: rows of x, up to 256 threads to one; channels, 512 to 16 of them;
+// bytes of codes that are laid out anew, of x and w each, a thread to 16.
+constexpr long long kMostRows = 1LL << 23, kMostChannels = 1LL << 26, kMostCodes = 1LL << 34;
 
 size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
@@ -152,15 +154,22 @@ fq_status forward(const fq_linear &d, void *workspace, size_t ws_bytes, void *st
         if (!workspace || ws_bytes < workspace_of(d).bytes) return FQ_ERR_WORKSPACE;
         if (!aligned(workspace, kAlign)) return FQ_ERR_ALIGN;
     }
-    for (long long row = 0; row < d.m; row += kMostRows) {
-        fq_linear part = d;
-        part.m = d.m - row < kMostRows ? d.m - row : kMostRows;
-        part.x = d.x ? (const char *)d.x + (size_t)(row * d.ldx) * size_of(d.x_dtype) : nullptr;
-        part.xs = d.xs ? d.xs + row * d.xs_step : nullptr;
-        part.y = (char *)d.y + (size_t)(row * d.ldy) * size_of(d.y_dtype);
-        const fq_status ran = run(part, workspace, stream);
-        if (ran != FQ_OK) return ran;
-    }
+    const long long most = kMostCodes / (workspace_of(d).pitch ? workspace_of(d).pitch : 1);
+    const long long rows = most < kMostRows ? most : kMostRows, channels = most < kMostChannels ? most : kMostChannels;
+    for (long long row = 0; row < d.m; row += rows)
+        for (long long column = 0; column < d.n; column += channels) {
+            fq_linear part = d;
+            part.m = d.m - row < rows ? d.m - row : rows;
+            part.n = d.n - column < channels ? d.n - column : channels;
+            part.x = d.x ? (const char *)d.x + (size_t)(row * d.ldx) * size_of(d.x_dtype) : nullptr;
+            part.xs = d.xs ? d.xs + row * d.xs_step : nullptr;
+            part.w = d.w ? d.w + column * d.ldw : nullptr;
+            part.ws = d.ws + column * d.ws_step;
+            part.bias = d.bias ? d.bias + column : nullptr;
+            part.y = (char *)d.y + (size_t)(row * d.ldy + column) * size_of(d.y_dtype);
+            const fq_status ran = run(part, workspace, stream);
+            if (ran != FQ_OK) return ran;
+        }
     return FQ_OK;
 }
 
