@@ -12,19 +12,23 @@ _DTYPES = (torch.float16, torch.float32)
 
 
 class _Plan:
-    """A plan of the library with its workspace and the tensors whose addresses it holds."""
+    """A plan of the library with its workspace, and the tensors whose addresses it holds but the gradients: those are the
+    program's to free when a step has been enqueued, and a plan is taken again only where they are at the same addresses."""
 
-    def __init__(self, key, params, device):
-        self.key, self.params = key, params
+    def __init__(self, key, params, held, device):
+        self.key, self.held = key, held
         self.workspace = torch.empty(fq.fq_adamw_workspace_bytes(params), dtype=torch.uint8, device=device)
         self.handle = fq.fq_adamw_create(params, self.workspace)
         self.stream = torch.cuda.current_stream()
 
-    def used_here(self):
-        """The workspace was allocated on another stream than the current one: it stays until that is done with it, too."""
+    def used_here(self, gradients):
+        """What was allocated on another stream than the current one stays until that is done with it, too."""
         stream = torch.cuda.current_stream()
         if stream != self.stream:
             self.workspace.record_stream(stream)
+        if stream != torch.cuda.default_stream():
+            for g in gradients:                     # (nothing happens to one that is of this stream)
+                g.record_stream(stream)
 
     def __del__(self):
         if getattr(self, "handle", None):
@@ -88,7 +92,8 @@ class AdamW(torch.optim.Optimizer):
                 raise TypeError("gradients must be dense and contiguous")
             params = [fq.FqParam.from_torch(p.detach(), p.grad, s["m"], s["v"], s.get("m_scale"), s.get("v_scale"), p16=c,
                                             weight_decay=group["weight_decay"]) for p, s, c in chosen]
-            plan = self._plans[index] = _Plan(key, params, chosen[0][0].device)
+            held = [(p.detach(), c, *s.values()) for p, s, c in chosen]
+            plan = self._plans[index] = _Plan(key, params, held, chosen[0][0].device)
         return plan
 
     @torch.no_grad()
@@ -106,7 +111,7 @@ class AdamW(torch.optim.Optimizer):
                 plan = self._plan(index, group)
                 if plan is not None:
                     beta1, beta2 = group["betas"]
-                    plan.used_here()
+                    plan.used_here([p.grad for p in group["params"] if p.grad is not None])
                     fq.fq_adamw_step(plan.handle, fq.FqAdamW(group["lr"], beta1, beta2, group["eps"], group["step"], group["seed"],
                                                              grad_scale))
         return loss
