@@ -54,6 +54,7 @@ def test_a_gradient_outlives_a_step_on_another_stream():
     big, side = torch.ones(8192, 8192, device="cuda"), torch.cuda.Stream()
     p.grad = torch.ones(1 << 20, device="cuda")
     at = p.grad.data_ptr()
+    opt.step()                                       # (makes the plan, whose table may wait for the GPU)
     side.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(side):
         product = big
@@ -64,4 +65,4 @@ def test_a_gradient_outlives_a_step_on_another_stream():
     assert torch.empty(1 << 20, device="cuda").data_ptr() != at
     assert not side.query()                          # (or this has shown nothing)
     torch.cuda.current_stream().wait_stream(side)
-    assert bool((p.detach() < -9e-3).all())
+    assert bool((p.detach() < -1.9e-2).all())
