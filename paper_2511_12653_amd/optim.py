@@ -4,11 +4,20 @@ fq_adamw_step call (one launch) per parameter group.
 Marshalling only.  The moments are float32, or float8_e4m3fn codes with a scale per 256 elements (`states="float8"`, a quarter
 of the memory, rounded stochastically).  There is no CPU path: CPU parameters raise.
 """
+import math
+
 import torch
 
 from . import binding as fq
 
 _DTYPES = (torch.float16, torch.float32)
+
+
+def _check_rates(group):
+    """What the library would refuse in a step."""
+    lr, (beta1, beta2), eps, decay = group["lr"], group["betas"], group["eps"], group["weight_decay"]
+    if not (math.isfinite(lr) and 0.0 <= beta1 < 1.0 and 0.0 <= beta2 < 1.0 and math.isfinite(eps) and eps >= 0.0 and math.isfinite(decay)):
+        raise ValueError("lr %r, betas %r, eps %r or weight_decay %r is out of range" % (lr, (beta1, beta2), eps, decay))
 
 
 class _Plan:
@@ -41,7 +50,8 @@ class AdamW(torch.optim.Optimizer):
     states: "float32" or "float8".  seed: of the stochastic rounding of float8 states.  A group may override lr, betas, eps,
     weight_decay and states, and may bring `copies`: one float16 tensor (or None) per float32 parameter, which receives
     its new values.  Elements whose gradient is not finite are left as they are.  All parameters of a group share
-    its step count; one without a gradient is skipped.
+    its step count; one without a gradient is skipped.  A group in which none has a gradient does not count the step, nor does any
+    group count or make a step that is refused.
     """
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, states="float32", seed=0):
@@ -103,17 +113,23 @@ class AdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
+        # Everything is looked at before anything is launched: a step that is refused moves no group, and does not count.
+        launches = []
         for index, group in enumerate(self.param_groups):
-            group["step"] += 1
             if not group["params"]:
                 continue
+            _check_rates(group)
             with torch.cuda.device(group["params"][0].device):
                 plan = self._plan(index, group)
-                if plan is not None:
-                    beta1, beta2 = group["betas"]
-                    plan.used_here([p.grad for p in group["params"] if p.grad is not None])
-                    fq.fq_adamw_step(plan.handle, fq.FqAdamW(group["lr"], beta1, beta2, group["eps"], group["step"], group["seed"],
-                                                             grad_scale))
+            if plan is not None:
+                beta1, beta2 = group["betas"]
+                launches.append((group, plan, fq.FqAdamW(group["lr"], beta1, beta2, group["eps"], group["step"] + 1, group["seed"],
+                                                         grad_scale)))
+        for group, plan, rates in launches:
+            with torch.cuda.device(group["params"][0].device):
+                plan.used_here([p.grad for p in group["params"] if p.grad is not None])
+                fq.fq_adamw_step(plan.handle, rates)
+            group["step"] += 1
         return loss
 
     def __setstate__(self, state):
