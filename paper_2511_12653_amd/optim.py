@@ -49,9 +49,10 @@ class AdamW(torch.optim.Optimizer):
 
     states: "float32" or "float8".  seed: of the stochastic rounding of float8 states.  A group may override lr, betas, eps,
     weight_decay and states, and may bring `copies`: one float16 tensor (or None) per float32 parameter, which receives
-    its new values.  Elements whose gradient is not finite are left as they are.  All parameters of a group share
-    its step count; one without a gradient is skipped.  A group in which none has a gradient does not count the step, nor does any
-    group count or make a step that is refused.
+    its new values.  Elements whose gradient is not finite are left as they are.  A group counts its steps; for a parameter whose
+    first gradient comes later they count from that one on.  Steps in which it has none after that leave it as it is and do
+    count.  A group in which no parameter has a gradient does not count the step, nor does any group count or make a step that is
+    refused.
     """
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, states="float32", seed=0):
@@ -74,9 +75,12 @@ class AdamW(torch.optim.Optimizer):
         # (groups round differently: each has its own part of the seeds)
         group["seed"] = int(group["seed"]) + ((len(self.param_groups) - 1) << 32)
 
-    def _state_of(self, p, group):
+    def _state_of(self, p, group, made):
         state = self.state[p]
         if not state:
+            made.append(p)
+            if group["step"]:
+                state["late"] = group["step"]       # steps of the group before its first
             if group["states"] == "float8":
                 blocks = (p.numel() + 255) // 256
                 for name in ("m", "v"):
@@ -87,23 +91,33 @@ class AdamW(torch.optim.Optimizer):
                     state[name] = torch.zeros(p.shape, device=p.device)
         return state
 
-    def _plan(self, index, group):
-        chosen = [(p, self._state_of(p, group), c)
-                  for p, c in zip(group["params"], group["copies"] or [None] * len(group["params"])) if p.grad is not None]
-        if not chosen:
-            return None
+    def _launches(self, index, group, grad_scale, made):
+        """A launch for the parameters with a gradient, or, where some had their first one late, for those of each step number:
+        [(plan, what fq_adamw_step takes, gradients)]."""
+        chosen = {}
+        for p, c in zip(group["params"], group["copies"] or [None] * len(group["params"])):
+            if p.grad is not None:
+                state = self._state_of(p, group, made)
+                chosen.setdefault(state.get("late", 0), []).append((p, state, c))
+        beta1, beta2 = group["betas"]
+        return [(self._plan((index, late), group, some),
+                 fq.FqAdamW(group["lr"], beta1, beta2, group["eps"], group["step"] + 1 - late, group["seed"], grad_scale),
+                 [p.grad for p, _, _ in some]) for late, some in chosen.items()]
+
+    def _plan(self, place, group, chosen):
+        tensors = [[t for name, t in s.items() if name != "late"] for _, s, _ in chosen]
         # All that the plan's table is made of.  Gradients are often other tensors in every step: then it is made anew.
         key = (group["weight_decay"],) + tuple(
             (p.numel(), p.dtype, p.data_ptr(), p.grad.dtype, p.grad.stride(), p.grad.data_ptr(), c is not None and c.data_ptr())
-            + tuple(t.data_ptr() for t in s.values()) for p, s, c in chosen)
-        plan = self._plans.get(index)
+            + tuple(t.data_ptr() for t in ts) for (p, _, c), ts in zip(chosen, tensors))
+        plan = self._plans.get(place)
         if plan is None or plan.key != key:
             if any(p.grad.is_sparse or not p.grad.is_contiguous() for p, _, _ in chosen):
                 raise TypeError("gradients must be dense and contiguous")
             params = [fq.FqParam.from_torch(p.detach(), p.grad, s["m"], s["v"], s.get("m_scale"), s.get("v_scale"), p16=c,
                                             weight_decay=group["weight_decay"]) for p, s, c in chosen]
-            held = [(p.detach(), c, *s.values()) for p, s, c in chosen]
-            plan = self._plans[index] = _Plan(key, params, held, chosen[0][0].device)
+            held = [(p.detach(), c, *ts) for (p, _, c), ts in zip(chosen, tensors)]
+            plan = self._plans[place] = _Plan(key, params, held, chosen[0][0].device)
         return plan
 
     @torch.no_grad()
@@ -114,22 +128,24 @@ class AdamW(torch.optim.Optimizer):
             with torch.enable_grad():
                 loss = closure()
         # Everything is looked at before anything is launched: a step that is refused moves no group, and does not count.
-        launches = []
-        for index, group in enumerate(self.param_groups):
-            if not group["params"]:
-                continue
-            _check_rates(group)
+        launches, made = [], []
+        try:
+            for index, group in enumerate(self.param_groups):
+                if group["params"]:
+                    _check_rates(group)
+                    with torch.cuda.device(group["params"][0].device):
+                        launches.append((group, self._launches(index, group, grad_scale, made)))
+        except BaseException:
+            for p in made:                          # (its first gradient is yet to come)
+                del self.state[p]
+            raise
+        for group, parts in launches:
             with torch.cuda.device(group["params"][0].device):
-                plan = self._plan(index, group)
-            if plan is not None:
-                beta1, beta2 = group["betas"]
-                launches.append((group, plan, fq.FqAdamW(group["lr"], beta1, beta2, group["eps"], group["step"] + 1, group["seed"],
-                                                         grad_scale)))
-        for group, plan, rates in launches:
-            with torch.cuda.device(group["params"][0].device):
-                plan.used_here([p.grad for p in group["params"] if p.grad is not None])
-                fq.fq_adamw_step(plan.handle, rates)
-            group["step"] += 1
+                for plan, rates, gradients in parts:
+                    plan.used_here(gradients)
+                    fq.fq_adamw_step(plan.handle, rates)
+            if parts:
+                group["step"] += 1
         return loss
 
     def __setstate__(self, state):
@@ -153,5 +169,5 @@ class AdamW(torch.optim.Optimizer):
         own = [p for g in self.param_groups for p in g["params"]]
         for i, p in zip(saved, own):
             if i in state_dict["state"]:
-                self.state[p] = {k: v.to(p.device, copy=True) for k, v in state_dict["state"][i].items()}
+                self.state[p] = {k: v.to(p.device, copy=True) if torch.is_tensor(v) else v for k, v in state_dict["state"][i].items()}
         self._plans = {}
