@@ -122,7 +122,7 @@ class AdamW(torch.optim.Optimizer):
 
     @torch.no_grad()
     def step(self, closure=None, grad_scale=None):
-        """grad_scale: one float32 on the GPU that all gradients are multiplied by, or None."""
+        """grad_scale: one float32 on the GPU that all gradients are multiplied by, or None.  Not under graph capture."""
         loss = None
         if closure is not None:
             with torch.enable_grad():
@@ -134,6 +134,9 @@ class AdamW(torch.optim.Optimizer):
                 if group["params"]:
                     _check_rates(group)
                     with torch.cuda.device(group["params"][0].device):
+                        # (replays would repeat the step number and its random bits, and a table copied by a capture is read later)
+                        if torch.cuda.is_current_stream_capturing():
+                            raise RuntimeError("AdamW.step() cannot be captured into a graph; fq_adamw_step with a plan of its own can")
                         launches.append((group, self._launches(index, group, grad_scale, made)))
         except BaseException:
             for p in made:                          # (its first gradient is yet to come)

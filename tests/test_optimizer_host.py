@@ -1,0 +1,48 @@
+"""What the AdamW optimizer refuses before anything reaches a GPU: host logic, with tensors on the CPU that say they are on a card."""
+import contextlib
+
+import pytest
+import torch
+
+from paper_2511_12653_amd import AdamW
+from paper_2511_12653_amd import binding as fq
+
+
+class OnCard(torch.Tensor):
+    """A tensor whose memory is the CPU's and whose device is card `card`."""
+    card = 0
+    is_cuda = property(lambda self: True)
+    device = property(lambda self: torch.device("cuda", self.card))
+
+    def get_device(self):
+        return self.card
+
+
+def on_card(t, card=0, parameter=False):
+    t = t.as_subclass(OnCard)
+    t.card = card
+    return t.requires_grad_() if parameter else t
+
+
+def parameter(n=8, card=0, dtype=torch.float32):
+    return on_card(torch.zeros(n, dtype=dtype), card, True)
+
+
+@pytest.fixture
+def no_gpu(monkeypatch):
+    """Fails where the library is called."""
+    def called(*_):
+        raise AssertionError("the library was called")
+    monkeypatch.setattr(torch.cuda, "device", lambda *_: contextlib.nullcontext())
+    for name in ("fq_adamw_create", "fq_adamw_workspace_bytes", "fq_adamw_step"):
+        monkeypatch.setattr(fq, name, called)
+
+
+def test_a_step_is_not_captured(monkeypatch, no_gpu):
+    p = parameter()
+    opt = AdamW([p])
+    p.grad = torch.ones(8).as_subclass(OnCard)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+    with pytest.raises(RuntimeError, match="captur"):
+        opt.step()
+    assert opt.param_groups[0]["step"] == 0 and not opt.state
