@@ -20,6 +20,19 @@ def _check_rates(group):
         raise ValueError("lr %r, betas %r, eps %r or weight_decay %r is out of range" % (lr, (beta1, beta2), eps, decay))
 
 
+def _check_group(group):
+    if group["states"] not in ("float32", "float8"):
+        raise ValueError("states must be float32 or float8, not %r" % (group["states"],))
+    for p in group["params"]:
+        if not p.is_cuda:
+            raise RuntimeError("AdamW runs on the GPU only (no CPU fallback)")
+        if p.dtype not in _DTYPES or not p.is_contiguous():
+            raise TypeError("parameters must be contiguous float16 or float32")
+    if group["copies"] is not None and len(group["copies"]) != len(group["params"]):
+        raise ValueError("copies must hold a tensor or None for each parameter")
+    _check_rates(group)
+
+
 class _Plan:
     """A plan of the library with its workspace, and the tensors whose addresses it holds but the gradients: those are the
     program's to free when a step has been enqueued, and a plan is taken again only where they are at the same addresses."""
@@ -63,17 +76,13 @@ class AdamW(torch.optim.Optimizer):
     def add_param_group(self, group):
         super().add_param_group(group)
         group = self.param_groups[-1]
-        if group["states"] not in ("float32", "float8"):
-            raise ValueError("states must be float32 or float8, not %r" % (group["states"],))
-        for p in group["params"]:
-            if not p.is_cuda:
-                raise RuntimeError("AdamW runs on the GPU only (no CPU fallback)")
-            if p.dtype not in _DTYPES or not p.is_contiguous():
-                raise TypeError("parameters must be contiguous float16 or float32")
-        if group["copies"] is not None and len(group["copies"]) != len(group["params"]):
-            raise ValueError("copies must hold a tensor or None for each parameter")
-        # (groups round differently: each has its own part of the seeds)
-        group["seed"] = int(group["seed"]) + ((len(self.param_groups) - 1) << 32)
+        try:
+            _check_group(group)
+            # (groups round differently: each has its own part of the seeds)
+            group["seed"] = int(group["seed"]) + ((len(self.param_groups) - 1) << 32)
+        except Exception:
+            self.param_groups.pop()
+            raise
 
     def _state_of(self, p, group, made):
         state = self.state[p]

@@ -46,3 +46,32 @@ def test_a_step_is_not_captured(monkeypatch, no_gpu):
     with pytest.raises(RuntimeError, match="captur"):
         opt.step()
     assert opt.param_groups[0]["step"] == 0 and not opt.state
+
+
+def refused():
+    return [(RuntimeError, {"params": [torch.zeros(8, requires_grad=True)]}),
+            (TypeError, {"params": [parameter(dtype=torch.float64)]}),
+            (ValueError, {"params": [parameter()], "states": "float4"}),
+            (ValueError, {"params": [parameter()], "copies": []}),
+            (ValueError, {"params": [parameter()], "lr": float("inf")}),
+            (ValueError, {"params": [parameter()], "lr": float("nan")}),
+            (ValueError, {"params": [parameter()], "betas": (1.0, 0.999)}),
+            (ValueError, {"params": [parameter()], "betas": (0.9, -0.1)}),
+            (ValueError, {"params": [parameter()], "betas": (0.9, float("nan"))}),
+            (ValueError, {"params": [parameter()], "eps": -1e-8}),
+            (ValueError, {"params": [parameter()], "eps": float("inf")}),
+            (ValueError, {"params": [parameter()], "weight_decay": float("nan")})]
+
+
+@pytest.mark.parametrize("which", range(len(refused())))
+def test_a_refused_group_does_not_stay(which):
+    error, group = refused()[which]
+    opt = AdamW([parameter()])
+    for _ in range(2):
+        with pytest.raises(error):
+            opt.add_param_group(group)
+        assert len(opt.param_groups) == 1
+    with pytest.raises(error):
+        AdamW([group])
+    opt.add_param_group({"params": [parameter()], "lr": 1e-2, "seed": 5})
+    assert len(opt.param_groups) == 2 and opt.param_groups[1]["seed"] == 5 + (1 << 32) and opt.param_groups[1]["lr"] == 1e-2
