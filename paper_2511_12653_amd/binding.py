@@ -147,6 +147,7 @@ def _device_of(tensors):
         raise ValueError("tensors must be on the GPU (no CPU fallback)")
     if len(devices) > 1:
         raise ValueError("tensors are on different GPUs")
+    return devices.pop() if devices else None
 
 
 class FqParam(ctypes.Structure):
@@ -178,13 +179,13 @@ class FqParam(ctypes.Structure):
             if t is not None and (t.dtype != torch.float32 or t.numel() != (n + 255) // 256):
                 raise ValueError("scales must be %d float32 values" % ((n + 255) // 256))
         given = (p, g, m, v, m_scale, v_scale, p16)
-        _device_of(given)
+        device = _device_of(given)
         if any(t is not None and not t.is_contiguous() for t in given):
             raise ValueError("tensors must be contiguous")
         ptr = lambda t: None if t is None else t.data_ptr()
         self = cls(n, dtypes[p.dtype], dtypes[g.dtype], FQ_STATE_F8 if f8 else FQ_STATE_F32, lr_scale, weight_decay,
                    ptr(p), ptr(g), ptr(p16), ptr(m), ptr(v), ptr(m_scale), ptr(v_scale))
-        self._keep = given
+        self._keep, self._device = given, device
         return self
 
 
@@ -496,6 +497,12 @@ def fq_adamw_workspace_bytes(params) -> int:
 
 def fq_adamw_create(params, workspace, stream=None):
     """Returns an opaque plan handle (ctypes.c_void_p); release it with fq_adamw_destroy."""
+    params = list(params)
+    devices = {getattr(t, "_device", None) for t in params}
+    if hasattr(workspace, "get_device"):
+        devices.add(workspace.get_device())
+    if len(devices - {None}) > 1:
+        raise ValueError("the list's tensors and its workspace must be on one GPU")
     arr, n = _params(params)
     p, nbytes = _ws(workspace)
     plan = ctypes.c_void_p()

@@ -30,6 +30,8 @@ def _check_group(group):
             raise TypeError("parameters must be contiguous float16 or float32")
     if group["copies"] is not None and len(group["copies"]) != len(group["params"]):
         raise ValueError("copies must hold a tensor or None for each parameter")
+    if len({t.get_device() for t in (*group["params"], *(group["copies"] or ())) if t is not None}) > 1:
+        raise ValueError("a group's parameters and copies must be on one GPU")
     _check_rates(group)
 
 
@@ -142,6 +144,8 @@ class AdamW(torch.optim.Optimizer):
             for index, group in enumerate(self.param_groups):
                 if group["params"]:
                     _check_rates(group)
+                    if grad_scale is not None and grad_scale.get_device() != group["params"][0].get_device():
+                        raise ValueError("grad_scale is not on the GPU of the group")
                     with torch.cuda.device(group["params"][0].device):
                         # (replays would repeat the step number and its random bits, and a table copied by a capture is read later)
                         if torch.cuda.is_current_stream_capturing():

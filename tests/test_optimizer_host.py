@@ -75,3 +75,37 @@ def test_a_refused_group_does_not_stay(which):
         AdamW([group])
     opt.add_param_group({"params": [parameter()], "lr": 1e-2, "seed": 5})
     assert len(opt.param_groups) == 2 and opt.param_groups[1]["seed"] == 5 + (1 << 32) and opt.param_groups[1]["lr"] == 1e-2
+
+
+def test_a_group_lies_on_one_card(no_gpu, monkeypatch):
+    opt = AdamW([parameter(card=1)])
+    for given in ({"params": [parameter(), parameter(card=1)]},
+                  {"params": [parameter(), parameter()], "copies": [None, on_card(torch.zeros(8, dtype=torch.float16), 1)]}):
+        with pytest.raises(ValueError, match="GPU"):
+            opt.add_param_group(given)
+    opt.add_param_group({"params": [parameter(), parameter()]})      # (another group's card is its own)
+    opt.add_param_group({"params": []})
+
+
+def test_the_gradients_scale_lies_on_the_groups_card(no_gpu, monkeypatch):
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    p = parameter()
+    p.grad = on_card(torch.ones(8))
+    opt = AdamW([p])
+    with pytest.raises(ValueError, match="GPU"):
+        opt.step(grad_scale=on_card(torch.ones(1), 1))
+    assert opt.param_groups[0]["step"] == 0 and not opt.state
+
+
+def f32(card=0):
+    return [on_card(torch.zeros(8), card) for _ in range(4)]
+
+
+def test_a_list_lies_on_one_card(monkeypatch):
+    params = [fq.FqParam.from_torch(*f32()), fq.FqParam.from_torch(*f32(1))]
+    with pytest.raises(ValueError, match="GPU"):
+        fq.fq_adamw_create(params, (1 << 20, 4096), stream=0)
+    with pytest.raises(ValueError, match="GPU"):
+        fq.fq_adamw_create(params[:1], on_card(torch.zeros(4096, dtype=torch.uint8), 1), stream=0)
+    with pytest.raises(ValueError, match="GPU"):
+        fq.FqParam.from_torch(*f32()[:3], f32(1)[0])
