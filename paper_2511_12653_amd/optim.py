@@ -108,6 +108,8 @@ class AdamW(torch.optim.Optimizer):
         chosen = {}
         for p, c in zip(group["params"], group["copies"] or [None] * len(group["params"])):
             if p.grad is not None:
+                if p.grad.layout is not torch.strided:
+                    raise TypeError("gradients must be dense and contiguous")
                 state = self._state_of(p, group, made)
                 chosen.setdefault(state.get("late", 0), []).append((p, state, c))
         beta1, beta2 = group["betas"]
@@ -123,7 +125,7 @@ class AdamW(torch.optim.Optimizer):
             + tuple(t.data_ptr() for t in ts) for (p, _, c), ts in zip(chosen, tensors))
         plan = self._plans.get(place)
         if plan is None or plan.key != key:
-            if any(p.grad.is_sparse or not p.grad.is_contiguous() for p, _, _ in chosen):
+            if not all(p.grad.is_contiguous() for p, _, _ in chosen):
                 raise TypeError("gradients must be dense and contiguous")
             params = [fq.FqParam.from_torch(p.detach(), p.grad, s["m"], s["v"], s.get("m_scale"), s.get("v_scale"), p16=c,
                                             weight_decay=group["weight_decay"]) for p, s, c in chosen]

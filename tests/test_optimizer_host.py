@@ -109,3 +109,17 @@ def test_a_list_lies_on_one_card(monkeypatch):
         fq.fq_adamw_create(params[:1], on_card(torch.zeros(4096, dtype=torch.uint8), 1), stream=0)
     with pytest.raises(ValueError, match="GPU"):
         fq.FqParam.from_torch(*f32()[:3], f32(1)[0])
+
+
+def test_sparse_gradients_are_refused(no_gpu, monkeypatch):
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    zeros = torch.zeros
+    monkeypatch.setattr(torch, "zeros", lambda *a, device=None, **kw: zeros(*a, **kw))
+    p = on_card(zeros(4, 2), parameter=True)
+    opt = AdamW([p])
+    dense = zeros(4, 2)
+    dense[1] = 1.0
+    p.grad = dense.to_sparse()
+    with pytest.raises(TypeError, match="dense"):
+        opt.step()
+    assert opt.param_groups[0]["step"] == 0 and not opt.state
