@@ -26,6 +26,7 @@ def linear_int8(x, w, w_scale, bias=None, x_scale=None, out=None, out_dtype=None
     n, k = w.shape
     rows = x.numel() // k if k else x.shape[:-1].numel()
     shape = (*x.shape[:-1], n)
+    given = out
     if out is None:
         out = torch.empty(shape, dtype=out_dtype or (torch.float16 if x.dtype == torch.int8 else x.dtype), device=x.device)
         y = out.view(rows, n)
@@ -40,4 +41,6 @@ def linear_int8(x, w, w_scale, bias=None, x_scale=None, out=None, out_dtype=None
         d = fq.FqLinear.from_torch(x2, w, w_scale, y, bias=bias, x_scale=x_scale)
         workspace = torch.empty(fq.fq_linear_workspace_bytes(d), dtype=torch.uint8, device=x.device)
         fq.fq_linear_forward(d, workspace)
+    if given is not None and not given.is_inference():
+        torch.autograd.graph.increment_version(given)      # (a backward pass that has saved it is told)
     return out

@@ -41,6 +41,8 @@ class _Plan:
 
     def __init__(self, key, params, held, device):
         self.key, self.held = key, held
+        # what a step writes and a program may have saved for a backward pass (inference tensors have no versions to count)
+        self.written = [t for of_one in held for t in of_one[:2] if t is not None and not t.is_inference()]
         self.workspace = torch.empty(fq.fq_adamw_workspace_bytes(params), dtype=torch.uint8, device=device)
         self.handle = fq.fq_adamw_create(params, self.workspace)
         self.stream = torch.cuda.current_stream()
@@ -162,6 +164,7 @@ class AdamW(torch.optim.Optimizer):
                 for plan, rates, gradients in parts:
                     plan.used_here(gradients)
                     fq.fq_adamw_step(plan.handle, rates)
+                    torch.autograd.graph.increment_version(plan.written)
             if parts:
                 group["step"] += 1
         return loss
