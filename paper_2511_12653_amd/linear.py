@@ -5,6 +5,7 @@ one).  There is no CPU path: CPU tensors raise.  There is no gradient either: co
 through `fake_quantize` and the float product, whose values these are.
 """
 import torch
+from torch.autograd.forward_ad import unpack_dual
 
 from . import binding as fq
 
@@ -17,8 +18,10 @@ def linear_int8(x, w, w_scale, bias=None, x_scale=None, out=None, out_dtype=None
     writes them.  bias: n float32 values or None.  out: [..., n] float16 or float32, made in out_dtype (default: x's type, or
     float16 for codes) if not given.
     """
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, w_scale, bias, x_scale)):
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, w_scale, bias, x_scale, out)):
         raise RuntimeError("linear_int8 has no gradient: call it under torch.no_grad(), train through fake_quantize")
+    if any(t is not None and unpack_dual(t).tangent is not None for t in (x, w_scale, bias, x_scale, out)):
+        raise RuntimeError("linear_int8 has no gradient in forward mode either: give it primal tensors")
     if not x.is_cuda:
         raise RuntimeError("linear_int8 runs on the GPU only (no CPU fallback)")
     if x.dim() < 1 or w.dim() != 2 or x.shape[-1] != w.shape[1]:

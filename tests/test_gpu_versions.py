@@ -1,6 +1,8 @@
-"""What linear_int8 and the AdamW optimizer write counts as written for autograd."""
+"""What linear_int8 and the AdamW optimizer write counts as written for autograd, and linear_int8 loses neither a tangent nor a
+history."""
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 from paper_2511_12653_amd import AdamW, linear_int8
 
@@ -42,3 +44,30 @@ def test_a_given_output_counts_as_written():
         assert torch.equal(linear_int8(x, w, ws, b, out=torch.ones(4, 8, device="cuda")), out)
         quiet = torch.ones(4, 8, device="cuda")
     assert torch.equal(linear_int8(x, w, ws, b, out=quiet), out)
+
+
+@pytest.mark.parametrize("which", ["x", "w_scale", "bias", "x_scale"])
+def test_linear_int8_refuses_a_tangent(which):
+    x, w, ws, b = operands()
+    given = {"x": x, "w": w, "w_scale": ws, "bias": b}
+    if which == "x_scale":
+        given.update(x=torch.ones(4, 16, dtype=torch.int8, device="cuda"), x_scale=torch.ones(4, device="cuda"))
+    for grad in (True, False):
+        with torch.set_grad_enabled(grad), forward_ad.dual_level():
+            dual = dict(given)
+            dual[which] = forward_ad.make_dual(given[which], torch.ones_like(given[which]))
+            with pytest.raises(RuntimeError, match="gradient"):
+                linear_int8(**dual)
+            linear_int8(**given)                     # (a level alone is nothing)
+    linear_int8(**given)
+
+
+def test_linear_int8_refuses_an_output_with_a_history():
+    x, w, ws, b = operands()
+    out = torch.ones(4, 8, device="cuda", requires_grad=True) * 2
+    with pytest.raises(RuntimeError, match="gradient"):
+        linear_int8(x, w, ws, b, out=out)
+    assert bool((out == 2).all())
+    with torch.no_grad():
+        linear_int8(x, w, ws, b, out=out)
+    assert torch.equal(out.detach(), linear_int8(x, w, ws, b))
