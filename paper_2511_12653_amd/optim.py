@@ -39,10 +39,10 @@ class _Plan:
     """A plan of the library with its workspace, and the tensors whose addresses it holds but the gradients: those are the
     program's to free when a step has been enqueued, and a plan is taken again only where they are at the same addresses."""
 
-    def __init__(self, key, params, held, device):
-        self.key, self.held = key, held
+    def __init__(self, key, params, values, copies, states, device):
+        self.key, self.held = key, (values, copies, states)
         # what a step writes and a program may have saved for a backward pass (inference tensors have no versions to count)
-        self.written = [t for of_one in held for t in of_one[:2] if t is not None and not t.is_inference()]
+        self.written = [t for t in (*values, *copies) if t is not None and not t.is_inference()]
         self.workspace = torch.empty(fq.fq_adamw_workspace_bytes(params), dtype=torch.uint8, device=device)
         self.handle = fq.fq_adamw_create(params, self.workspace)
         self.stream = torch.cuda.current_stream()
@@ -88,51 +88,67 @@ class AdamW(torch.optim.Optimizer):
             self.param_groups.pop()
             raise
 
-    def _state_of(self, p, group, made):
+    def _begin(self, p, group):
+        """Makes the state of a parameter in front of its first step."""
         state = self.state[p]
-        if not state:
-            made.append(p)
-            if group["step"]:
-                state["late"] = group["step"]       # steps of the group before its first
-            if group["states"] == "float8":
-                blocks = (p.numel() + 255) // 256
-                for name in ("m", "v"):
-                    state[name] = torch.zeros(p.shape, dtype=torch.float8_e4m3fn, device=p.device)
-                    state[name + "_scale"] = torch.zeros(blocks, device=p.device)
-            else:
-                for name in ("m", "v"):
-                    state[name] = torch.zeros(p.shape, device=p.device)
-        return state
+        if group["step"]:
+            state["late"] = group["step"]           # steps of the group before that
+        if group["states"] == "float8":
+            blocks = (p.numel() + 255) // 256
+            for name in ("m", "v"):
+                state[name] = torch.zeros(p.shape, dtype=torch.float8_e4m3fn, device=p.device)
+                state[name + "_scale"] = torch.zeros(blocks, device=p.device)
+        else:
+            for name in ("m", "v"):
+                state[name] = torch.zeros(p.shape, device=p.device)
 
     def _launches(self, index, group, grad_scale, made):
         """A launch for the parameters with a gradient, or, where some had their first one late, for those of each step number:
         [(plan, what fq_adamw_step takes, gradients)]."""
-        chosen = {}
-        for p, c in zip(group["params"], group["copies"] or [None] * len(group["params"])):
-            if p.grad is not None:
-                if p.grad.layout is not torch.strided:
-                    raise TypeError("gradients must be dense and contiguous")
-                state = self._state_of(p, group, made)
-                chosen.setdefault(state.get("late", 0), []).append((p, state, c))
+        params = group["params"]
+        columns = [params, [p.grad for p in params], group["copies"] or [None] * len(params)]
+        pick = lambda some: [[column[i] for i in some] for column in columns]      # noqa: E731
+        if any(g is None for g in columns[1]):
+            columns = pick([i for i, g in enumerate(columns[1]) if g is not None])
+            if not columns[0]:
+                return []
+        states = [self.state[p] for p in columns[0]]
+        if not all(states):
+            for p, state in zip(columns[0], states):
+                if not state:
+                    made.append(p)
+                    self._begin(p, group)
+        columns.append(states)
+        parts = {0: columns}
+        if any("late" in state for state in states):
+            places = {}
+            for i, state in enumerate(states):
+                places.setdefault(state.get("late", 0), []).append(i)
+            parts = {late: pick(some) for late, some in places.items()}
         beta1, beta2 = group["betas"]
-        return [(self._plan((index, late), group, some),
-                 fq.FqAdamW(group["lr"], beta1, beta2, group["eps"], group["step"] + 1 - late, group["seed"], grad_scale),
-                 [p.grad for p, _, _ in some]) for late, some in chosen.items()]
+        return [(self._plan((index, late), group["weight_decay"], *part),
+                 fq.FqAdamW(group["lr"], beta1, beta2, group["eps"], group["step"] + 1 - late, group["seed"], grad_scale), part[1])
+                for late, part in parts.items()]
 
-    def _plan(self, place, group, chosen):
-        tensors = [[t for name, t in s.items() if name != "late"] for _, s, _ in chosen]
+    def _plan(self, place, decay, params, grads, copies, states):
+        tensors = [t for state in states for t in state.values()]
+        if place[1]:
+            tensors = [t for t in tensors if torch.is_tensor(t)]
         # All that the plan's table is made of.  Gradients are often other tensors in every step: then it is made anew.
-        key = (group["weight_decay"],) + tuple(
-            (p.numel(), p.dtype, p.data_ptr(), p.grad.dtype, p.grad.stride(), p.grad.data_ptr(), c is not None and c.data_ptr())
-            + tuple(t.data_ptr() for t in ts) for (p, _, c), ts in zip(chosen, tensors))
+        try:
+            if not all(map(torch.Tensor.is_contiguous, grads)):
+                raise TypeError("gradients must be dense and contiguous")
+            key = (decay, *(list(map(torch.Tensor.data_ptr, ts)) for ts in (params, grads, tensors)), list(map(torch.Tensor.numel, params)),
+                   [p.dtype for p in params], [g.dtype for g in grads], [None if c is None else c.data_ptr() for c in copies])
+        except RuntimeError:
+            if all(g.layout is torch.strided for g in grads):
+                raise
+            raise TypeError("gradients must be dense and contiguous") from None
         plan = self._plans.get(place)
         if plan is None or plan.key != key:
-            if not all(p.grad.is_contiguous() for p, _, _ in chosen):
-                raise TypeError("gradients must be dense and contiguous")
-            params = [fq.FqParam.from_torch(p.detach(), p.grad, s["m"], s["v"], s.get("m_scale"), s.get("v_scale"), p16=c,
-                                            weight_decay=group["weight_decay"]) for p, s, c in chosen]
-            held = [(p.detach(), c, *ts) for (p, _, c), ts in zip(chosen, tensors)]
-            plan = self._plans[place] = _Plan(key, params, held, chosen[0][0].device)
+            lists = [fq.FqParam.from_torch(p.detach(), g, s["m"], s["v"], s.get("m_scale"), s.get("v_scale"), p16=c, weight_decay=decay)
+                     for p, g, c, s in zip(params, grads, copies, states)]
+            plan = self._plans[place] = _Plan(key, lists, [p.detach() for p in params], copies, tensors, params[0].device)
         return plan
 
     @torch.no_grad()
