@@ -71,3 +71,11 @@ def test_linear_int8_refuses_an_output_with_a_history():
     with torch.no_grad():
         linear_int8(x, w, ws, b, out=out)
     assert torch.equal(out.detach(), linear_int8(x, w, ws, b))
+
+
+def test_linear_int8_in_a_function_transform():
+    x, w, ws, b = operands()
+    with pytest.raises(RuntimeError):
+        torch.func.jvp(lambda t: linear_int8(t, w, ws, b), (x,), (torch.ones_like(x),))
+    with pytest.raises(RuntimeError):
+        torch.func.grad(lambda t: linear_int8(t, w, ws, b).sum())(x)
