@@ -5,6 +5,7 @@ Marshalling only.  The moments are float32, or float8_e4m3fn codes with a scale 
 of the memory, rounded stochastically).  There is no CPU path: CPU parameters raise.
 """
 import math
+import weakref
 
 import torch
 
@@ -45,6 +46,7 @@ class _Plan:
         self.written = [t for t in (*values, *copies) if t is not None and not t.is_inference()]
         self.workspace = torch.empty(fq.fq_adamw_workspace_bytes(params), dtype=torch.uint8, device=device)
         self.handle = fq.fq_adamw_create(params, self.workspace)
+        weakref.finalize(self, fq.fq_adamw_destroy, self.handle)       # (at the latest while the library is still there)
         self.stream = torch.cuda.current_stream()
 
     def used_here(self, gradients):
@@ -55,10 +57,6 @@ class _Plan:
         if stream != torch.cuda.default_stream():
             for g in gradients:                     # (nothing happens to one that is of this stream)
                 g.record_stream(stream)
-
-    def __del__(self):
-        if getattr(self, "handle", None):
-            fq.fq_adamw_destroy(self.handle)
 
 
 class AdamW(torch.optim.Optimizer):
