@@ -373,7 +373,8 @@ void fq_adamw_destroy(fq_adamw_plan *plan);
  * whole 16 bytes: what lies between two rows, and the rest of the 16 bytes in which the first begins and the last ends, may be
  * read and has no effect.  Fastest where the rows of x (FQ_I8) and w begin on 16-byte boundaries and k is a multiple of 16:
  * others are laid out anew in the workspace first (whose size therefore depends on the pointers), but with few tokens or
- * short rows.  One to three launches (for each part of 2^23 tokens, 2^26 channels or 16 GiB of codes to lay out anew).  The workspace need not be initialised and may be shared by calls that do not overlap in time.
+ * short rows.  One to three launches (for each part of 2^23 tokens, 2^26 channels or 16 GiB of codes to lay out anew).  The
+ * workspace need not be initialised and may be shared by calls that do not overlap in time.
  */
 typedef struct fq_linear {
     int64_t m, n, k;                  /* tokens, output channels, values per token; any may be 0; k <= 131071 */

@@ -9,7 +9,7 @@
 //
 // With FP32 states memory bounds it: 120 million elements 544 us, 6.2 TB/s.  In FP8 it is memory too where the elements have many
 // bytes (240 million, FP32 p, FP16 g and copy: 16 bytes each, 640 us, 6.0 TB/s), and arithmetic where they have few (20 million in FP16: 10
-// bytes each, 44 us, 4.5 TB/s).  Short lists cost the launch and a trip to memory or two (88 tensors, 0.4 million elements: 4.2 us).
+// bytes each, 43 to 45 us, 4.5 TB/s).  Short lists cost the launch and a trip to memory or two (88 tensors, 0.4 million elements: 4.2 us).
 #include <hip/hip_fp16.h>
 
 #include "fq_adamw.h"
@@ -170,7 +170,7 @@ __device__ __forceinline__ void step_rows(const AdamwTensor &t, const AdamwStep 
             continue;
         }
         // What bounds this is the arithmetic (about 75 instructions an element; with the compiler's root and quotient, a
-        // guard per element and four products to a hash it was 114: 20 million FP16 elements 53 us, now 43).
+        // guard per element and four products to a hash it was 114: 20 million FP16 elements 53 us, now 43 to 45).
         float m[4], v[4];
         unsigned both;
         auto moments = [&](bool guarded) {

@@ -204,9 +204,9 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(QuantizeArgs a, unsi
 // ---------------------------------------------------------------------------------------------
 // Product of a tile of BM tokens by BN channels.  What bounds it, by tile: 256 x 256 the matrix cores, which are busy 65 % of the
 // cycles at a clock that their power holds down (8192 x 8192 x 8192 460 us, 2.39 POP/s; codes that are all zero are 12 to 25 % faster);
-// the smaller ones, taken where large ones leave compute units without work, what a compute unit can load, 40 to 50 bytes a cycle (17
-// x 64 x 4096, a block or two in all: 16 KiB of a 64 x 64 step in 0.15 us, 32 KiB of a 128 x 128 step in 0.37).  More stages, and codes
-// read from LDS a whole step ahead, change neither (5 % either way).
+// the smaller ones, taken where large ones leave compute units without work, what a compute unit can move by itself: a 128 x 128 step, 32 KiB
+// from the L2s and 96 through LDS, takes 0.30 us with 32 or 64 blocks on the chip and 0.36 with 160 (the matrix cores work 0.21 of it), a 64 x 64
+// step of 16 KiB 0.15.  More stages, and codes read from LDS a whole step ahead, change neither (5 % either way).
 //
 // BM / WM by BN / WN of it belong to a wavefront, which builds them from
 // 32 x 32 matrix instructions: lane l holds 16 codes of channel l % 32 and of token l % 32, and of the sums those of token
@@ -971,7 +971,8 @@ int launch_quantize_rows(const QuantizeArgs &a, const AlignArgs &other, void *st
 // The tiles, and what a step of 128 codes of a block takes: at least `wait`, and `work` for each block that a compute unit
 // holds at once (`resident` of them at most); in us.  What is in front of the first step and behind the last takes kEnds and the time of the
 // blocks' parts of y at 5 TB/s (with few steps the most of it: 11707 x 9600 x 272 89 us in 256 x 256, 45 of them for y).  The tile
-// with the least sum is taken.  Measured, codes at aligned rows, us, the tiles in the order of the table (- : not in question):
+// with the least sum is taken.  (Sums are up to 1.5 times off, either way: 600 x 4096 x 4096 in 256 x 256 60 for 41, 20 x 16384 x 4096 in 32 x 64 7.8
+// for 12.5.  The tiles chosen below are the best or within 2 % of it.)  Measured, codes at aligned rows, us, the tiles in the order of the table (- : not in question):
 //   8192 x 8192 x 8192   461   483   565   582   856   1091
 //   2048 x 4096 x 4096  44.5  34.0  37.0  38.3  55.0   73.9
 //   19200 x 384 x 384   12.3   8.8   8.6  11.1  14.4   16.9

@@ -64,7 +64,8 @@ class AdamW(torch.optim.Optimizer):
 
     states: "float32" or "float8".  seed: of the stochastic rounding of float8 states.  A group may override lr, betas, eps,
     weight_decay and states, and may bring `copies`: one float16 tensor (or None) per float32 parameter, which receives
-    its new values.  Elements whose gradient is not finite are left as they are.  A group counts its steps; for a parameter whose
+    its new values.  Gradients may be float16 or float32 (torch gives a float32 parameter a float16 gradient only where its
+    grad_dtype says so).  Elements whose gradient is not finite are left as they are.  A group counts its steps; for a parameter whose
     first gradient comes later they count from that one on.  Steps in which it has none after that leave it as it is and do
     count.  A group in which no parameter has a gradient does not count the step, nor does any group count or make a step that is
     refused.
@@ -132,7 +133,8 @@ class AdamW(torch.optim.Optimizer):
         tensors = [t for state in states for t in state.values()]
         if place[1]:
             tensors = [t for t in tensors if torch.is_tensor(t)]
-        # All that the plan's table is made of.  Gradients are often other tensors in every step: then it is made anew.
+        # All that the plan's table is made of.  Gradients are often at other addresses in every step: then it is made anew (88 tensors:
+        # 400 to 670 us on the host; a plan that is taken again 73).
         try:
             if not all(map(torch.Tensor.is_contiguous, grads)):
                 raise TypeError("gradients must be dense and contiguous")

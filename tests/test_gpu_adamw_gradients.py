@@ -66,3 +66,22 @@ def test_a_gradient_outlives_a_step_on_another_stream():
     assert not side.query()                          # (or this has shown nothing)
     torch.cuda.current_stream().wait_stream(side)
     assert bool((p.detach() < -1.9e-2).all())
+
+
+@pytest.mark.parametrize("states", ["float32", "float8"])
+def test_half_gradients_of_float_parameters(states):
+    """What torch refuses until grad_dtype allows it; the same bits as with the gradients' values in FP32."""
+    torch.manual_seed(3)
+    start, g = torch.randn(900, device="cuda"), torch.randn(900, device="cuda", dtype=torch.float16)
+    ends = []
+    for dtype in (torch.float32, torch.float16):
+        p = torch.nn.Parameter(start.clone())
+        p.grad_dtype = dtype
+        copy = torch.zeros(900, device="cuda", dtype=torch.float16)
+        opt = AdamW([{"params": [p], "copies": [copy]}], lr=1e-2, states=states, seed=7)
+        for _ in range(3):
+            p.grad = g.to(dtype)
+            opt.step()
+        assert torch.equal(copy, p.detach().half())
+        ends.append(p.detach())
+    assert torch.equal(*ends)
