@@ -1,5 +1,5 @@
 """Torch front door to the multi-tensor AdamW step: `AdamW(params, ...)`, a torch.optim.Optimizer whose step() is one
-fq_adamw_step call (one launch) per parameter group.
+fq_adamw_step call (one launch) per parameter group, or for each step number in it where some had their first gradient late.
 
 Marshalling only.  The moments are float32, or float8_e4m3fn codes with a scale per 256 elements (`states="float8"`, a quarter
 of the memory, rounded stochastically).  There is no CPU path: CPU parameters raise.
