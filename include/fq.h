@@ -49,11 +49,12 @@ typedef enum fq_status {
     FQ_ERR_QRANGE = -4,        /* need qmin <= 0 <= qmax, qmin < qmax, |q| <= 32768; int8 codes need [-128,127] */
     FQ_ERR_ALIGN = -5,         /* pointer not aligned to its element size (workspace: 256 bytes) */
     FQ_ERR_WORKSPACE = -6,     /* workspace NULL or smaller than fq_workspace_bytes() */
-    FQ_ERR_SCALE_PARAMS = -7,  /* need finite eps, 0 < s_min <= s_max, no NaN */
+    FQ_ERR_SCALE_PARAMS = -7,  /* need finite eps, 0 < s_min <= s_max, no NaN; fq_norm: finite eps >= 0; fq_dropout: 0 <= p <= 1 */
     FQ_ERR_LAUNCH = -8,        /* the HIP runtime reported an error while enqueuing */
     FQ_ERR_ALIAS = -9,         /* output partially overlaps its input (exact in-place is allowed; q may not
                                   overlap x or y at all; nothing that fq_adamw or fq_linear writes may overlap
-                                  anything else of the same tensor or call) */
+                                  anything else of the same tensor or call; fq_norm, fq_dropout, fq_adapters: but
+                                  for the exact in-place that each names) */
     FQ_ERR_OPTIMIZER = -10     /* bad fq_adam or fq_adamw: step < 1, beta outside [0,1), lr/eps not finite or eps < 0;
                                   bad fq_param: lr_scale or weight_decay not finite */
 } fq_status;
@@ -61,7 +62,7 @@ typedef enum fq_status {
 typedef enum fq_dtype {
     FQ_F16 = 0,
     FQ_F32 = 1,
-    FQ_I8 = 2                  /* integer codes: the x of fq_linear only */
+    FQ_I8 = 2                  /* integer codes: the x of fq_linear and fq_adapters, the y of fq_norm */
 } fq_dtype;
 
 enum {
@@ -390,6 +391,101 @@ typedef struct fq_linear {
 } fq_linear;
 size_t fq_linear_workspace_bytes(const fq_linear *d);     /* 0 if d does not validate; host only */
 fq_status fq_linear_forward(const fq_linear *d, void *workspace, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Layer norm over rows of `width` values, forward and backward, and in a form that gives the codes that fq_linear takes:
+ * what stands in front of a quantized layer.
+ *   mean = (sum of x) / width,  rstd = 1 / sqrt((sum of (x - mean)^2) / width + eps),  h = (x - mean) * rstd
+ *   y = h * weight + bias
+ * The sums of a row are binary64; mean and rstd are rounded to binary32 once and the rest is binary32, but where y is
+ * codes (y_dtype FQ_I8): there y is worked out in binary64, rounded to binary32 once, and quantized as fq_linear
+ * quantizes FP32 rows:  ys = max|y| / 127,  code = clip(round(y / ys), -127, 127).
+ * A row with a NaN or an infinity gives a row of NaN (codes 0, scale NaN).  Where all values of a row are equal and eps is
+ * 0, rstd is infinite and the row NaN.
+ * The backward pass, with a = gy * weight, sums over the row, and h by the statistics that the forward pass gave:
+ *   gx = rstd * (a - (sum of a) / width - h * (sum of a*h) / width)
+ *   gweight = sum over rows of gy * h,  gbias = sum over rows of gy      (rounded to w_dtype once)
+ * No float atomics: sums are in a fixed order, results the same bit for bit from run to run.
+ * Rows may lie any distance apart and at any address that their type allows.  y may be exactly x, gx exactly x or gy (same
+ * type and distance).  Forward one launch, backward one or two (wide rows: three).  The workspace of the backward pass need not be initialised and may be
+ * shared by calls that do not overlap in time.
+ */
+typedef struct fq_norm {
+    int64_t rows, width;              /* any may be 0; width <= 2^24 */
+    int32_t x_dtype;                  /* FQ_F16 or FQ_F32: of x and gx */
+    int32_t y_dtype;                  /* FQ_F16, FQ_F32: of y and gy; FQ_I8 (forward only): codes */
+    int32_t w_dtype;                  /* FQ_F16 or FQ_F32: of weight, bias and their gradients */
+    float eps;                        /* finite, >= 0 */
+    int64_t ldx, ldy, ldgy, ldgx;     /* from a row to the next, in elements, >= width (of what is given) */
+    const void *x;                    /* in  [rows][ldx] */
+    const void *weight, *bias;        /* in  [width], optional: 1 and 0 */
+    void *y;                          /* out (forward) [rows][ldy] */
+    float *ys;                        /* out (forward), FQ_I8 only: [rows], the scales of the codes */
+    float *stats;                     /* [rows][2], mean and rstd: out (forward, optional), in (backward) */
+    const void *gy;                   /* in  (backward) [rows][ldgy] */
+    void *gx;                         /* out (backward), optional */
+    void *gweight, *gbias;            /* out (backward), optional: [width] */
+} fq_norm;
+fq_status fq_norm_forward(const fq_norm *d, void *hip_stream);
+size_t fq_norm_workspace_bytes(const fq_norm *d);         /* of the backward pass; 0 if d does not validate for it; host only */
+fq_status fq_norm_backward(const fq_norm *d, void *workspace, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Dropout whose mask is never stored, and the residual that its result is added to:
+ *   y_i = (keep_i ? x_i * scale : 0) + residual_i,    scale = 1 / (1 - p) in binary32 (p = 1: nothing is kept)
+ * in binary32, each operation rounded, and rounded to y's type once.  What is dropped does not count, whatever it is
+ * (a NaN, an infinity).  The backward pass is the same call on the gradient, without residual.
+ * keep_i is a hash of place i under two keys of seed and step; all products modulo 2^32 (k: 2^64), >> shifting in zeros:
+ *   k = seed*0x9E3779B97F4A7C15 + step*0xD1B54A32D192ED03 + (i >> 32)*0x8CB92BA72F3D8DD7
+ *   k = (k ^ (k >> 32))*0x9E3779B97F4A7C15;  k = (k ^ (k >> 29))*0xD1B54A32D192ED03
+ *   k0 = k >> 32;  k1 = (k ^ (k >> 32)) mod 2^32
+ *   h = (i mod 2^32)*0x9E3779B1 + k0;  h = (h ^ (h >> 16))*0x6A09E667;  h = ((h ^ (h >> 15)) + k1)*0xBB67AE85
+ *   keep_i = (h >> 1) >= round(p * 2^31)
+ * (k1 between the products: with one key the masks of two steps would be one sequence, shifted.)  One seed for a program, or a
+ * layer, and a new step for every call makes masks that have nothing to do with each other.  step_on_device lets a captured
+ * graph do that: the number there is added to step when the kernel runs.
+ */
+typedef struct fq_dropout_args {
+    int64_t n;                        /* elements, contiguous; may be 0; at most 2^35 */
+    int32_t x_dtype, y_dtype;         /* FQ_F16 or FQ_F32: of x; of y and residual */
+    double p;                         /* 0 <= p <= 1 */
+    uint64_t seed, step;
+    const uint64_t *step_on_device;   /* device pointer, optional */
+    const void *x;                    /* in */
+    const void *residual;             /* in, optional */
+    void *y;                          /* out; may be exactly x or residual (of the same type) */
+} fq_dropout_args;
+fq_status fq_dropout(const fq_dropout_args *d, void *hip_stream);
+
+/*
+ * Low-rank adapters of many requests beside a shared layer (that of fq_linear, whose codes are constants: what is special to a
+ * request is added to its output):
+ *   t[i][l] = (sum over j of x[i][j] * a[ids[i]][l][j]) (* xs[i]),   l < rank
+ *   y[i][j] = base[i][j] + scale[ids[i]] * (sum over l of t[i][l] * b[ids[i]][j][l])
+ * All sums and t are binary32 or better, y is rounded to its type once.  Tokens come in any order; ids outside [0, count)
+ * mean no adapter (y = base).  A token's NaN or infinity stays in its row, an adapter's with its tokens.
+ * Rows of x, base and y may lie any distance apart and at any address that their type allows; a and b are contiguous.
+ * y may be exactly base (same type and distance).  Two launches.  The workspace need not be initialised and may be shared by
+ * calls that do not overlap in time.  There is no backward pass.
+ */
+typedef struct fq_adapters {
+    int64_t m, n, k;                  /* tokens, output channels, values per token; any may be 0; k and n <= 2^20 */
+    int64_t count, rank;              /* adapters; rank of each, at most 256; any may be 0 */
+    int32_t x_dtype;                  /* FQ_F16, FQ_F32, or FQ_I8: codes with their scales */
+    int32_t y_dtype, base_dtype;      /* FQ_F16 or FQ_F32 */
+    int32_t xs_step;                  /* 1: a scale per token; 0: one scale for all (FQ_I8 only) */
+    int64_t ldx, ldy, ldbase;         /* >= k, n, n */
+    const void *x;                    /* in  [m][ldx] */
+    const float *xs;                  /* in, FQ_I8 only */
+    const int32_t *ids;               /* in  [m]: each token's adapter */
+    const void *a;                    /* in  [count][rank][k], FP16 */
+    const void *b;                    /* in  [count][n][rank], FP16 */
+    const float *scale;               /* in, optional: [count]; 1 without */
+    const void *base;                 /* in, optional: [m][ldbase]; 0 without */
+    void *y;                          /* out [m][ldy] */
+} fq_adapters;
+size_t fq_adapters_workspace_bytes(const fq_adapters *d); /* 0 if d does not validate; host only */
+fq_status fq_adapters_forward(const fq_adapters *d, void *workspace, size_t ws_bytes, void *hip_stream);
 
 /*
  * Measurement aid, not part of the operation: a streaming kernel without arithmetic in the launch

@@ -260,6 +260,157 @@ class FqLinear(ctypes.Structure):
         return self
 
 
+def _pitch(t):
+    """From a row of a matrix to the next, in elements."""
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("the values of a row must be contiguous")
+    if rows <= 1:
+        return cols
+    if t.stride(0) < cols:
+        raise ValueError("rows must not overlap")
+    return t.stride(0)
+
+
+def _pointer(t):
+    return None if t is None else t.data_ptr()
+
+
+class FqNorm(ctypes.Structure):
+    """Mirror of `struct fq_norm` (host struct; the pointers inside are device pointers)."""
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int64),
+                ("x_dtype", ctypes.c_int32), ("y_dtype", ctypes.c_int32), ("w_dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("ldx", ctypes.c_int64), ("ldy", ctypes.c_int64), ("ldgy", ctypes.c_int64), ("ldgx", ctypes.c_int64),
+                ("x", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("y", ctypes.c_void_p),
+                ("ys", ctypes.c_void_p), ("stats", ctypes.c_void_p), ("gy", ctypes.c_void_p), ("gx", ctypes.c_void_p),
+                ("gweight", ctypes.c_void_p), ("gbias", ctypes.c_void_p)]
+
+    @classmethod
+    def from_torch(cls, x, y=None, weight=None, bias=None, y_scale=None, stats=None, gy=None, gx=None, gweight=None, gbias=None,
+                   eps=1e-5):
+        """x, y, gy, gx: [rows, width], whose rows may lie any distance apart; x and gx float16 or float32, gy and y either or
+        (y) int8, then with y_scale (rows float32).  weight, bias and their gradients: width values of one type, float16 or
+        float32.  stats: [rows, 2] float32."""
+        import torch
+        types = {torch.float16: FQ_F16, torch.float32: FQ_F32, torch.int8: FQ_I8}
+        values = (torch.float16, torch.float32)
+        if x.dtype not in values or (gx is not None and gx.dtype != x.dtype):
+            raise TypeError("x must be float16 or float32, and gx of its type")
+        out = y if y is not None else gy
+        if out is None:
+            raise ValueError("y or gy is needed")
+        if out.dtype not in types or (gy is not None and gy.dtype not in values):
+            raise TypeError("y must be float16, float32 or int8, gy float16 or float32")
+        if y is not None and gy is not None and y.dtype != gy.dtype:
+            raise TypeError("gy must be of y's type")
+        for t in (x, y, gy, gx):
+            if t is not None and (t.dim() != 2 or t.shape != x.shape):
+                raise ValueError("x, y, gy and gx must be matrices of one shape")
+        rows, width = x.shape
+        if (y is not None and y.dtype == torch.int8) != (y_scale is not None):
+            raise ValueError("y_scale belongs to int8 codes, and to nothing else")
+        kinds = {t.dtype for t in (weight, bias, gweight, gbias) if t is not None}
+        if len(kinds) > 1 or not kinds <= set(values):
+            raise TypeError("weight, bias and their gradients must be of one type, float16 or float32")
+        for t, count, name in ((weight, width, "weight"), (bias, width, "bias"), (gweight, width, "gweight"), (gbias, width, "gbias"),
+                               (y_scale, rows, "y_scale"), (stats, 2 * rows, "stats")):
+            if t is None:
+                continue
+            if t.numel() != count:
+                raise ValueError("%s has %d values, want %d" % (name, t.numel(), count))
+            if not t.is_contiguous() or (t.dtype != torch.float32 and (t is y_scale or t is stats)):
+                raise TypeError("%s must be contiguous%s" % (name, " float32" if t is y_scale or t is stats else ""))
+        given = (x, y, weight, bias, y_scale, stats, gy, gx, gweight, gbias)
+        _device_of(given)
+        pitch = lambda t: width if t is None else _pitch(t)     # noqa: E731
+        self = cls(rows, width, types[x.dtype], types[out.dtype], types[kinds.pop()] if kinds else FQ_F32, eps, pitch(x), pitch(y),
+                   pitch(gy), pitch(gx), _pointer(x), _pointer(weight), _pointer(bias), _pointer(y), _pointer(y_scale),
+                   _pointer(stats), _pointer(gy), _pointer(gx), _pointer(gweight), _pointer(gbias))
+        self._keep = given
+        return self
+
+
+class FqDropout(ctypes.Structure):
+    """Mirror of `struct fq_dropout_args` (host struct); change step in place from call to call."""
+    _fields_ = [("n", ctypes.c_int64), ("x_dtype", ctypes.c_int32), ("y_dtype", ctypes.c_int32), ("p", ctypes.c_double),
+                ("seed", ctypes.c_uint64), ("step", ctypes.c_uint64), ("step_on_device", ctypes.c_void_p),
+                ("x", ctypes.c_void_p), ("residual", ctypes.c_void_p), ("y", ctypes.c_void_p)]
+
+    @classmethod
+    def from_torch(cls, x, y, p, seed, step=0, residual=None, step_on_device=None):
+        """x, y, residual: contiguous tensors of as many values, float16 or float32 (residual of y's type); step_on_device: one
+        int64 on the GPU, or None."""
+        import torch
+        types = {torch.float16: FQ_F16, torch.float32: FQ_F32}
+        if x.dtype not in types or y.dtype not in types or (residual is not None and residual.dtype != y.dtype):
+            raise TypeError("x and y must be float16 or float32, and residual of y's type")
+        for t in (y, residual):
+            if t is not None and t.numel() != x.numel():
+                raise ValueError("tensor has %d elements, x has %d" % (t.numel(), x.numel()))
+        if step_on_device is not None and (step_on_device.dtype != torch.int64 or step_on_device.numel() != 1):
+            raise TypeError("step_on_device must be one int64")
+        if not (0 <= seed < 1 << 64 and 0 <= step < 1 << 64):
+            raise ValueError("seed and step must be whole numbers of 64 bits")
+        given = (x, y, residual, step_on_device)
+        _device_of(given)
+        if any(t is not None and not t.is_contiguous() for t in given):
+            raise ValueError("tensors must be contiguous")
+        self = cls(x.numel(), types[x.dtype], types[y.dtype], p, seed, step, _pointer(step_on_device), _pointer(x),
+                   _pointer(residual), _pointer(y))
+        self._keep = given
+        return self
+
+
+class FqAdapters(ctypes.Structure):
+    """Mirror of `struct fq_adapters` (host struct; the pointers inside are device pointers)."""
+    _fields_ = [("m", ctypes.c_int64), ("n", ctypes.c_int64), ("k", ctypes.c_int64), ("count", ctypes.c_int64),
+                ("rank", ctypes.c_int64), ("x_dtype", ctypes.c_int32), ("y_dtype", ctypes.c_int32),
+                ("base_dtype", ctypes.c_int32), ("xs_step", ctypes.c_int32),
+                ("ldx", ctypes.c_int64), ("ldy", ctypes.c_int64), ("ldbase", ctypes.c_int64),
+                ("x", ctypes.c_void_p), ("xs", ctypes.c_void_p), ("ids", ctypes.c_void_p), ("a", ctypes.c_void_p),
+                ("b", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("base", ctypes.c_void_p), ("y", ctypes.c_void_p)]
+
+    @classmethod
+    def from_torch(cls, x, ids, a, b, y, base=None, scale=None, x_scale=None):
+        """x [m, k] float16, float32 or int8 (then with x_scale, m float32 values or one), base and y [m, n] float16 or float32,
+        whose rows may lie any distance apart; ids: m int32; a [count, rank, k], b [count, n, rank]: contiguous float16;
+        scale: count float32 values."""
+        import torch
+        types = {torch.float16: FQ_F16, torch.float32: FQ_F32, torch.int8: FQ_I8}
+        values = (torch.float16, torch.float32)
+        if x.dtype not in types or y.dtype not in values or (base is not None and base.dtype not in values):
+            raise TypeError("x must be float16, float32 or int8, y and base float16 or float32")
+        if a.dtype != torch.float16 or b.dtype != torch.float16 or ids.dtype != torch.int32:
+            raise TypeError("a and b must be float16, ids int32")
+        if x.dim() != 2 or y.dim() != 2 or a.dim() != 3 or b.dim() != 3:
+            raise ValueError("x and y must have two dimensions, a and b three")
+        (m, k), (count, rank, _) = x.shape, a.shape
+        n = y.shape[1]
+        if tuple(y.shape) != (m, n) or tuple(a.shape) != (count, rank, k) or tuple(b.shape) != (count, n, rank) or (
+                base is not None and tuple(base.shape) != (m, n)):
+            raise ValueError("x %s, a %s, b %s, y %s and base do not fit" % tuple(tuple(t.shape) for t in (x, a, b, y)))
+        if (x.dtype == torch.int8) != (x_scale is not None):
+            raise ValueError("x_scale belongs to int8 codes, and to nothing else")
+        for t, name in ((ids, "ids"), (a, "a"), (b, "b"), (scale, "scale"), (x_scale, "x_scale")):
+            if t is not None and not t.is_contiguous():
+                raise ValueError("%s must be contiguous" % name)
+        for t, size, name in ((ids, m, "ids"), (scale, count, "scale"), (x_scale, m, "x_scale")):
+            if t is None:
+                continue
+            if t.numel() != size and (t.numel() != 1 or t is not x_scale):
+                raise ValueError("%s has %d values, want %d" % (name, t.numel(), size))
+            if t is not ids and t.dtype != torch.float32:
+                raise TypeError("%s must be float32" % name)
+        given = (x, ids, a, b, y, base, scale, x_scale)
+        _device_of(given)
+        self = cls(m, n, k, count, rank, types[x.dtype], types[y.dtype], FQ_F16 if base is None else types[base.dtype],
+                   0 if x_scale is None or (x_scale.numel() == 1 and m != 1) else 1, _pitch(x), _pitch(y),
+                   n if base is None else _pitch(base), _pointer(x), _pointer(x_scale), _pointer(ids), _pointer(a), _pointer(b),
+                   _pointer(scale), _pointer(base), _pointer(y))
+        self._keep = given
+        return self
+
+
 class FqLayoutInfo(ctypes.Structure):
     """Mirror of `struct fq_layout_info`."""
     _fields_ = [("blocks", ctypes.c_int64), ("units_per_channel", ctypes.c_int64),
@@ -320,6 +471,18 @@ _lib.fq_linear_workspace_bytes.argtypes = [ctypes.POINTER(FqLinear)]
 _lib.fq_linear_workspace_bytes.restype = ctypes.c_size_t
 _lib.fq_linear_forward.argtypes = [ctypes.POINTER(FqLinear), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
 _lib.fq_linear_forward.restype = ctypes.c_int
+_lib.fq_norm_forward.argtypes = [ctypes.POINTER(FqNorm), ctypes.c_void_p]
+_lib.fq_norm_forward.restype = ctypes.c_int
+_lib.fq_norm_workspace_bytes.argtypes = [ctypes.POINTER(FqNorm)]
+_lib.fq_norm_workspace_bytes.restype = ctypes.c_size_t
+_lib.fq_norm_backward.argtypes = [ctypes.POINTER(FqNorm), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+_lib.fq_norm_backward.restype = ctypes.c_int
+_lib.fq_dropout.argtypes = [ctypes.POINTER(FqDropout), ctypes.c_void_p]
+_lib.fq_dropout.restype = ctypes.c_int
+_lib.fq_adapters_workspace_bytes.argtypes = [ctypes.POINTER(FqAdapters)]
+_lib.fq_adapters_workspace_bytes.restype = ctypes.c_size_t
+_lib.fq_adapters_forward.argtypes = [ctypes.POINTER(FqAdapters), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+_lib.fq_adapters_forward.restype = ctypes.c_int
 _lib.fq_layout.argtypes = [ctypes.POINTER(FqTensor), ctypes.POINTER(FqLayoutInfo)]
 _lib.fq_layout.restype = ctypes.c_int
 _lib.fq_status_string.argtypes = [ctypes.c_int]
@@ -399,7 +562,7 @@ def _native(function):
 
 
 if _fqcall:
-    _fqcall.setup(FqTensor, FqDistill, ctypes.c_void_p, _check, FqLinear, FqAdamW)
+    _fqcall.setup(FqTensor, FqDistill, ctypes.c_void_p, _check, FqLinear, FqAdamW, FqNorm, FqDropout, FqAdapters)
 
 
 def fq_status_string(status) -> str:
@@ -527,6 +690,36 @@ def fq_linear_workspace_bytes(d: FqLinear) -> int:
 def fq_linear_forward(d: FqLinear, workspace, stream=None):
     p, nbytes = _ws(workspace)
     _check(_lib.fq_linear_forward(ctypes.byref(d), p, nbytes, _stream(stream)))
+
+
+@_native
+def fq_norm_forward(d: FqNorm, stream=None):
+    _check(_lib.fq_norm_forward(ctypes.byref(d), _stream(stream)))
+
+
+def fq_norm_workspace_bytes(d: FqNorm) -> int:
+    return int(_lib.fq_norm_workspace_bytes(ctypes.byref(d)))
+
+
+@_native
+def fq_norm_backward(d: FqNorm, workspace, stream=None):
+    p, nbytes = _ws(workspace)
+    _check(_lib.fq_norm_backward(ctypes.byref(d), p, nbytes, _stream(stream)))
+
+
+@_native
+def fq_dropout(d: FqDropout, stream=None):
+    _check(_lib.fq_dropout(ctypes.byref(d), _stream(stream)))
+
+
+def fq_adapters_workspace_bytes(d: FqAdapters) -> int:
+    return int(_lib.fq_adapters_workspace_bytes(ctypes.byref(d)))
+
+
+@_native
+def fq_adapters_forward(d: FqAdapters, workspace, stream=None):
+    p, nbytes = _ws(workspace)
+    _check(_lib.fq_adapters_forward(ctypes.byref(d), p, nbytes, _stream(stream)))
 
 
 def fq_probe_stream(inputs, a, b, out, nbytes, stream=None):

@@ -20,11 +20,14 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfq.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("fq_kernels.hip", "fq_distill.hip", "fq_adamw.hip", "fq_linear.hip",
-                                               "fq_api.cpp", "fq_adamw_api.cpp", "fq_linear_api.cpp")]
+                                               "fq_norm.hip", "fq_dropout.hip", "fq_adapters.hip",
+                                               "fq_api.cpp", "fq_adamw_api.cpp", "fq_linear_api.cpp", "fq_norm_api.cpp",
+                                               "fq_dropout_api.cpp", "fq_adapters_api.cpp")]
 CALL_SOURCE = os.path.join(CSRC, "fq_call.c")
 CALL = os.path.join(HERE, "_fqcall" + sysconfig.get_config_var("EXT_SUFFIX"))
 CC = os.environ.get("CC", "gcc")
-HEADERS = [os.path.join(CSRC, f) for f in ("fq_internal.h", "fq_device.h", "fq_adamw.h", "fq_linear.h")] + [
+HEADERS = [os.path.join(CSRC, f) for f in ("fq_internal.h", "fq_device.h", "fq_adamw.h", "fq_linear.h", "fq_norm.h", "fq_dropout.h",
+                                            "fq_adapters.h", "fq_rows.h", "fq_extent.h")] + [
     os.path.join(HERE, "..", "include", "fq.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-ffp-contract=off",

@@ -3,7 +3,7 @@
  * counterpart in binding.py takes; it recognises the forms below and leaves every other one, and every error, to
  * that counterpart, which `wrap` hands over.
  *
- *   descriptor   FqTensor / FqDistill / FqLinear / FqAdamW itself (not a subclass)
+ *   descriptor   FqTensor / FqDistill / FqLinear / FqAdamW / FqNorm / FqDropout / FqAdapters itself (not a subclass)
  *   plan         ctypes.c_void_p
  *   workspace    torch.Tensor itself, or a tuple of two ints
  *   stream       left out: torch's current stream, once binding.py has given its lookups (`streams`)
@@ -16,12 +16,14 @@
 
 #include "../../include/fq.h"
 
-enum { FORWARD, BACKWARD, PLAN_RUN, PLAN_RUN_ADAM, DISTILL, LAYOUT_BYTES, LINEAR, ADAMW_STEP, CALLS };
+enum { FORWARD, BACKWARD, PLAN_RUN, PLAN_RUN_ADAM, DISTILL, LAYOUT_BYTES, LINEAR, ADAMW_STEP, NORM_FORWARD, NORM_BACKWARD, DROPOUT,
+       ADAPTERS, CALLS };
 static const char *const names[CALLS] = {"fq_forward", "fq_backward", "fq_plan_run", "fq_plan_run_adam", "fq_distill_loss",
-                                         "fq_workspace_bytes", "fq_linear_forward", "fq_adamw_step"};
+                                         "fq_workspace_bytes", "fq_linear_forward", "fq_adamw_step", "fq_norm_forward", "fq_norm_backward",
+                                         "fq_dropout", "fq_adapters_forward"};
 
 static PyObject *python_form[CALLS];                     /* the counterparts */
-static PyObject *tensor_type, *distill_type, *pointer_type, *check, *linear_type, *adamw_type;
+static PyObject *tensor_type, *distill_type, *pointer_type, *check, *linear_type, *adamw_type, *norm_type, *dropout_type, *adapters_type;
 static PyObject *raw_stream, *current_device, *torch_tensor;
 static PyObject *str_data_ptr, *str_numel, *str_element_size;
 
@@ -187,6 +189,45 @@ static PyObject *call_adamw_step(PyObject *self, PyObject *const *args, Py_ssize
     return done(status);
 }
 
+/* A call with a descriptor alone, and one with a workspace, too. */
+#define CALL_OF_DESCRIPTOR(function, CALL, type, struct_name)                                                          \
+    static PyObject *call_##function(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)       \
+    {                                                                                                                  \
+        (void)self;                                                                                                    \
+        if (nargs != 1 || kwnames || !raw_stream || !type || !is_a(args[0], type)) return to_python(CALL, args, nargs, kwnames); \
+        const struct_name *d = memory_of(args[0]);                                                                     \
+        void *stream;                                                                                                  \
+        fq_status status;                                                                                              \
+        if (!d || current_stream(&stream)) return NULL;                                                                \
+        Py_BEGIN_ALLOW_THREADS                                                                                         \
+        status = function(d, stream);                                                                                  \
+        Py_END_ALLOW_THREADS                                                                                           \
+        return done(status);                                                                                           \
+    }
+#define CALL_WITH_WORKSPACE(function, CALL, type, struct_name)                                                         \
+    static PyObject *call_##function(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)       \
+    {                                                                                                                  \
+        (void)self;                                                                                                    \
+        if (nargs != 2 || kwnames || !raw_stream || !type || !is_a(args[0], type) || !is_workspace(args[1]))           \
+            return to_python(CALL, args, nargs, kwnames);                                                              \
+        const struct_name *d = memory_of(args[0]);                                                                     \
+        void *stream, *ws;                                                                                             \
+        size_t bytes;                                                                                                  \
+        fq_status status;                                                                                              \
+        if (!d) return NULL;                                                                                           \
+        const int left = workspace(args[1], &ws, &bytes);                                                              \
+        if (left > 0) return to_python(CALL, args, nargs, kwnames);                                                    \
+        if (left || current_stream(&stream)) return NULL;                                                              \
+        Py_BEGIN_ALLOW_THREADS                                                                                         \
+        status = function(d, ws, bytes, stream);                                                                       \
+        Py_END_ALLOW_THREADS                                                                                           \
+        return done(status);                                                                                           \
+    }
+CALL_OF_DESCRIPTOR(fq_norm_forward, NORM_FORWARD, norm_type, fq_norm)
+CALL_WITH_WORKSPACE(fq_norm_backward, NORM_BACKWARD, norm_type, fq_norm)
+CALL_OF_DESCRIPTOR(fq_dropout, DROPOUT, dropout_type, fq_dropout_args)
+CALL_WITH_WORKSPACE(fq_adapters_forward, ADAPTERS, adapters_type, fq_adapters)
+
 static PyObject *call_plan_run(PyObject *self, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames)
 {
     (void)self;
@@ -244,15 +285,18 @@ static void keep(PyObject **slot, PyObject *value)
 
 static PyObject *setup(PyObject *self, PyObject *args)
 {
-    PyObject *t, *d, *p, *c, *l = NULL, *a = NULL;
+    PyObject *t, *d, *p, *c, *l = NULL, *a = NULL, *n = NULL, *o = NULL, *r = NULL;
     (void)self;
-    if (!PyArg_ParseTuple(args, "OOOO|OO", &t, &d, &p, &c, &l, &a)) return NULL;
+    if (!PyArg_ParseTuple(args, "OOOO|OOOOO", &t, &d, &p, &c, &l, &a, &n, &o, &r)) return NULL;
     keep(&tensor_type, t);
     keep(&distill_type, d);
     keep(&pointer_type, p);
     keep(&check, c);
     keep(&linear_type, l);
     keep(&adamw_type, a);
+    keep(&norm_type, n);
+    keep(&dropout_type, o);
+    keep(&adapters_type, r);
     Py_RETURN_NONE;
 }
 
@@ -293,7 +337,12 @@ static PyMethodDef methods[] = {
     {"fq_workspace_bytes", FAST(call_workspace_bytes), "fq_workspace_bytes(tensors, mode)\n--\n\n"},
     {"fq_linear_forward", FAST(call_linear), "fq_linear_forward(d, workspace, stream=None)\n--\n\n"},
     {"fq_adamw_step", FAST(call_adamw_step), "fq_adamw_step(plan, h, stream=None)\n--\n\n"},
-    {"setup", setup, METH_VARARGS, "setup(FqTensor, FqDistill, c_void_p, check, FqLinear=None, FqAdamW=None)\n--\n\n"},
+    {"fq_norm_forward", FAST(call_fq_norm_forward), "fq_norm_forward(d, stream=None)\n--\n\n"},
+    {"fq_norm_backward", FAST(call_fq_norm_backward), "fq_norm_backward(d, workspace, stream=None)\n--\n\n"},
+    {"fq_dropout", FAST(call_fq_dropout), "fq_dropout(d, stream=None)\n--\n\n"},
+    {"fq_adapters_forward", FAST(call_fq_adapters_forward), "fq_adapters_forward(d, workspace, stream=None)\n--\n\n"},
+    {"setup", setup, METH_VARARGS,
+     "setup(FqTensor, FqDistill, c_void_p, check, FqLinear=None, FqAdamW=None, FqNorm=None, FqDropout=None, FqAdapters=None)\n--\n\n"},
     {"streams", streams, METH_VARARGS, "streams(raw, device, Tensor)\n--\n\n"},
     {"wrap", wrap, METH_O, "wrap(function)\n--\n\nThe native form of the binding's function, which takes what that one leaves to it."},
     {NULL, NULL, 0, NULL}};

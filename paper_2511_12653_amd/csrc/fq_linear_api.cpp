@@ -2,6 +2,7 @@
 #include <cstring>
 
 #include "../../include/fq.h"
+#include "fq_extent.h"
 #include "fq_linear.h"
 
 namespace fq {
@@ -11,31 +12,6 @@ constexpr size_t kAlign = 256;
 // What a launch takes, so that its grid has less than 2^32 threads: rows of x, up to 256 threads to one; channels, 512 to 16 of them;
 // bytes of codes that are laid out anew, of x and w each, a thread to 16.
 constexpr long long kMostRows = 1LL << 23, kMostChannels = 1LL << 26, kMostCodes = 1LL << 34;
-
-size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-
-bool aligned(const void *p, size_t a) { return (uintptr_t)p % a == 0; }
-
-size_t size_of(int32_t dtype) { return dtype == FQ_I8 ? 1 : dtype == FQ_F16 ? 2 : 4; }
-
-// Rows of a matrix in memory: bytes of one, from one to the next, and how many.
-struct Rows {
-    uintptr_t at;
-    size_t width, pitch, count;
-    size_t span() const { return count ? (count - 1) * pitch + width : 0; }
-};
-
-// Whether two matrices share memory.  Columns of one buffer (equal pitches, rows that fall into each other's gaps) do not.
-bool overlap(const Rows &a, const Rows &b)
-{
-    if (!a.at || !b.at || !a.width || !b.width || !a.count || !b.count) return false;
-    if (a.at >= b.at + b.span() || b.at >= a.at + a.span()) return false;
-    if (a.pitch == b.pitch) {
-        const size_t off = a.at <= b.at ? (b.at - a.at) % a.pitch : (a.pitch - (a.at - b.at) % a.pitch) % a.pitch;
-        if (off >= a.width && off + b.width <= a.pitch) return false;
-    }
-    return true;
-}
 
 // Whether the tiles take rows of codes as they lie.
 bool fits(const void *p, long long ld, long long k)
@@ -62,11 +38,6 @@ Workspace workspace_of(const fq_linear &d)
     if (!fits(d.w, d.ldw, d.k)) end += round_up((size_t)d.n * (size_t)at.pitch, kAlign);
     if (end > at.bytes) at.bytes = end;
     return at;
-}
-
-bool pitch_fits(long long rows, long long pitch, long long width)
-{
-    return pitch >= width && pitch <= (1LL << 56) / (rows > 0 ? rows : 1);
 }
 
 fq_status validate(const fq_linear &d)
