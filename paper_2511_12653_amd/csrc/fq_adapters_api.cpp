@@ -4,19 +4,14 @@
 #include "../../include/fq.h"
 #include "fq_adapters.h"
 #include "fq_extent.h"
+#include "fq_internal.h"
 
 namespace fq {
 namespace {
 
 constexpr size_t kAlign = 256;
-constexpr long long kMostBlocks = 1LL << 22;     // of a launch, each at least 256 channels of a token
-
-// Tokens of a launch.
-long long tokens_of(const fq_adapters &d)
-{
-    const long long strips = (d.n + 255) / 256, most = kMostBlocks / (strips > 0 ? strips : 1);
-    return d.m < most ? d.m : most;
-}
+constexpr long long kDownBlocks = 4 * kComputeUnits, kMostSplits = 32;     // blocks that x a^T is cut into, about
+constexpr long long kUpWaves = 4 * kComputeUnits, kUpBlocks = 8 * kComputeUnits;
 
 fq_status validate(const fq_adapters &d)
 {
@@ -45,19 +40,60 @@ fq_status validate(const fq_adapters &d)
     return FQ_OK;
 }
 
-size_t workspace_of(const fq_adapters &d)
-{
-    const size_t bytes = round_up((size_t)tokens_of(d) * (size_t)d.rank * sizeof(float), kAlign);
-    return d.n > 0 && bytes > kAlign ? bytes : kAlign;
-}
+long long at_most(long long v, long long most) { return v < most ? v : most; }
+long long at_least(long long v, long long least) { return v > least ? v : least; }
+long long ceiling(long long v, long long by) { return (v + by - 1) / by; }
 
-AdapterArgs args_of(const fq_adapters &d, void *workspace)
+// How m tokens of the call are cut up.
+AdapterArgs plan_of(const fq_adapters &d, long long m)
 {
     AdapterArgs a;
     std::memset(&a, 0, sizeof a);
-    a.ids = d.ids; a.a = d.a; a.b = d.b; a.scale = d.scale; a.t = (float *)workspace;
+    a.m = (int)m; a.n = (int)d.n; a.k = (int)d.k; a.count = d.rank > 0 ? (int)d.count : 0; a.rank = (int)d.rank;
+    a.pitch = (int)ceiling(d.rank, 16) * 16;
+    a.chunks = (int)ceiling(d.rank, 64);
+    a.token_tiles = m >= 32LL * a.count && d.rank <= 192 ? 4 : 1;        // (t of 64 tokens and 192 ranks: 51 KB of LDS)
+    const long long tile = 16 * a.token_tiles, some = at_most(a.count + 1LL, m);
+    a.grouped = m > kWindow && a.count > 0 && a.count <= kMostGrouped;
+    a.tiles_most = (int)(a.grouped ? m / tile + some : ceiling(m, kWindow) * at_most(m, kWindow));
+    const long long tiles = at_least(m / tile + at_most(a.count, m), 1) * at_least(a.chunks, 1);
+    // a block takes 256 values of k at a time
+    a.splits = (int)at_least(at_most(at_most(kDownBlocks / tiles, ceiling(d.k, 256)), kMostSplits), 1);
+    a.wide = tiles * ceiling(d.n, 64) > kUpWaves ? 4 : 1;
+    const long long strips = ceiling(d.n, 64 * a.wide);          // that a block of four wavefronts takes at a time
+    a.groups = (int)at_least(at_most(strips, ceiling(kUpBlocks, a.tiles_most)), 1);
+    return a;
+}
+
+struct Workspace {
+    size_t order = 0, tiles = 0, t = 0, bytes = kAlign;
+};
+
+Workspace workspace_of(const fq_adapters &d)
+{
+    Workspace at;
+    if (d.m == 0 || d.n == 0 || d.count == 0 || d.rank == 0) return at;
+    const AdapterArgs a = plan_of(d, at_most(d.m, kAdaptersMostTokens));
+    at.tiles = round_up((size_t)a.m * sizeof(int), kAlign);
+    // (the last tokens of a call may come in a launch of fewer, in smaller tiles; calls of several launches do not cut up k)
+    at.t = at.tiles + round_up((size_t)(a.grouped ? a.m / 16 + at_most(a.count + 1LL, a.m) : 0) * sizeof(AdapterTile) + sizeof(int), kAlign);
+    at.bytes = at.t + round_up((size_t)a.m * (size_t)a.pitch * sizeof(float) * (size_t)(d.m > kAdaptersMostTokens ? 1 : a.splits), kAlign);
+    return at;
+}
+
+AdapterArgs args_of(const fq_adapters &d, long long m, void *workspace)
+{
+    AdapterArgs a = plan_of(d, m);
+    const Workspace at = workspace_of(d);
+    if (d.m > kAdaptersMostTokens) a.splits = 1;
+    char *const ws = (char *)workspace;
+    if (a.count > 0) {
+        a.order = (int *)(ws + at.order);
+        a.tiles = (AdapterTile *)(ws + at.tiles);
+        a.t = (float *)(ws + at.t);
+    }
+    a.a = d.a; a.b = d.b; a.scale = d.scale;
     a.ldx = d.ldx; a.ldy = d.ldy; a.ldbase = d.ldbase;
-    a.n = (int)d.n; a.k = (int)d.k; a.count = d.rank > 0 ? (int)d.count : 0; a.rank = (int)d.rank;
     a.xs_step = d.xs_step; a.x_type = d.x_dtype; a.y16 = d.y_dtype == FQ_F16; a.base16 = d.base_dtype == FQ_F16;
     return a;
 }
@@ -69,7 +105,7 @@ extern "C" {
 
 size_t fq_adapters_workspace_bytes(const fq_adapters *d)
 {
-    return d && fq::validate(*d) == FQ_OK ? fq::workspace_of(*d) : 0;
+    return d && fq::validate(*d) == FQ_OK ? fq::workspace_of(*d).bytes : 0;
 }
 
 fq_status fq_adapters_forward(const fq_adapters *d, void *workspace, size_t ws_bytes, void *hip_stream)
@@ -77,12 +113,10 @@ fq_status fq_adapters_forward(const fq_adapters *d, void *workspace, size_t ws_b
     if (!d) return FQ_ERR_NULL;
     const fq_status st = fq::validate(*d);
     if (st != FQ_OK || d->m == 0 || d->n == 0) return st;
-    if (!workspace || ws_bytes < fq::workspace_of(*d)) return FQ_ERR_WORKSPACE;
+    if (!workspace || ws_bytes < fq::workspace_of(*d).bytes) return FQ_ERR_WORKSPACE;
     if (!fq::aligned(workspace, fq::kAlign)) return FQ_ERR_ALIGN;
-    fq::AdapterArgs a = fq::args_of(*d, workspace);
-    const long long tokens = fq::tokens_of(*d);
-    for (long long row = 0; row < d->m; row += tokens) {
-        a.m = (int)(d->m - row < tokens ? d->m - row : tokens);
+    for (long long row = 0; row < d->m; row += fq::kAdaptersMostTokens) {
+        fq::AdapterArgs a = fq::args_of(*d, fq::at_most(d->m - row, fq::kAdaptersMostTokens), workspace);
         a.x = d->x ? (const char *)d->x + (size_t)(row * d->ldx) * fq::size_of(d->x_dtype) : nullptr;
         a.xs = d->x_dtype == FQ_I8 ? d->xs + row * d->xs_step : nullptr;
         a.ids = d->ids + row;
