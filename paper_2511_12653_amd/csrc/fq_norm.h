@@ -19,28 +19,14 @@ struct NormArgs {
     float *partial;            // [parts][2][width] sums of the rows' shares of gweight and gbias
     long long rows;
     long long ldx, ldy, ldgy, ldgx;
-    int width, parts;
+    int width, parts, blocks;
+    int lanes, vecs;           // that a row has; vectors of eight values that a lane has
     float eps;
+    double inverse;            // 1 / width
     int x16, y16, codes, w16;  // 1: FP16 (else FP32); y is codes
 };
 
-struct NormShape {
-    int lanes, vecs;           // that a row has; vectors of eight values that a lane has
-    int rows() const { return lanes < 256 ? 256 / lanes : 1; }      // rows of a block at a time
-};
-
-inline NormShape norm_shape(long long width)
-{
-    if (width <= 128) return {16, 1};
-    if (width <= 256) return {16, 2};
-    if (width <= 384) return {16, 3};
-    if (width <= 512) return {64, 1};
-    if (width <= 1024) return {64, 2};
-    if (width <= 2048) return {256, 1};
-    if (width <= 4096) return {256, 2};
-    if (width <= 8192) return {512, 2};
-    return {1024, 2};          // (wider rows are read again)
-}
+constexpr int norm_threads(int lanes) { return lanes > 64 ? lanes : 256; }       // of a block
 
 int launch_norm_forward(const NormArgs &a, void *stream);
 int launch_norm_backward(const NormArgs &a, void *stream);

@@ -12,7 +12,7 @@ namespace {
 
 constexpr size_t kAlign = 256;
 constexpr long long kMostRows = 1LL << 36, kMostRowsOfPart = 256, kMostParts = 1LL << 21;
-constexpr long long kChipBlocks = 2 * kComputeUnits;
+constexpr long long kAloneGroups = 2;
 
 bool float_type(int32_t dtype) { return dtype == FQ_F16 || dtype == FQ_F32; }
 
@@ -63,15 +63,50 @@ fq_status validate(const fq_norm &d, bool backward)
     return alias(out, 3, in, 4, 2) ? FQ_ERR_ALIAS : FQ_OK;
 }
 
+// How rows are spread over the chip: lanes of a row, vectors of eight values to a lane, blocks to a compute unit, which then go from row
+// to row.  What a row costs beside its values (its sums over the lanes, its root) is paid by every wavefront that has a part of it, so
+// lanes have as many values as registers allow; more blocks hide more of it, fewer ask for weight and bias less often.  FP16, us, with the
+// shape here / others: forward 19200 x 384 (16, 3, 3) 7.6 / (64, 1) 11.2; 16384 x 2048 (64, 4, 2) 26.3 / (256, 1) 36.2; 32768 x 8192 (256, 4, 1)
+// 176 / (256, 4, 2) 195 / (512, 2, 2) 191; codes 16384 x 4096 (256, 2, 6) 58.2 / (256, 2, 2) 70 / (512, 2) 80; backward 19200 x 384 (64, 1, 2)
+// 15.5 / (16, 3, 2) 17.3; 1201 x 1155 (256, 1, 1) 11.4 / (64, 3, 1) 12.0; 32768 x 8192 (256, 4, 1) 285 / (512, 2, 1) 293.
+struct Shape {
+    int lanes, vecs, blocks;
+    int rows() const { return norm_threads(lanes) / lanes; }         // of a block at a time
+};
+
+Shape shape_of(const fq_norm &d, bool backward)
+{
+    const long long width = d.width;
+    if (width > kNormHeldWidth) return {1024, 2, 2};
+    if (width < 8) return {16, 1, 4};
+    if (backward) {
+        if (width <= 256) return {16, width <= 128 ? 1 : 2, 2};
+        if (width <= 1024) return {64, width <= 512 ? 1 : 2, 2};
+        if (width <= 2048) return {256, 1, 2};
+        if (width <= 4096) return {256, 2, 2};
+        return {width <= 8192 ? 256 : 512, 4, 1};
+    }
+    const bool codes = d.y_dtype == FQ_I8;
+    if (width <= 128) return {16, 1, 6};
+    if (width <= 512) return {16, width <= 256 ? 2 : width <= 384 ? 3 : 4, codes ? 2 : 3};
+    if (width <= 1536) return {64, width <= 1024 ? 2 : 3, codes ? 6 : 2};
+    if (width <= 2048) return {64, 4, 2};
+    if (width <= 4096) return {256, 2, codes ? 6 : 2};
+    if (width <= 8192) return {256, 4, codes ? 6 : 1};
+    return {512, 4, 1};
+}
+
 // Blocks of the backward pass, each of which makes a partial sum of every column: as many as the chip holds, and enough for no
 // more than kMostRowsOfPart rows to one (those are added in binary32, the parts in binary64).  Rows that no block holds go in
-// strips of columns: so many blocks to a part.
+// strips of columns: so many blocks to a part.  A few rows are one part, which needs no second launch.
 int parts_of(const fq_norm &d)
 {
-    const long long rows = norm_shape(d.width).rows(), groups = (d.rows + rows - 1) / rows;
-    const long long least = (groups + kMostRowsOfPart - 1) / kMostRowsOfPart;
-    const long long strips = d.width > kNormHeldWidth ? (d.width + kNormStrip - 1) / kNormStrip : 1;
-    const long long chip = strips < kChipBlocks ? kChipBlocks / strips : 1;
+    const Shape s = shape_of(d, true);
+    const long long groups = (d.rows + s.rows() - 1) / s.rows(), least = (groups + kMostRowsOfPart - 1) / kMostRowsOfPart;
+    const bool held = d.width <= kNormHeldWidth;
+    if (held && groups <= kAloneGroups) return 1;
+    const long long strips = held ? 1 : (d.width + kNormStrip - 1) / kNormStrip;
+    const long long chip = held ? (long long)s.blocks * kComputeUnits : strips < 2 * kComputeUnits ? 2 * kComputeUnits / strips : 1;
     const long long parts = groups < chip ? groups : least > chip ? least : chip, most = kMostParts / strips;
     return (int)(parts < most ? parts : most);
 }
@@ -82,15 +117,19 @@ size_t workspace_of(const fq_norm &d)
     return round_up((size_t)parts_of(d) * 2 * (size_t)d.width * sizeof(float), kAlign);
 }
 
-NormArgs args_of(const fq_norm &d)
+NormArgs args_of(const fq_norm &d, bool backward)
 {
     NormArgs a;
     std::memset(&a, 0, sizeof a);
     a.x = d.x; a.w = d.weight; a.b = d.bias; a.y = d.y; a.stats = d.stats;
     a.ys = d.ys; a.gy = d.gy; a.gx = d.gx; a.gw = d.gweight; a.gb = d.gbias;
-    a.rows = d.rows; a.width = (int)d.width; a.eps = d.eps;
+    a.rows = d.rows; a.width = (int)d.width; a.eps = d.eps; a.inverse = 1.0 / (double)d.width;
     a.ldx = d.ldx; a.ldy = d.ldy; a.ldgy = d.ldgy; a.ldgx = d.ldgx;
     a.x16 = d.x_dtype == FQ_F16; a.y16 = d.y_dtype == FQ_F16; a.codes = d.y_dtype == FQ_I8; a.w16 = d.w_dtype == FQ_F16;
+    const Shape s = shape_of(d, backward);
+    const long long groups = (d.rows + s.rows() - 1) / s.rows(), chip = (long long)s.blocks * kComputeUnits;
+    a.lanes = s.lanes; a.vecs = s.vecs;
+    a.blocks = (int)(groups < chip ? groups : chip);
     return a;
 }
 
@@ -104,7 +143,7 @@ fq_status fq_norm_forward(const fq_norm *d, void *hip_stream)
     if (!d) return FQ_ERR_NULL;
     const fq_status st = fq::validate(*d, false);
     if (st != FQ_OK || d->rows == 0 || d->width == 0) return st;
-    return fq::launch_norm_forward(fq::args_of(*d), hip_stream) == 0 ? FQ_OK : FQ_ERR_LAUNCH;
+    return fq::launch_norm_forward(fq::args_of(*d, false), hip_stream) == 0 ? FQ_OK : FQ_ERR_LAUNCH;
 }
 
 size_t fq_norm_workspace_bytes(const fq_norm *d)
@@ -117,7 +156,7 @@ fq_status fq_norm_backward(const fq_norm *d, void *workspace, size_t ws_bytes, v
     if (!d) return FQ_ERR_NULL;
     const fq_status st = fq::validate(*d, true);
     if (st != FQ_OK || d->width == 0 || (!d->gx && !d->gweight && !d->gbias)) return st;
-    fq::NormArgs a = fq::args_of(*d);
+    fq::NormArgs a = fq::args_of(*d, true);
     if (d->rows > 0 && (d->gweight || d->gbias)) {
         if (!workspace || ws_bytes < fq::workspace_of(*d)) return FQ_ERR_WORKSPACE;
         if (!fq::aligned(workspace, fq::kAlign)) return FQ_ERR_ALIGN;
@@ -125,6 +164,7 @@ fq_status fq_norm_backward(const fq_norm *d, void *workspace, size_t ws_bytes, v
         a.parts = fq::parts_of(*d);
     }
     if (d->rows == 0 && !d->gweight && !d->gbias) return FQ_OK;
+    if (a.partial && d->width <= fq::kNormHeldWidth) a.blocks = a.parts;
     return fq::launch_norm_backward(a, hip_stream) == 0 ? FQ_OK : FQ_ERR_LAUNCH;
 }
 
