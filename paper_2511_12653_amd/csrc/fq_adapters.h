@@ -10,7 +10,10 @@ constexpr long long kAdaptersMostWidth = 1LL << 20;
 constexpr int kAdaptersMostRank = 256;
 constexpr int kWindow = 64;                      // tokens that a wavefront sorts out by itself
 constexpr long long kAdaptersMostTokens = 1 << 16;       // of a launch
-constexpr int kMostGrouped = 8192;               // adapters that tokens are grouped by
+constexpr int kSorted = 1024;                    // tokens (and adapters) that a block sorts out by itself
+constexpr int kMostGrouped = 8192;               // adapters that tokens are grouped by in a launch of its own
+
+enum AdapterWay { kWindows, kSorting, kList };   // how a block comes to its tokens
 
 struct AdapterTile {                             // tokens of one adapter
     int id, first, count;                        // adapter (-1: none); places in `order`
@@ -25,15 +28,16 @@ struct AdapterArgs {
     const void *base;
     void *y;
     float *t;                  // [splits][m][pitch] sums over a part of k each
-    int *order;                // [m] tokens by adapter
-    AdapterTile *tiles;        // [tiles_most]
+    int *order;                // kList: [m] tokens by adapter
+    AdapterTile *tiles;        // kList: [tiles_most]
     long long ldx, ldy, ldbase;
     int m, n, k, count, rank;
     int pitch;                 // of a row of t: whole 16 values
-    int grouped;               // 1: order and tiles are made; 0: windows of kWindow tokens, in the order that they come in
+    int way;                   // AdapterWay
     int tiles_most;            // tiles there can be
-    int token_tiles;           // tokens of a tile in 16s: 1 or 4
-    int splits, chunks;        // parts of k; of the ranks, 64 each
+    int token_tiles;           // tokens of a tile in 16s: 1 or 2
+    int rank_tiles;            // ranks of a block in 16s: 1, 2 or 4
+    int splits, chunks;        // parts of k; of the ranks
     int wide, groups;          // channels of a wavefront at a time in 16s: 1 or 4; blocks that share a tile's channels
     int xs_step;
     int x_type;                // fq_dtype

@@ -10,7 +10,7 @@ namespace fq {
 namespace {
 
 constexpr size_t kAlign = 256;
-constexpr long long kDownBlocks = 4 * kComputeUnits, kMostSplits = 32;     // blocks that x a^T is cut into, about
+constexpr long long kDownBlocks = 4 * kComputeUnits, kMostSplits = 8;      // blocks that the chip holds
 constexpr long long kUpWaves = 4 * kComputeUnits, kUpBlocks = 8 * kComputeUnits;
 
 fq_status validate(const fq_adapters &d)
@@ -51,15 +51,16 @@ AdapterArgs plan_of(const fq_adapters &d, long long m)
     std::memset(&a, 0, sizeof a);
     a.m = (int)m; a.n = (int)d.n; a.k = (int)d.k; a.count = d.rank > 0 ? (int)d.count : 0; a.rank = (int)d.rank;
     a.pitch = (int)ceiling(d.rank, 16) * 16;
-    a.chunks = (int)ceiling(d.rank, 64);
-    a.token_tiles = m >= 32LL * a.count && d.rank <= 192 ? 4 : 1;        // (t of 64 tokens and 192 ranks: 51 KB of LDS)
+    a.token_tiles = m >= 16LL * a.count && d.n >= 8 && d.k >= 16 ? 2 : 1;
+    a.rank_tiles = d.rank <= 16 || d.k < 16 ? 1 : d.rank <= 32 ? 2 : 4;
+    a.chunks = (int)ceiling(d.rank, 16 * a.rank_tiles);
     const long long tile = 16 * a.token_tiles, some = at_most(a.count + 1LL, m);
-    a.grouped = m > kWindow && a.count > 0 && a.count <= kMostGrouped;
-    a.tiles_most = (int)(a.grouped ? m / tile + some : ceiling(m, kWindow) * at_most(m, kWindow));
+    a.way = m <= kWindow || a.count == 0 || a.count > kMostGrouped ? kWindows : m <= kSorted && a.count <= kSorted ? kSorting : kList;
+    a.tiles_most = (int)(a.way != kWindows ? m / tile + some : ceiling(m, kWindow) * at_most(m, kWindow));
     const long long tiles = at_least(m / tile + at_most(a.count, m), 1) * at_least(a.chunks, 1);
     // a block takes 256 values of k at a time
     a.splits = (int)at_least(at_most(at_most(kDownBlocks / tiles, ceiling(d.k, 256)), kMostSplits), 1);
-    a.wide = tiles * ceiling(d.n, 64) > kUpWaves ? 4 : 1;
+    a.wide = a.token_tiles == 2 || (d.n >= 8 && tiles * ceiling(d.n, 64) > kUpWaves) ? 4 : 1;
     const long long strips = ceiling(d.n, 64 * a.wide);          // that a block of four wavefronts takes at a time
     a.groups = (int)at_least(at_most(strips, ceiling(kUpBlocks, a.tiles_most)), 1);
     return a;
@@ -76,7 +77,7 @@ Workspace workspace_of(const fq_adapters &d)
     const AdapterArgs a = plan_of(d, at_most(d.m, kAdaptersMostTokens));
     at.tiles = round_up((size_t)a.m * sizeof(int), kAlign);
     // (the last tokens of a call may come in a launch of fewer, in smaller tiles; calls of several launches do not cut up k)
-    at.t = at.tiles + round_up((size_t)(a.grouped ? a.m / 16 + at_most(a.count + 1LL, a.m) : 0) * sizeof(AdapterTile) + sizeof(int), kAlign);
+    at.t = at.tiles + round_up((size_t)(a.way == kList ? a.m / 16 + at_most(a.count + 1LL, a.m) : 0) * sizeof(AdapterTile) + sizeof(int), kAlign);
     at.bytes = at.t + round_up((size_t)a.m * (size_t)a.pitch * sizeof(float) * (size_t)(d.m > kAdaptersMostTokens ? 1 : a.splits), kAlign);
     return at;
 }
