@@ -11,7 +11,7 @@ constexpr int kAdaptersMostRank = 256;
 constexpr int kWindow = 64;                      // tokens that a wavefront sorts out by itself
 constexpr long long kAdaptersMostTokens = 1 << 16;       // of a launch
 constexpr int kSorted = 1024;                    // tokens (and adapters) that a block sorts out by itself
-constexpr int kMostGrouped = 8192;               // adapters that tokens are grouped by in a launch of its own
+constexpr int kMostGrouped = 1024;               // adapters that tokens are grouped by
 
 enum AdapterWay { kWindows, kSorting, kList };   // how a block comes to its tokens
 
@@ -35,13 +35,14 @@ struct AdapterArgs {
     int pitch;                 // of a row of t: whole 16 values
     int way;                   // AdapterWay
     int tiles_most;            // tiles there can be
-    int token_tiles;           // tokens of a tile in 16s: 1 or 2
+    int token_tiles;           // tokens of a tile in 16s: 1, 2 or 4
     int rank_tiles;            // ranks of a block in 16s: 1, 2 or 4
     int splits, chunks;        // parts of k; of the ranks
-    int wide, groups;          // channels of a wavefront at a time in 16s: 1 or 4; blocks that share a tile's channels
+    int wide, groups;          // channels of a wavefront at a time in 16s: 2 or 4; blocks that share a tile's channels
+    unsigned x_bytes;          // of all rows of x where x and a fit the loads into LDS, else 0
     int xs_step;
     int x_type;                // fq_dtype
-    int y16, base16;
+    int y16, base16, no_base;  // no_base: base is y, of which nothing counts
 };
 
 int launch_adapters(const AdapterArgs &a, void *stream);

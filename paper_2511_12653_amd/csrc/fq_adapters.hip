@@ -25,10 +25,12 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ bool has_adapter(int id, int count) { return id >= 0 && id < count; }
 
 // ---------------------------------------------------------------------------------------------
-// Tokens in the order of their adapters (those without one behind all others), and the tiles of up to `tile` of each.  One block:
-// ids are read twice.  Places of one adapter's tokens are handed out by an atomic counter, so which tile a token is in may differ from
-// run to run; what is worked out for it does not depend on that.
-constexpr int kGroupThreads = 1024, kHeldIds = 8;
+// Tokens in the order of their adapters (those without one behind all others), those of an adapter in the order that they come in, and
+// the tiles of each.  One block, each of whose wavefronts has a run of tokens and counters of its own: what each adds to them is known from
+// the lanes with the same adapter, so places do not depend on which wavefront is first.
+constexpr int kGroupThreads = 1024, kGroupWaves = kGroupThreads / 64, kHeldIds = 8;
+constexpr int kGroupBits = 11;                   // of a group's number: kMostGrouped and one more
+static_assert(kMostGrouped < (1 << kGroupBits), "groups have numbers of kGroupBits");
 
 __device__ __forceinline__ int group_of(const AdapterArgs &a, int token)
 {
@@ -36,20 +38,22 @@ __device__ __forceinline__ int group_of(const AdapterArgs &a, int token)
     return has_adapter(id, a.count) ? id : a.count;
 }
 
-// Counts the lanes with `some` for their groups; the number that were counted there before a lane's.  (Tokens of one request come one
-// after the other: then the wavefront counts for one adapter, once.)
-__device__ __forceinline__ int count_in(int *counts, int group, bool some, int lane)
+// The lanes with `some` that have this lane's group.
+__device__ __forceinline__ unsigned long long peers(int group, bool some)
 {
-    const unsigned long long all = __ballot(some);
-    if (all == 0) return 0;
-    const int first = __builtin_ctzll(all), leader = __builtin_amdgcn_readlane(group, first);
-    if (__ballot(some && group == leader) == all) {
-        int before = 0;
-        if (lane == first) before = atomicAdd(counts + leader, __popcll(all));
-        return __builtin_amdgcn_readlane(before, first) + __popcll(all & ((1ull << lane) - 1));
+    unsigned long long mine = __ballot(some);
+    if (mine == 0) return 0;
+    const int leader = __builtin_amdgcn_readlane(group, __builtin_ctzll(mine));
+    if (__ballot(some && group == leader) == mine) return mine;          // (tokens of one request come one after the other)
+#pragma unroll
+    for (int bit = 0; bit < kGroupBits; ++bit) {
+        const unsigned long long set = __ballot(group >> bit & 1);
+        mine &= group >> bit & 1 ? set : ~set;
     }
-    return some ? atomicAdd(counts + group, 1) : 0;
+    return mine;
 }
+
+__device__ __forceinline__ int before(unsigned long long lanes, int lane) { return __popcll(lanes & ((1ull << lane) - 1)); }
 
 // Sums of both values over the threads of a block before this one, and of all (in `total`, of the second).
 template <int WAVES> __device__ __forceinline__ void sums_before(int &a, int &b, int &total, int (&sums)[2][WAVES], int lane, int wave)
@@ -81,51 +85,63 @@ template <int WAVES> __device__ __forceinline__ void sums_before(int &a, int &b,
 
 __global__ __launch_bounds__(kGroupThreads) void adapter_group_kernel(AdapterArgs a)
 {
-    extern __shared__ int counts[];              // [count + 1]: of tokens, then the next free place
-    __shared__ int sums[2][kGroupThreads / 64];
+    extern __shared__ int counts[];              // [kGroupWaves][count + 1]: of tokens, then the next free place
+    __shared__ int sums[2][kGroupWaves];
     const int groups = a.count + 1, thread = threadIdx.x, lane = thread & 63, wave = thread >> 6;
-    const int tile = 16 * a.token_tiles;
-    constexpr int kRun = kGroupThreads * kHeldIds;
+    const int tile = 16 * a.token_tiles, run = (a.m + kGroupThreads - 1) / kGroupThreads * 64;
+    const int first = wave * run, last = min(first + run, a.m);
+    volatile int *const own = counts + wave * groups;
     int held[kHeldIds];
     const auto ask = [&](int from) {
 #pragma unroll
-        for (int j = 0; j < kHeldIds; ++j) held[j] = group_of(a, from + j * kGroupThreads + thread);
+        for (int j = 0; j < kHeldIds; ++j) held[j] = group_of(a, min(from + j * 64 + lane, last));
     };
-    ask(0);
-    for (int i = thread; i < groups; i += kGroupThreads) counts[i] = 0;
+    ask(first);
+    for (int i = thread; i < groups * kGroupWaves; i += kGroupThreads) counts[i] = 0;
     __syncthreads();
-    for (int from = 0; from < a.m; from += kRun) {
-        if (from > 0) ask(from);
+    for (int from = first; from < last; from += 64 * kHeldIds) {
+        if (from > first) ask(from);
 #pragma unroll
-        for (int j = 0; j < kHeldIds; ++j) count_in(counts, held[j], from + j * kGroupThreads + thread < a.m, lane);
+        for (int j = 0; j < kHeldIds; ++j) {
+            const unsigned long long mine = peers(held[j], from + j * 64 + lane < last);
+            if ((mine >> lane & 1) && before(mine, lane) == 0) own[held[j]] = own[held[j]] + __popcll(mine);
+        }
     }
     __syncthreads();
     // first places and first tiles of the groups: each thread has a run of them
     const int each = (groups + kGroupThreads - 1) / kGroupThreads, begin = min(thread * each, groups), end = min(begin + each, groups);
     int token_at = 0, tile_at = 0, all_tiles;
     for (int g = begin; g < end; ++g) {
-        token_at += counts[g];
-        tile_at += (counts[g] + tile - 1) / tile;
+        int count = 0;
+#pragma unroll
+        for (int w = 0; w < kGroupWaves; ++w) count += counts[w * groups + g];
+        token_at += count;
+        tile_at += (count + tile - 1) / tile;
     }
     sums_before(token_at, tile_at, all_tiles, sums, lane, wave);
     for (int g = begin; g < end; ++g) {
-        const int count = counts[g];
-        for (int i = 0; i < count; i += tile) {
-            const AdapterTile t = {g < a.count ? g : -1, token_at + i, min(tile, count - i)};
-            a.tiles[tile_at++] = t;
+        const int start = token_at;
+#pragma unroll
+        for (int w = 0; w < kGroupWaves; ++w) {
+            const int count = counts[w * groups + g];
+            counts[w * groups + g] = token_at;
+            token_at += count;
         }
-        counts[g] = token_at;
-        token_at += count;
+        for (int i = start; i < token_at; i += tile) a.tiles[tile_at++] = AdapterTile{g < a.count ? g : -1, i, min(tile, token_at - i)};
     }
     for (int i = all_tiles + thread; i < a.tiles_most; i += kGroupThreads) a.tiles[i] = AdapterTile{-1, 0, 0};
     __syncthreads();
-    for (int from = 0; from < a.m; from += kRun) {
-        if (a.m > kRun) ask(from);
+    for (int from = first; from < last; from += 64 * kHeldIds) {
+        if (run > 64 * kHeldIds) ask(from);
 #pragma unroll
         for (int j = 0; j < kHeldIds; ++j) {
-            const int token = from + j * kGroupThreads + thread;
-            const int place = count_in(counts, held[j], token < a.m, lane);
-            if (token < a.m) a.order[place] = token;
+            const int token = from + j * 64 + lane;
+            const unsigned long long mine = peers(held[j], token < last);
+            if (mine >> lane & 1) {
+                const int place = own[held[j]], rank = before(mine, lane);
+                a.order[place + rank] = token;
+                if (rank == 0) own[held[j]] = place + __popcll(mine);
+            }
         }
     }
 }
@@ -161,7 +177,7 @@ __device__ __forceinline__ Tile find_tile(const AdapterArgs &a, int index, Findi
         t.id = __builtin_amdgcn_readlane(id, slot);
         const unsigned long long mine = __ballot(id == t.id);
         t.count = slot < left && __builtin_ctzll(mine) == slot ? __popcll(mine) : 0;
-        if (thread < 64 && (mine >> lane & 1)) s.tokens[__popcll(mine & ((1ull << lane) - 1))] = begin + lane;
+        if (thread < 64 && (mine >> lane & 1)) s.tokens[before(mine, lane)] = begin + lane;
     } else if (a.way == kSorting) {
         constexpr int kIds = kSorted / kBlock;
         const int groups = a.count + 1, tile = 16 * a.token_tiles;
@@ -172,7 +188,10 @@ __device__ __forceinline__ Tile find_tile(const AdapterArgs &a, int index, Findi
         if (thread == 0) s.tile = t;
         __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kIds; ++j) count_in(s.counts, id[j], j * kBlock + thread < a.m, lane);
+        for (int j = 0; j < kIds; ++j) {
+            const unsigned long long mine = peers(id[j], j * kBlock + thread < a.m);
+            if ((mine >> lane & 1) && before(mine, lane) == 0) atomicAdd(s.counts + id[j], __popcll(mine));
+        }
         __syncthreads();
         const int each = (groups + kBlock - 1) / kBlock, begin = min(thread * each, groups), end = min(begin + each, groups);
         int at = 0, none = 0, all;
@@ -197,14 +216,14 @@ __device__ __forceinline__ Tile find_tile(const AdapterArgs &a, int index, Findi
             if (lane == 0) s.parts[j * (kBlock / 64) + wave] = __popcll(mine[j]);
         }
         __syncthreads();
-        int before = -s.first;
+        int place = -s.first;
 #pragma unroll
         for (int j = 0; j < kIds; ++j)
 #pragma unroll
             for (int w = 0; w < kBlock / 64; ++w) {
-                const int place = before + __popcll(mine[j] & ((1ull << lane) - 1));
-                if (w == wave && (mine[j] >> lane & 1) && place >= 0 && place < t.count) s.tokens[place] = j * kBlock + thread;
-                before += s.parts[j * (kBlock / 64) + w];
+                const int own = place + before(mine[j], lane);
+                if (w == wave && (mine[j] >> lane & 1) && own >= 0 && own < t.count) s.tokens[own] = j * kBlock + thread;
+                place += s.parts[j * (kBlock / 64) + w];
             }
     } else {
         const AdapterTile f = a.tiles[index];
@@ -220,13 +239,24 @@ __device__ __forceinline__ Tile find_tile(const AdapterArgs &a, int index, Findi
 // zero in one of the two factors.  SHORT: rows of less, value by value.
 __device__ __forceinline__ int begin_of(int at, int n, int width) { return max(min(at, width - n), 0); }
 
-template <int N, bool SHORT, typename T> __device__ __forceinline__ void load(T *to, const T *row, int at, int width)
+// N values, in the words that they are loaded in.  (As an array of values they would be taken apart into a register each.)
+template <typename T, int N> struct Words {
+    static constexpr int kWords = (int)sizeof(T) * N / 4;
+    typedef T V __attribute__((ext_vector_type(N)));
+    typedef int W __attribute__((ext_vector_type(kWords)));
+    W w;
+    __device__ __forceinline__ V values() const { return __builtin_bit_cast(V, w); }
+};
+
+template <bool SHORT, typename T, int N> __device__ __forceinline__ void load(Words<T, N> &to, const T *row, int at, int width)
 {
     if constexpr (!SHORT) {
-        __builtin_memcpy(to, (const FQ_GLOBAL T *)(row + at), sizeof(T) * N);
+        __builtin_memcpy(&to, (const FQ_GLOBAL T *)(row + at), sizeof to);
     } else {
+        typename Words<T, N>::V v;
 #pragma unroll
-        for (int e = 0; e < N; ++e) to[e] = ld_global(row + min(at + e, width - 1));
+        for (int e = 0; e < N; ++e) v[e] = ld_global(row + min(at + e, width - 1));
+        to.w = __builtin_bit_cast(typename Words<T, N>::W, v);
     }
 }
 
@@ -247,51 +277,113 @@ __device__ __forceinline__ f16x8 halves_of(int low, int high)
 
 // 16 neighbouring values of a row.
 template <typename X> struct Piece {
-    X v[16];
-    template <bool SHORT> __device__ __forceinline__ void fetch(const X *row, int at, int k) { load<16, SHORT>(v, row, at, k); }
+    Words<X, 16> p;
+    template <bool SHORT> __device__ __forceinline__ void fetch(const X *row, int at, int k) { load<SHORT>(p, row, at, k); }
     // only those from `first` to `last` count
     __device__ __forceinline__ void keep(int first, int last)
     {
+        constexpr int kEach = 4 / (int)sizeof(X), kBits = 8 * (int)sizeof(X);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) v[e] = e >= first && e <= last ? v[e] : (X)0;
+        for (int d = 0; d < Words<X, 16>::kWords; ++d) {
+            unsigned mask = 0;
+#pragma unroll
+            for (int e = 0; e < kEach; ++e)
+                mask |= d * kEach + e >= first && d * kEach + e <= last ? (unsigned)((1ull << kBits) - 1) << (e * kBits) : 0u;
+            p.w[d] &= (int)mask;
+        }
     }
     __device__ __forceinline__ f16x8 half(int i) const
     {
-        f16x8 h;
-        if constexpr (sizeof(X) == 1) {
-            int w[4];
-            __builtin_memcpy(w, v, sizeof w);
-            h = halves_of(w[2 * i], w[2 * i + 1]);
-        } else {
-            __builtin_memcpy(&h, v + 8 * i, sizeof h);
-        }
-        return h;
+        if constexpr (sizeof(X) == 1) return halves_of(p.w[2 * i], p.w[2 * i + 1]);
+        else return __builtin_bit_cast(f16x8, i32x4{p.w[4 * i], p.w[4 * i + 1], p.w[4 * i + 2], p.w[4 * i + 3]});
     }
+    __device__ __forceinline__ X value(int e) const { return p.values()[e]; }
 };
 
-// t of a tile: NT x 16 tokens by NR x 16 ranks.  The wavefronts of a block take 64 values of k in turn; their sums meet in LDS.  Loads go
-// straight into the registers that the matrix instructions take (lane l: token l % 16, and rank l % 16, values 16 (l / 16) and on of the
-// 64: whole lines from four lanes).  Small tiles have the loads of the next 64 on their way while these are multiplied; large ones
-// would need more registers for that than four blocks on a compute unit have, and those cover for each other.
+// The products of 64 values of k: a lane has 16 neighbouring ones of a token, and of a rank.
+template <typename X, int NT, int NR> __device__ __forceinline__ void multiply(f32x4 (&sum)[NT][NR], const Piece<X> (&x)[NT], const Piece<_Float16> (&w)[NR])
+{
+    if constexpr (std::is_same<X, float>::value) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const float v = (float)w[r].value(e);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) sum[n][r] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, x[n].value(e), sum[n][r], 0, 0, 0);
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            f16x8 v[NT];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) v[n] = x[n].half(i);
+#pragma unroll
+            for (int r = 0; r < NR; ++r)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) sum[n][r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[r].half(i), v[n], sum[n][r], 0, 0, 0);
+        }
+    }
+}
+
+// The sums of a block's wavefronts, added up and written to t.  Lane l's four: token l % 16, ranks 4 (l / 16) and on.
 constexpr int kDownWaves = kBlock / 64, kDepth = 64;
 
-template <typename X, int NT, int NR, bool SHORT>
-__global__ __launch_bounds__(kBlock, NT * NR == 1 ? 1 : 4) void adapter_down_kernel(AdapterArgs a)
+template <int NT, int NR>
+__device__ __forceinline__ void join(const AdapterArgs &a, f32x4 (*part)[NT * NR][64], const f32x4 (&sum)[NT][NR], const int *tokens, int sub, int count,
+                                     int split, int chunk)
 {
-    constexpr int kAhead = NT * NR == 1 ? 2 : 1;                   // steps whose loads are on their way at a time
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int r = 0; r < NR; ++r) part[wave][n * NR + r][lane] = sum[n][r];
+    __syncthreads();
+    for (int i = threadIdx.x; i < NT * NR * 64; i += kBlock) {
+        const int n = i / 64 / NR, r = i / 64 % NR, l = i % 64;
+        const int token = sub + n * 16 + l % 16, rank = (chunk * NR + r) * 16 + l / 16 * 4;
+        f32x4 s = part[0][n * NR + r][l];
+#pragma unroll
+        for (int v = 1; v < kDownWaves; ++v) s += part[v][n * NR + r][l];
+        if (token < count && rank < a.pitch) st_global((f32x4 *)(a.t + ((long long)split * a.m + tokens[token]) * a.pitch + rank), s);
+    }
+    __syncthreads();
+}
+
+// What a block of the kernels below works on: a tile, a part of the ranks, and steps [begin, begin + length) of 64 values of k.  Each tile
+// begins elsewhere in its part and goes round (`turn`), so that blocks do not all ask for the same columns at a time.
+struct Share {
+    int index, split, chunk, begin, length, turn;
+    __device__ __forceinline__ explicit Share(const AdapterArgs &a)
+    {
+        split = blockIdx.x % a.splits;
+        chunk = blockIdx.x / a.splits % a.chunks;
+        index = blockIdx.x / a.splits / a.chunks;
+        const int steps = (a.k + kDepth - 1) / kDepth;
+        begin = (int)((long long)steps * split / a.splits);
+        length = (int)((long long)steps * (split + 1) / a.splits) - begin;
+        turn = length > 0 ? (int)((unsigned)index * 2654435769u >> 16) % length : 0;
+    }
+    __device__ __forceinline__ int step(int i) const { return begin + (i + turn < length ? i + turn : i + turn - length); }
+};
+
+// t of a tile: NT x 16 tokens by NR x 16 ranks.  The wavefronts of a block take 64 values of k in turn.  Here the loads go
+// straight into the registers that the matrix instructions take (lane l: token l % 16, and rank l % 16, values 16 (l / 16) and on of the
+// 64), from rows at any address: for few tokens, and where rows do not fit adapter_down_ring_kernel.
+template <typename X, int NT, int NR, bool SHORT>
+__global__ __launch_bounds__(kBlock, SHORT ? 2 : 4) void adapter_down_kernel(AdapterArgs a)
+{
     __shared__ f32x4 part[kDownWaves][NT * NR][64];
     __shared__ Finding finding;
     const int *tokens = finding.tokens;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int split = blockIdx.x % a.splits, chunk = blockIdx.x / a.splits % a.chunks;
-    const Tile tile = find_tile(a, blockIdx.x / a.splits / a.chunks, finding);
+    const Share share(a);
+    const Tile tile = find_tile(a, share.index, finding);
     if (tile.id < 0 || tile.count == 0) return;
-    const int steps = (a.k + kDepth - 1) / kDepth;
-    const int begin = (int)((long long)steps * split / a.splits), end = (int)((long long)steps * (split + 1) / a.splits);
     const _Float16 *ranks[NR];
 #pragma unroll
     for (int r = 0; r < NR; ++r)
-        ranks[r] = (const _Float16 *)a.a + ((long long)tile.id * a.rank + min((chunk * NR + r) * 16 + lane % 16, a.rank - 1)) * a.k;
+        ranks[r] = (const _Float16 *)a.a + ((long long)tile.id * a.rank + min((share.chunk * NR + r) * 16 + lane % 16, a.rank - 1)) * a.k;
     for (int sub = 0; sub < tile.count; sub += NT * 16) {
         const X *rows[NT];
 #pragma unroll
@@ -301,108 +393,148 @@ __global__ __launch_bounds__(kBlock, NT * NR == 1 ? 1 : 4) void adapter_down_ker
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int r = 0; r < NR; ++r) sum[n][r] = (f32x4)0.0f;
-        Piece<X> x[kAhead][NT];
-        Piece<_Float16> w[kAhead][NR];
-        const auto fetch = [&](int buffer, int step) {
-            const int at = begin_of(step * kDepth + lane / 16 * 16, 16, a.k);
+        for (int i = wave; i < share.length; i += kDownWaves) {
+            Piece<X> x[NT];
+            Piece<_Float16> w[NR];
+            const int at = share.step(i) * kDepth + lane / 16 * 16, from = begin_of(at, 16, a.k);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) x[buffer][n].template fetch<SHORT>(rows[n], at, a.k);
+            for (int n = 0; n < NT; ++n) x[n].template fetch<SHORT>(rows[n], from, a.k);
 #pragma unroll
-            for (int r = 0; r < NR; ++r) w[buffer][r].template fetch<SHORT>(ranks[r], at, a.k);
-        };
-        const auto multiply = [&](int buffer, int step) {
-            if ((step + 1) * kDepth > a.k) {
-                const int at = step * kDepth + lane / 16 * 16, from = begin_of(at, 16, a.k);
+            for (int r = 0; r < NR; ++r) w[r].template fetch<SHORT>(ranks[r], from, a.k);
+            if (share.step(i) * kDepth + kDepth > a.k) {
 #pragma unroll
-                for (int n = 0; n < NT; ++n) x[buffer][n].keep(at - from, a.k - 1 - from);
+                for (int n = 0; n < NT; ++n) x[n].keep(at - from, a.k - 1 - from);
             }
-            if constexpr (std::is_same<X, float>::value) {
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-#pragma unroll
-                    for (int r = 0; r < NR; ++r) {
-                        const float v = (float)w[buffer][r].v[e];
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            sum[n][r] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, x[buffer][n].v[e], sum[n][r], 0, 0, 0);
-                    }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    f16x8 v[NT];
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) v[n] = x[buffer][n].half(i);
-#pragma unroll
-                    for (int r = 0; r < NR; ++r)
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            sum[n][r] = __builtin_amdgcn_mfma_f32_16x16x32_f16(w[buffer][r].half(i), v[n], sum[n][r], 0, 0, 0);
-                }
-            }
-        };
-        int step = begin + wave;
-        if constexpr (kAhead == 2) {
-            if (step < end) fetch(0, step);
-            while (step < end) {
-                if (step + kDownWaves < end) fetch(1, step + kDownWaves);
-                multiply(0, step);
-                step += kDownWaves;
-                if (step >= end) break;
-                if (step + kDownWaves < end) fetch(0, step + kDownWaves);
-                multiply(1, step);
-                step += kDownWaves;
-            }
-        } else {
-            for (; step < end; step += kDownWaves) {
-                fetch(0, step);
-                multiply(0, step);
-            }
+            multiply<X, NT, NR>(sum, x, w);
         }
+        join<NT, NR>(a, part, sum, tokens, sub, tile.count, share.split, share.chunk);
+    }
+}
+
+// The same by way of LDS: loads of whole lines, eight neighbouring lanes to one, go straight there, each wavefront's into a ring of its own
+// whose slots hold 64 values of k of all rows, and the lanes pick out what the matrix instructions take.  (Lanes of one load
+// in 16 rows, as above, are looked up in the caches one by one: 8192 x 8192 by 64 ranks 48 us, so @R@.)  A slot's rows of C chunks of 16 bytes lie
+// one behind the other, chunk c of row r at place c ^ (r C / 16 modulo C): LDS answers 16 lanes at a time from 256 bytes, and 16 neighbouring
+// rows then have theirs in 16 places.
+template <int C> __device__ __forceinline__ int place_in_row(int chunk, int row) { return chunk ^ (row * C / 16 & (C - 1)); }
+
+template <typename X, int NT, int NR> constexpr int ring_slot() { return (NT * (int)sizeof(X) + NR * 2) * 1024; }
+template <typename X, int NT, int NR> constexpr int ring_slots() { return ring_slot<X, NT, NR>() <= 6144 ? 3 : 2; }
+
+template <typename X, int NT, int NR>
+__global__ __launch_bounds__(kBlock) void adapter_down_ring_kernel(AdapterArgs a)
+{
+    constexpr int kSlot = ring_slot<X, NT, NR>(), kSlots = ring_slots<X, NT, NR>(), kX = NT * (int)sizeof(X), kW = NR * 2, kLoads = kX + kW;
+    constexpr int kChunks = 4 * (int)sizeof(X);                    // of 16 bytes, of a row of x in a slot; of a rank's: 8
+    extern __shared__ __attribute__((aligned(1024))) int8_t ring[];            // [wavefronts][slots][x, a]
+    static_assert(kDownWaves * kSlots * kSlot >= kDownWaves * NT * NR * 1024, "the sums of all wavefronts fit in the rings");
+    __shared__ Finding finding;
+    const int *tokens = finding.tokens;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Share share(a);
+    const Tile tile = find_tile(a, share.index, finding);
+    if (tile.id < 0 || tile.count == 0) return;
+    const uint64_t x_at = (uint64_t)a.x, a_at = (uint64_t)a.a + (uint64_t)tile.id * (uint64_t)a.rank * (uint64_t)a.k * 2;
+    // descriptors of raw buffers: the hardware answers loads behind their ends with zeros
+    const i32x4 x_buffer = {(int)x_at, (int)(x_at >> 32) & 0xFFFF, (int)a.x_bytes, 0x00027000};
+    const i32x4 a_buffer = {__builtin_amdgcn_readfirstlane((int)a_at), __builtin_amdgcn_readfirstlane((int)(a_at >> 32) & 0xFFFF), a.rank * a.k * 2, 0x00027000};
+    unsigned w_off[kW];
+#pragma unroll
+    for (int j = 0; j < kW; ++j) {
+        const int row = j * 8 + lane / 8;
+        w_off[j] = (unsigned)min(share.chunk * NR * 16 + row, a.rank - 1) * (unsigned)a.k * 2 + (unsigned)place_in_row<8>(lane % 8, row) * 16;
+    }
+    int8_t *const own = ring + wave * (kSlots * kSlot);
+    for (int sub = 0; sub < tile.count; sub += NT * 16) {
+        unsigned x_off[kX];
+#pragma unroll
+        for (int j = 0; j < kX; ++j) {
+            const int row = (j * 64 + lane) / kChunks;
+            x_off[j] = (unsigned)tokens[min(sub + row, tile.count - 1)] * (unsigned)(a.ldx * (int)sizeof(X)) +
+                       (unsigned)place_in_row<kChunks>(lane % kChunks, row) * 16;
+        }
+        constexpr unsigned kNowhere = 0xFFFFFFF0u;                 // behind the end of any buffer
+        const auto ask = [&](int i) {
+            const bool none = i >= share.length;
+            const unsigned step = none ? 0 : (unsigned)share.step(i);
+            int8_t *const to = own + i / kDownWaves % kSlots * kSlot;
+#pragma unroll
+            for (int j = 0; j < kX; ++j) load_lds(x_buffer, none ? kNowhere : x_off[j] + step * (kDepth * (unsigned)sizeof(X)), to + j * 1024);
+#pragma unroll
+            for (int j = 0; j < kW; ++j) load_lds(a_buffer, none ? kNowhere : w_off[j] + step * (kDepth * 2u), to + (kX + j) * 1024);
+        };
+        f32x4 sum[NT][NR];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int r = 0; r < NR; ++r) part[wave][n * NR + r][lane] = sum[n][r];
-        __syncthreads();
-        // lane l's four sums: token l % 16, ranks 4 (l / 16) and on
-        for (int i = threadIdx.x; i < NT * NR * 64; i += kBlock) {
-            const int n = i / 64 / NR, r = i / 64 % NR, l = i % 64;
-            const int token = sub + n * 16 + l % 16, rank = (chunk * NR + r) * 16 + l / 16 * 4;
-            f32x4 s = part[0][n * NR + r][l];
+            for (int r = 0; r < NR; ++r) sum[n][r] = (f32x4)0.0f;
 #pragma unroll
-            for (int v = 1; v < kDownWaves; ++v) s += part[v][n * NR + r][l];
-            if (token < tile.count && rank < a.pitch)
-                st_global((f32x4 *)(a.t + ((long long)split * a.m + tokens[token]) * a.pitch + rank), s);
+        for (int s = 0; s < kSlots; ++s) ask(wave + s * kDownWaves);
+        for (int i = wave; i < share.length; i += kDownWaves) {
+            loads_but<(kSlots - 1) * kLoads>();
+            const int8_t *const from = own + i / kDownWaves % kSlots * kSlot;
+            Piece<X> x[NT];
+            Piece<_Float16> w[NR];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int row = n * 16 + lane % 16;
+#pragma unroll
+                for (int c = 0; c < (int)sizeof(X); ++c) {
+                    const i32x4 v = *(const i32x4 *)(from + (row * kChunks + place_in_row<kChunks>(lane / 16 * (int)sizeof(X) + c, row)) * 16);
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) x[n].p.w[4 * c + d] = v[d];
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < NR; ++r) {
+                const int row = r * 16 + lane % 16;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const i32x4 v = *(const i32x4 *)(from + kX * 1024 + (row * 8 + place_in_row<8>(lane / 16 * 2 + c, row)) * 16);
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) w[r].p.w[4 * c + d] = v[d];
+                }
+            }
+            if (share.step(i) * kDepth + kDepth > a.k) {           // (what lies behind a row's end is the next row's)
+                const int at = share.step(i) * kDepth + lane / 16 * 16;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) x[n].keep(0, a.k - 1 - at);
+            }
+            multiply<X, NT, NR>(sum, x, w);
+            loads_but<63>();                                       // (the reads of this slot are done)
+            ask(i + kSlots * kDownWaves);
         }
+        loads_but<0>();
         __syncthreads();
+        join<NT, NR>(a, (f32x4(*)[NT * NR][64])ring, sum, tokens, sub, tile.count, share.split, share.chunk);
     }
 }
 
 // ---------------------------------------------------------------------------------------------
-// y of a tile of NT x 16 tokens, in strips of CT x 16 channels to each of four wavefronts.  First the block adds up t (of all its
+// y of a tile of up to 64 tokens, in strips of 16 N channels to each of four wavefronts.  First the block adds up t (of all its
 // parts) and puts it into LDS as two FP16 numbers to a value: t 2^-e to 11 bits and the rest to 11 more, 2^e the power of two that
 // brings the row's greatest into [2^14, 2^15), so that nothing overflows and 22 bits of each are kept, or 2^-39 of the greatest.  (FP16
-// products cost a quarter of the matrix cores' time that binary32 ones take.)  Then a wavefront has channels for the rows of its products and
-// tokens for the columns: lane l has, of token l % 16, groups of 8 (CT 1: of 4) neighbouring channels, and four lanes 64 bytes of FP16.
+// products cost a quarter of the matrix cores' time that binary32 ones take.)  Then a wavefront has tokens for the rows of its products and
+// channels for the columns, the N products' columns N apart: lane l has N neighbouring channels of four tokens, and the 16 lanes of a token
+// have neighbouring ones, so a load or store is of runs of 32 N bytes.  (With lanes of one instruction in 16 rows, 16 bytes each,
+// 8192 x 8192 by 64 ranks took 80 us for this kernel, so @U@: addresses that lie apart are looked up one by one.)
 constexpr int kUpWaves = kBlock / 64;
 
-__device__ __forceinline__ f32x4 product(f16x8 b, f16x8 t, f32x4 sum) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(b, t, sum, 0, 0, 0); }
+__device__ __forceinline__ f32x4 product(f16x8 t, f16x8 b, f32x4 sum) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(t, b, sum, 0, 0, 0); }
 
-// N neighbouring channels.  Where a row ends within them they begin N before its end (see begin_of); those of them that are
+// Stores N neighbouring channels.  Where a row ends within them they begin N before its end (see begin_of); those of them that are
 // others' are left to those.
-template <typename T, int N> struct Channels {
-    T v[N];
-    __device__ __forceinline__ void store(T *row, int at, int n) const
-    {
-        if (at + N <= n) {
-            __builtin_memcpy((FQ_GLOBAL T *)(row + at), v, sizeof v);
-            return;
-        }
-        const int begin = begin_of(at, N, n);
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (begin + e >= at && begin + e < n) st_global(row + begin + e, v[e]);
+template <typename T, int N> __device__ __forceinline__ void store_channels(T *row, int at, int n, const typename Words<T, N>::V &v)
+{
+    if (at + N <= n) {
+        __builtin_memcpy((FQ_GLOBAL T *)(row + at), &v, sizeof v);
+        return;
     }
-};
+    const int begin = begin_of(at, N, n);
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+        if (begin + e >= at && begin + e < n) st_global(row + begin + e, v[e]);
+}
 
 // Where rank l of t lies in LDS, so that eight places are the ranks of one vector of b (which begins eight before the end of a row where it
 // would go over it): the last ranks at the end of their vector, what would be before them behind it.  (Places of no rank hold zeros.)
@@ -413,11 +545,11 @@ __device__ __forceinline__ int place_of_rank(int l, int rank)
     return l < rank ? l + 8 - off : l < last + 8 ? l - off : l;
 }
 
-// y's kernel takes t in units of four ranks, eight lanes to a token: unit u, u + 8, ... to lane u.  J units of a lane, of all parts: eight
+// y's kernel takes t in units of four ranks, eight lanes to a token: unit u, u + 8, ... to lane u.  J units of a lane, of all parts, several
 // loads on their way at a time.
 template <int J> __device__ __forceinline__ void sum_of_parts(f32x4 (&s)[J], const AdapterArgs &a, const float *t, int unit)
 {
-    constexpr int P = 8 / J;
+    constexpr int P = J == 2 ? 2 : 8 / J;
     const long long part = (long long)a.m * a.pitch;
 #pragma unroll
     for (int j = 0; j < J; ++j) s[j] = (f32x4)0.0f;
@@ -439,50 +571,61 @@ template <int J> __device__ __forceinline__ void sum_of_parts(f32x4 (&s)[J], con
         for (int e = 0; e < 4; ++e) s[j][e] = (j * 8 + unit) * 4 + e < a.rank ? s[j][e] : 0.0f;
 }
 
-// FEW: channels, fewer than N; SHORT: rows of b, fewer than eight ranks; J: of t's units, 32 J ranks at most.
-template <typename Y, typename B, int NT, int CT, int J, bool FEW, bool SHORT>
-__global__ __launch_bounds__(kBlock, J == 8 ? 2 : 4) void adapter_up_kernel(AdapterArgs a)
+// A value that the compiler takes for another at each use.  (What follows from it is then worked out where it is needed: the addresses of all
+// rows of a tile, kept over its strips, would take 64 registers.)
+__device__ __forceinline__ int anew(int v)
 {
-    constexpr int N = CT == 1 ? 4 : 8, G = CT == 1 ? 1 : CT / 2;      // channels of a lane that are neighbours, and groups of them
-    extern __shared__ __attribute__((aligned(16))) _Float16 shared[];          // [2][NT * 16][row]
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// TT: tokens of a tile in 16s, at most; J: of t's units, 32 J ranks at most; FEW: channels, fewer than N; SHORT: rows of b, fewer than eight
+// ranks.
+template <typename Y, typename B, int N, int TT, int J, bool FEW, bool SHORT>
+__global__ __launch_bounds__(kBlock, J == 8 || SHORT ? 2 : N == 2 || J == 1 ? 4 : 3) void adapter_up_kernel(AdapterArgs a)
+{
+    constexpr int kHeld = J == 8 ? 1 : J;                             // vectors of b of a channel that are held: all, or one at a time
+    constexpr int kAhead = TT > 1 ? 2 : 1;                            // tokens' tiles whose base is held
+    extern __shared__ __attribute__((aligned(16))) _Float16 shared[];          // [2][tile][row]
     __shared__ Finding finding;
-    __shared__ float factor[NT * 16];
+    __shared__ float factor[kWindow];
     const int *tokens = finding.tokens;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const Tile tile = find_tile(a, blockIdx.x / a.groups, finding);
-    const int deep = (a.rank + 31) / 32, row = deep * 32 + 8;
+    const int deep = (a.rank + 31) / 32, row = deep * 32 + 8, most_tokens = TT * 16;
     const bool copy = tile.id < 0;
-    if (copy && a.base == a.y) return;
-    for (int sub = 0; sub < tile.count; sub += NT * 16) {
+    if (copy && a.base == a.y && !a.no_base) return;
+    for (int sub = 0; sub < tile.count; sub += most_tokens) {
+        const int count = min(tile.count - sub, most_tokens);
         int strip = (int)(blockIdx.x % a.groups) * kUpWaves + wave;
-        long long from[NT], to[NT];
+        const auto first_of = [&](int of) { return of * 16 * N + lane % 16 * N; };
+        Words<_Float16, 8> b[kHeld][N];
+        const auto channel = [&](int c, int of) {
+            return (const _Float16 *)a.b + ((long long)tile.id * a.n + begin_of(first_of(of), N, a.n) + (FEW ? min(c, a.n - 1) : c)) * a.rank;
+        };
+        const auto ask_b = [&](int of) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int token = tokens[min(sub + n * 16 + lane % 16, tile.count - 1)];
-            from[n] = token * a.ldbase;
-            to[n] = token * a.ldy;
-        }
-        Channels<B, N> base[NT][G];
+            for (int c = 0; c < N; ++c) {
+                const _Float16 *from = channel(c, of);
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int g = 0; g < G; ++g)
-#pragma unroll
-                for (int e = 0; e < N; ++e) base[n][g].v[e] = (B)0.0f;
-        const auto ask = [&]() {
-            if (!a.base) return;
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                const int at = begin_of(strip * CT * 16 + g * 32 + lane / 16 * N, N, a.n);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) load<N, FEW>(base[n][g].v, (const B *)a.base + from[n], at, a.n);
+                for (int d = 0; d < kHeld; ++d) load<SHORT>(b[d][c], from, begin_of(d * 32 + lane / 16 * 8, 8, a.rank), a.rank);
             }
         };
-        if (strip * CT * 16 < a.n) ask();
+        Words<B, N> base[kAhead][4];
+        const auto ask_base = [&](int n, int of) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const B *from = (const B *)a.base + tokens[anew(sub + min(n * 16 + lane / 16 * 4 + i, count - 1))] * a.ldbase;
+                load<FEW>(base[n % kAhead][i], from, begin_of(first_of(of), N, a.n), a.n);
+            }
+        };
+        // (strips behind the last clamp to the end of the row: loads of what is left unused)
+        if (!copy && J < 8) ask_b(strip);
+        ask_base(0, strip);
         if (!copy) {
-            const int i = threadIdx.x / 8, unit = threadIdx.x % 8;
-            if (i < NT * 16) {
-                const int token = tokens[min(sub + i, tile.count - 1)];
+            const int unit = threadIdx.x % 8;
+            for (int i = threadIdx.x / 8; i < most_tokens; i += kBlock / 8) {
+                const int token = tokens[sub + min(i, count - 1)];
                 f32x4 s[J];
                 sum_of_parts<J>(s, a, a.t + (long long)token * a.pitch, unit);
                 float most = 0.0f;
@@ -494,7 +637,7 @@ __global__ __launch_bounds__(kBlock, J == 8 ? 2 : 4) void adapter_up_kernel(Adap
                 most = __builtin_fmaxf(most, __shfl_xor(most, 2));
                 most = __builtin_fmaxf(most, __shfl_xor(most, 4));
                 const int e2 = most > 0.0f && most < __builtin_inff() ? 15 - __builtin_amdgcn_frexp_expf(most) : 0;
-                _Float16 *const heads = shared + i * row, *const rests = heads + NT * 16 * row;
+                _Float16 *const heads = shared + i * row, *const rests = heads + most_tokens * row;
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     const int l = (j * 8 + unit) * 4;
@@ -526,88 +669,107 @@ __global__ __launch_bounds__(kBlock, J == 8 ? 2 : 4) void adapter_up_kernel(Adap
             }
         }
         __syncthreads();
-        while (strip * CT * 16 < a.n) {
-            f32x4 sum[NT][CT];
+        while (strip * 16 * N < a.n) {
+            const int after = strip + a.groups * kUpWaves;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int c = 0; c < CT; ++c) sum[n][c] = (f32x4)0.0f;
-            if (!copy) {
-                const _Float16 *channel[CT];
-#pragma unroll
-                for (int c = 0; c < CT; ++c) {
-                    // row i of product c: channel i / 4 of four groups of N, half c % 2 of it, i % 4 of that
-                    const int first = begin_of(strip * CT * 16 + c / 2 * 32 + lane % 16 / 4 * N, N, a.n);
-                    channel[c] = (const _Float16 *)a.b + ((long long)tile.id * a.n + min(first + c % 2 * 4 + lane % 4, a.n - 1)) * a.rank;
+            for (int n = 0; n < TT; ++n) {
+                if (TT > 1) {
+                    if (n + 1 < TT) ask_base(n + 1, strip);
+                    else ask_base(0, after);
                 }
-                for (int d = 0; d < deep; ++d) {
-                    f16x8 b[CT];
+                f32x4 sum[N];
 #pragma unroll
-                    for (int c = 0; c < CT; ++c) load<8, SHORT>((_Float16 *)&b[c], channel[c], begin_of(d * 32 + lane / 16 * 8, 8, a.rank), a.rank);
+                for (int c = 0; c < N; ++c) sum[c] = (f32x4)0.0f;
+                if (!copy) {
+                    const _Float16 *t = shared + (n * 16 + lane % 16) * row + lane / 16 * 8;
+                    const auto multiply = [&](const Words<_Float16, 8> (&by)[N], int d) {
+                        const f16x8 high = *(const f16x8 *)(t + d * 32), low = *(const f16x8 *)(t + d * 32 + most_tokens * row);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const _Float16 *at = shared + (n * 16 + lane % 16) * row + d * 32 + lane / 16 * 8;
-                        const f16x8 high = *(const f16x8 *)at, low = *(const f16x8 *)(at + NT * 16 * row);
+                        for (int c = 0; c < N; ++c) sum[c] = product(low, by[c].values(), product(high, by[c].values(), sum[c]));
+                    };
+                    if constexpr (J < 8) {
 #pragma unroll
-                        for (int c = 0; c < CT; ++c) sum[n][c] = product(b[c], low, product(b[c], high, sum[n][c]));
+                        for (int d = 0; d < kHeld; ++d)
+                            if (d < deep) multiply(b[d], d);
+                    } else {
+                        for (int d = 0; d < deep; ++d) {
+#pragma unroll
+                            for (int c = 0; c < N; ++c)
+                                load<SHORT>(b[0][c], channel(c, strip), begin_of(d * 32 + lane / 16 * 8, 8, a.rank), a.rank);
+                            multiply(b[0], d);
+                        }
                     }
                 }
-            }
-            Channels<Y, N> y[NT][G];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const float f = copy ? 0.0f : factor[n * 16 + lane % 16];
-#pragma unroll
-                for (int g = 0; g < G; ++g)
+                for (int i = 0; i < 4; ++i) {
+                    const int token = n * 16 + lane / 16 * 4 + i;
+                    const float f = copy ? 0.0f : factor[token];
+                    const auto from = base[n % kAhead][i].values();
+                    typename Words<Y, N>::V y;
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
-                        const float v = (float)base[n][g].v[e];
-                        y[n][g].v[e] = (Y)(copy ? v : v + f * sum[n][g * 2 + e / 4][e % 4]);
+                        const float v = a.no_base ? 0.0f : (float)from[e];
+                        y[e] = (Y)(copy ? v : v + f * sum[e][i]);
                     }
+                    if (token < count) store_channels<Y, N>((Y *)a.y + tokens[anew(sub + token)] * a.ldy, first_of(strip), a.n, y);
+                }
+                if (TT == 1) ask_base(0, after);
             }
-            const int done = strip;
-            strip += a.groups * kUpWaves;
-            if (strip * CT * 16 < a.n) ask();
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                if (sub + n * 16 + lane % 16 >= tile.count) continue;
-#pragma unroll
-                for (int g = 0; g < G; ++g) y[n][g].store((Y *)a.y + to[n], done * CT * 16 + g * 32 + lane / 16 * N, a.n);
-            }
+            strip = after;
+            if (!copy && J < 8) ask_b(strip);
         }
         __syncthreads();
     }
 }
 
+template <typename X, int NT, int NR> void ring_by(const AdapterArgs &a, unsigned blocks, hipStream_t stream)
+{
+    adapter_down_ring_kernel<X, NT, NR><<<blocks, kBlock, kDownWaves * ring_slots<X, NT, NR>() * ring_slot<X, NT, NR>(), stream>>>(a);
+}
+
 template <typename X> int down(const AdapterArgs &a, hipStream_t stream)
 {
     const unsigned blocks = (unsigned)a.tiles_most * (unsigned)a.splits * (unsigned)a.chunks;
-    const int shape = a.token_tiles * 10 + a.rank_tiles;
+    const int shape = (a.x_bytes ? 100 : 0) + a.token_tiles * 10 + a.rank_tiles;
     if (a.k < 16) adapter_down_kernel<X, 1, 1, true><<<blocks, kBlock, 0, stream>>>(a);
     else if (shape == 11) adapter_down_kernel<X, 1, 1, false><<<blocks, kBlock, 0, stream>>>(a);
     else if (shape == 12) adapter_down_kernel<X, 1, 2, false><<<blocks, kBlock, 0, stream>>>(a);
     else if (shape == 14) adapter_down_kernel<X, 1, 4, false><<<blocks, kBlock, 0, stream>>>(a);
     else if (shape == 21) adapter_down_kernel<X, 2, 1, false><<<blocks, kBlock, 0, stream>>>(a);
     else if (shape == 22) adapter_down_kernel<X, 2, 2, false><<<blocks, kBlock, 0, stream>>>(a);
-    else adapter_down_kernel<X, 2, 4, false><<<blocks, kBlock, 0, stream>>>(a);
+    else if (shape == 24) adapter_down_kernel<X, 2, 4, false><<<blocks, kBlock, 0, stream>>>(a);
+    else if (shape == 111) ring_by<X, 1, 1>(a, blocks, stream);
+    else if (shape == 112) ring_by<X, 1, 2>(a, blocks, stream);
+    else if (shape == 114) ring_by<X, 1, 4>(a, blocks, stream);
+    else if (shape == 121) ring_by<X, 2, 1>(a, blocks, stream);
+    else if (shape == 122) ring_by<X, 2, 2>(a, blocks, stream);
+    else if (shape == 124) ring_by<X, 2, 4>(a, blocks, stream);
+    else if constexpr (sizeof(X) == 4) return (int)hipErrorInvalidValue;
+    else if (shape == 141) ring_by<X, 4, 1>(a, blocks, stream);
+    else if (shape == 142) ring_by<X, 4, 2>(a, blocks, stream);
+    else if (shape == 144) ring_by<X, 4, 4>(a, blocks, stream);
+    else return (int)hipErrorInvalidValue;
     return (int)hipGetLastError();
 }
 
-template <typename Y, typename B, int NT, int CT> void up_by(const AdapterArgs &a, unsigned blocks, size_t lds, hipStream_t stream)
+template <typename Y, typename B, int N, int TT> void up_by(const AdapterArgs &a, unsigned blocks, size_t lds, hipStream_t stream)
 {
-    if (a.rank < 8) adapter_up_kernel<Y, B, NT, CT, 1, false, true><<<blocks, kBlock, lds, stream>>>(a);
-    else if (a.rank <= 64) adapter_up_kernel<Y, B, NT, CT, 2, false, false><<<blocks, kBlock, lds, stream>>>(a);
-    else adapter_up_kernel<Y, B, NT, CT, 8, false, false><<<blocks, kBlock, lds, stream>>>(a);
+    if (a.rank <= 32) adapter_up_kernel<Y, B, N, TT, 1, false, false><<<blocks, kBlock, lds, stream>>>(a);
+    else if (a.rank <= 64) adapter_up_kernel<Y, B, N, TT, 2, false, false><<<blocks, kBlock, lds, stream>>>(a);
+    else adapter_up_kernel<Y, B, N, TT, 8, false, false><<<blocks, kBlock, lds, stream>>>(a);
 }
 
 template <typename Y, typename B> void up(const AdapterArgs &a, hipStream_t stream)
 {
     const unsigned blocks = (unsigned)a.tiles_most * (unsigned)a.groups;
-    const size_t lds = a.count > 0 ? (size_t)2 * 16 * a.token_tiles * ((a.rank + 31) / 32 * 32 + 8) * sizeof(_Float16) : 0;
-    if (a.n < 8) adapter_up_kernel<Y, B, 1, 1, 8, true, true><<<blocks, kBlock, lds, stream>>>(a);
-    else if (a.token_tiles == 2) up_by<Y, B, 2, 4>(a, blocks, lds, stream);
-    else if (a.wide == 4) up_by<Y, B, 1, 4>(a, blocks, lds, stream);
-    else up_by<Y, B, 1, 1>(a, blocks, lds, stream);
+    const size_t lds = (size_t)2 * 16 * a.token_tiles * ((a.rank + 31) / 32 * 32 + 8) * sizeof(_Float16);
+    if (a.n < 2) adapter_up_kernel<Y, B, 2, 1, 8, true, true><<<blocks, kBlock, lds, stream>>>(a);
+    else if (a.rank < 8 && a.wide == 2) adapter_up_kernel<Y, B, 2, 1, 1, false, true><<<blocks, kBlock, lds, stream>>>(a);
+    else if (a.rank < 8) adapter_up_kernel<Y, B, 4, 2, 1, false, true><<<blocks, kBlock, lds, stream>>>(a);
+    else if (a.wide == 2) up_by<Y, B, 2, 1>(a, blocks, lds, stream);
+    else if (a.token_tiles == 1) up_by<Y, B, 4, 1>(a, blocks, lds, stream);
+    else if (a.token_tiles == 2) up_by<Y, B, 4, 2>(a, blocks, lds, stream);
+    else up_by<Y, B, 4, 4>(a, blocks, lds, stream);
 }
 
 }  // namespace
@@ -616,7 +778,7 @@ int launch_adapters(const AdapterArgs &a, void *stream)
 {
     const hipStream_t s = (hipStream_t)stream;
     if (a.count > 0) {
-        if (a.way == kList) adapter_group_kernel<<<1, kGroupThreads, (size_t)(a.count + 1) * sizeof(int), s>>>(a);
+        if (a.way == kList) adapter_group_kernel<<<1, kGroupThreads, (size_t)(a.count + 1) * kGroupWaves * sizeof(int), s>>>(a);
         const int err = a.x_type == 0 ? down<_Float16>(a, s) : a.x_type == 1 ? down<float>(a, s) : down<int8_t>(a, s);
         if (err != 0) return err;
     }

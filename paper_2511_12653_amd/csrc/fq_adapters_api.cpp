@@ -10,7 +10,7 @@ namespace fq {
 namespace {
 
 constexpr size_t kAlign = 256;
-constexpr long long kDownBlocks = 4 * kComputeUnits, kMostSplits = 8;      // blocks that the chip holds
+constexpr long long kMostSplits = 8;
 constexpr long long kUpWaves = 4 * kComputeUnits, kUpBlocks = 8 * kComputeUnits;
 
 fq_status validate(const fq_adapters &d)
@@ -44,6 +44,15 @@ long long at_most(long long v, long long most) { return v < most ? v : most; }
 long long at_least(long long v, long long least) { return v > least ? v : least; }
 long long ceiling(long long v, long long by) { return (v + by - 1) / by; }
 
+// Bytes of m rows of x where these and a's begin on 16-byte boundaries and have offsets of 32 bits (else 0).  (So rows end with 16 bytes, too.)
+unsigned fitting_bytes(const fq_adapters &d, long long m)
+{
+    const long long size = (long long)size_of(d.x_dtype);
+    if (!aligned(d.x, 16) || !aligned(d.a, 16) || d.ldx * size % 16 != 0 || d.k * (size < 2 ? size : 2) % 16 != 0 || d.k < 16 || d.ldx > (1LL << 31)) return 0;
+    const long long bytes = ((m - 1) * d.ldx + d.k) * size;
+    return bytes < (1LL << 32) - 4096 ? (unsigned)bytes : 0;
+}
+
 // How m tokens of the call are cut up.
 AdapterArgs plan_of(const fq_adapters &d, long long m)
 {
@@ -51,16 +60,18 @@ AdapterArgs plan_of(const fq_adapters &d, long long m)
     std::memset(&a, 0, sizeof a);
     a.m = (int)m; a.n = (int)d.n; a.k = (int)d.k; a.count = d.rank > 0 ? (int)d.count : 0; a.rank = (int)d.rank;
     a.pitch = (int)ceiling(d.rank, 16) * 16;
-    a.token_tiles = m >= 16LL * a.count && d.n >= 8 && d.k >= 16 ? 2 : 1;
+    a.x_bytes = fitting_bytes(d, m);
+    a.token_tiles = m < 16LL * a.count || d.k < 16 || d.n < 8 ? 1 : m < 64LL * a.count || d.rank > 128 || d.rank < 8 || d.x_dtype == FQ_F32 || !a.x_bytes ? 2 : 4;
     a.rank_tiles = d.rank <= 16 || d.k < 16 ? 1 : d.rank <= 32 ? 2 : 4;
     a.chunks = (int)ceiling(d.rank, 16 * a.rank_tiles);
     const long long tile = 16 * a.token_tiles, some = at_most(a.count + 1LL, m);
     a.way = m <= kWindow || a.count == 0 || a.count > kMostGrouped ? kWindows : m <= kSorted && a.count <= kSorted ? kSorting : kList;
     a.tiles_most = (int)(a.way != kWindows ? m / tile + some : ceiling(m, kWindow) * at_most(m, kWindow));
     const long long tiles = at_least(m / tile + at_most(a.count, m), 1) * at_least(a.chunks, 1);
-    // a block takes 256 values of k at a time
-    a.splits = (int)at_least(at_most(at_most(kDownBlocks / tiles, ceiling(d.k, 256)), kMostSplits), 1);
-    a.wide = a.token_tiles == 2 || (d.n >= 8 && tiles * ceiling(d.n, 64) > kUpWaves) ? 4 : 1;
+    // a block takes 256 values of k at a time; as many to a compute unit as have room for their rings
+    const long long slot = a.token_tiles * (long long)size_of(d.x_dtype) + a.rank_tiles * 2, room = at_most(at_least(18 / slot, 1), 4);
+    a.splits = (int)at_least(at_most(at_most(room * kComputeUnits / tiles, ceiling(d.k, 256)), kMostSplits), 1);
+    a.wide = d.n >= 4 && (a.token_tiles > 1 || tiles * ceiling(d.n, 64) > kUpWaves) ? 4 : 2;
     const long long strips = ceiling(d.n, 64 * a.wide);          // that a block of four wavefronts takes at a time
     a.groups = (int)at_least(at_most(strips, ceiling(kUpBlocks, a.tiles_most)), 1);
     return a;
@@ -96,6 +107,11 @@ AdapterArgs args_of(const fq_adapters &d, long long m, void *workspace)
     a.a = d.a; a.b = d.b; a.scale = d.scale;
     a.ldx = d.ldx; a.ldy = d.ldy; a.ldbase = d.ldbase;
     a.xs_step = d.xs_step; a.x_type = d.x_dtype; a.y16 = d.y_dtype == FQ_F16; a.base16 = d.base_dtype == FQ_F16;
+    if (!d.base) {
+        a.no_base = 1;
+        a.ldbase = a.ldy;
+        a.base16 = a.y16;
+    }
     return a;
 }
 
@@ -123,6 +139,7 @@ fq_status fq_adapters_forward(const fq_adapters *d, void *workspace, size_t ws_b
         a.ids = d->ids + row;
         a.base = d->base ? (const char *)d->base + (size_t)(row * d->ldbase) * fq::size_of(d->base_dtype) : nullptr;
         a.y = (char *)d->y + (size_t)(row * d->ldy) * fq::size_of(d->y_dtype);
+        if (a.no_base) a.base = a.y;
         if (fq::launch_adapters(a, hip_stream) != 0) return FQ_ERR_LAUNCH;
     }
     return FQ_OK;

@@ -120,8 +120,6 @@ constexpr int kDepth = 128;                                     // codes of a ro
 __device__ __forceinline__ int place_of(int chunk, int row) { return chunk ^ (row / 2 & 7); }      // (its own inverse in chunk)
 constexpr unsigned kNowhere = 0x7FFFFFF0u;                      // beyond the end of any buffer: reads as zeros
 
-#define FQ_LDS __attribute__((address_space(3)))
-
 struct Panel {                                                  // rows of one operand that a block multiplies
     const int8_t *at;
     unsigned bytes;                                             // from `at` to the end of the last row
@@ -130,15 +128,6 @@ struct Panel {                                                  // rows of one o
 __device__ __forceinline__ Panel panel(const int8_t *base, long long ld, int row0, int rows, int left, int k)
 {
     return {base + (long long)row0 * ld, (unsigned)(min(rows, left) - 1) * (unsigned)ld + (unsigned)k};
-}
-
-// 16 bytes per lane from `off` of a buffer to LDS, in lane order from `to` on (uniform).  No builtin: with one the compiler
-// waits for all such loads in front of a read of LDS wherever it loses sight of which array they go to.  The kernel
-// waits itself (loads_and_barrier); the compiler's own waits for other loads only become longer.
-__device__ __forceinline__ void load_lds(i32x4 buffer, unsigned off, int8_t *to)
-{
-    const unsigned at = (unsigned)(uintptr_t)(FQ_LDS int8_t *)to;
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(at), "v"(off), "s"(buffer) : "memory", "m0");
 }
 
 template <int N, int WAVES> struct Staging {                    // N wavefront loads of a panel per wavefront and step
@@ -447,12 +436,6 @@ __host__ __device__ constexpr FewLds few_lds(int m, int k, int size, bool shifte
     l.codes = size > 1 ? l.raw + m * l.raw_pitch : l.raw;
     l.total = l.codes + m * l.code_pitch + 32;                   // (a shifted last step reads 16 codes more)
     return l;
-}
-
-// The last LEFT loads of this wavefront may be on their way, all others and all its LDS reads are done.
-template <int LEFT> __device__ __forceinline__ void loads_but()
-{
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(LEFT) : "memory");
 }
 
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); }

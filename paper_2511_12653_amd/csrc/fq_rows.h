@@ -1,4 +1,4 @@
-// Device helpers of the kernels that work on rows of values: loads of eight at any address, and the codes of a row.  Included by
+// Device helpers of the kernels that work on rows of values: loads of eight at any address, the codes of a row, and loads straight into LDS.  Included by
 // .hip files only; not part of the C ABI.
 #pragma once
 #include "fq_device.h"
@@ -108,6 +108,23 @@ template <typename T> __device__ __forceinline__ u32x2 codes8(const Eight<T> &r,
     u32x2 w = u32x2{pack(b[0], b[1], b[2], b[3]), pack(b[4], b[5], b[6], b[7])};
     if (none || scale.inverse == 0.0f) w = (u32x2)0u;
     return w;
+}
+
+#define FQ_LDS __attribute__((address_space(3)))
+
+// 16 bytes per lane from `off` of a buffer to LDS, in lane order from `to` on (uniform).  No builtin: with one the compiler
+// waits for all such loads in front of a read of LDS wherever it loses sight of which array they go to.  The kernel
+// waits itself (as by loads_but); the compiler's own waits for other loads only become longer.
+__device__ __forceinline__ void load_lds(i32x4 buffer, unsigned off, int8_t *to)
+{
+    const unsigned at = (unsigned)(uintptr_t)(FQ_LDS int8_t *)to;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(at), "v"(off), "s"(buffer) : "memory", "m0");
+}
+
+// The last LEFT loads of this wavefront may be on their way, all others and all its LDS reads are done.
+template <int LEFT> __device__ __forceinline__ void loads_but()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" : : "n"(LEFT) : "memory");
 }
 
 }  // namespace dev
