@@ -10,8 +10,8 @@ constexpr long long kAdaptersMostWidth = 1LL << 20;
 constexpr int kAdaptersMostRank = 256;
 constexpr int kWindow = 64;                      // tokens that a wavefront sorts out by itself
 constexpr long long kAdaptersMostTokens = 1 << 16;       // of a launch
-constexpr int kSorted = 1024;                    // tokens (and adapters) that a block sorts out by itself
-constexpr int kMostGrouped = 1024;               // adapters that tokens are grouped by
+constexpr int kSorted = 1024;                    // tokens that a block sorts out by itself
+constexpr int kMostGrouped = 1024;               // adapters that tokens are sorted by
 
 enum AdapterWay { kWindows, kSorting, kList };   // how a block comes to its tokens
 
@@ -35,7 +35,7 @@ struct AdapterArgs {
     int pitch;                 // of a row of t: whole 16 values
     int way;                   // AdapterWay
     int tiles_most;            // tiles there can be
-    int token_tiles;           // tokens of a tile in 16s: 1, 2 or 4
+    int token_tiles;           // tokens of a tile in 16s: 1, 2 or (with rank_tiles 4, FP16 and codes that fit) 4
     int rank_tiles;            // ranks of a block in 16s: 1, 2 or 4
     int splits, chunks;        // parts of k; of the ranks
     int wide, groups;          // channels of a wavefront at a time in 16s: 2 or 4; blocks that share a tile's channels

@@ -745,8 +745,6 @@ template <typename X> int down(const AdapterArgs &a, hipStream_t stream)
     else if (shape == 122) ring_by<X, 2, 2>(a, blocks, stream);
     else if (shape == 124) ring_by<X, 2, 4>(a, blocks, stream);
     else if constexpr (sizeof(X) == 4) return (int)hipErrorInvalidValue;
-    else if (shape == 141) ring_by<X, 4, 1>(a, blocks, stream);
-    else if (shape == 142) ring_by<X, 4, 2>(a, blocks, stream);
     else if (shape == 144) ring_by<X, 4, 4>(a, blocks, stream);
     else return (int)hipErrorInvalidValue;
     return (int)hipGetLastError();
@@ -769,7 +767,7 @@ template <typename Y, typename B> void up(const AdapterArgs &a, hipStream_t stre
     else if (a.wide == 2) up_by<Y, B, 2, 1>(a, blocks, lds, stream);
     else if (a.token_tiles == 1) up_by<Y, B, 4, 1>(a, blocks, lds, stream);
     else if (a.token_tiles == 2) up_by<Y, B, 4, 2>(a, blocks, lds, stream);
-    else up_by<Y, B, 4, 4>(a, blocks, lds, stream);
+    else adapter_up_kernel<Y, B, 4, 4, 2, false, false><<<blocks, kBlock, lds, stream>>>(a);
 }
 
 }  // namespace

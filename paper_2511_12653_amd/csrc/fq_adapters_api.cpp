@@ -10,8 +10,7 @@ namespace fq {
 namespace {
 
 constexpr size_t kAlign = 256;
-constexpr long long kMostSplits = 8;
-constexpr long long kUpWaves = 4 * kComputeUnits, kUpBlocks = 8 * kComputeUnits;
+constexpr long long kMostSplits = 8, kUpBlocks = 4 * kComputeUnits;
 
 fq_status validate(const fq_adapters &d)
 {
@@ -53,7 +52,11 @@ unsigned fitting_bytes(const fq_adapters &d, long long m)
     return bytes < (1LL << 32) - 4096 ? (unsigned)bytes : 0;
 }
 
-// How m tokens of the call are cut up.
+// How m tokens of the call are cut up.  Tiles of 32 tokens read the adapters half as often as those of 16, but leave compute units without
+// work where there are few (us, 4096 x 4096 by 16 ranks, 4 adapters, tiles of 16 / 32 / 64: 512 tokens 15.4 / 16.9 / 27, 2048 tokens 28.4 / 26.0 / 33,
+// 8192 tokens 76 / 65.8 / 66.7); those of 64 pay where an adapter has many bytes (8192 tokens, 64 ranks: 144 / 87 / 80.5).  k goes in as
+// many parts as make a block for each compute unit (512 tokens: 15.4 in eight parts, 21 in one), channels in as many groups as make four
+// (2048 tokens: 26.0 in eight, 29 in four).
 AdapterArgs plan_of(const fq_adapters &d, long long m)
 {
     AdapterArgs a;
@@ -61,19 +64,20 @@ AdapterArgs plan_of(const fq_adapters &d, long long m)
     a.m = (int)m; a.n = (int)d.n; a.k = (int)d.k; a.count = d.rank > 0 ? (int)d.count : 0; a.rank = (int)d.rank;
     a.pitch = (int)ceiling(d.rank, 16) * 16;
     a.x_bytes = fitting_bytes(d, m);
-    a.token_tiles = m < 16LL * a.count || d.k < 16 || d.n < 8 ? 1 : m < 64LL * a.count || d.rank > 128 || d.rank < 8 || d.x_dtype == FQ_F32 || !a.x_bytes ? 2 : 4;
+    const bool large = a.x_bytes > 0 && d.x_dtype != FQ_F32 && d.rank > 32 && d.rank <= 64 && m >= 64LL * a.count && m >= 4096;
+    a.token_tiles = m < 1024 || m < 16LL * a.count || d.k < 16 || d.n < 4 ? 1 : large ? 4 : 2;
     a.rank_tiles = d.rank <= 16 || d.k < 16 ? 1 : d.rank <= 32 ? 2 : 4;
     a.chunks = (int)ceiling(d.rank, 16 * a.rank_tiles);
     const long long tile = 16 * a.token_tiles, some = at_most(a.count + 1LL, m);
-    a.way = m <= kWindow || a.count == 0 || a.count > kMostGrouped ? kWindows : m <= kSorted && a.count <= kSorted ? kSorting : kList;
+    a.way = m <= kWindow || a.count == 0 || a.count > kMostGrouped ? kWindows : m <= kSorted ? kSorting : kList;
     a.tiles_most = (int)(a.way != kWindows ? m / tile + some : ceiling(m, kWindow) * at_most(m, kWindow));
-    const long long tiles = at_least(m / tile + at_most(a.count, m), 1) * at_least(a.chunks, 1);
-    // a block takes 256 values of k at a time; as many to a compute unit as have room for their rings
-    const long long slot = a.token_tiles * (long long)size_of(d.x_dtype) + a.rank_tiles * 2, room = at_most(at_least(18 / slot, 1), 4);
-    a.splits = (int)at_least(at_most(at_most(room * kComputeUnits / tiles, ceiling(d.k, 256)), kMostSplits), 1);
-    a.wide = d.n >= 4 && (a.token_tiles > 1 || tiles * ceiling(d.n, 64) > kUpWaves) ? 4 : 2;
+    const long long tiles = at_least(m / tile + at_most(a.count, m), 1), parts = tiles * at_least(a.chunks, 1);
+    a.splits = (int)at_least(at_most(at_most((kComputeUnits + parts / 2) / parts, ceiling(d.k, 256)), kMostSplits), 1);
+    a.wide = d.n >= 4 && (a.token_tiles > 1 || tiles * ceiling(d.n, 64) > kUpBlocks) ? 4 : 2;
     const long long strips = ceiling(d.n, 64 * a.wide);          // that a block of four wavefronts takes at a time
-    a.groups = (int)at_least(at_most(strips, ceiling(kUpBlocks, a.tiles_most)), 1);
+    a.groups = 1;
+    while (a.groups * tiles < kUpBlocks && a.groups < strips) a.groups *= 2;
+    if (a.groups > strips) a.groups = (int)strips;
     return a;
 }
 
