@@ -150,7 +150,7 @@ __global__ __launch_bounds__(kGroupThreads) void adapter_group_kernel(AdapterArg
 // The tile of a block: its adapter (-1: none) and its tokens, which go to `tokens`.  Three ways:
 //   windows   up to kWindow tokens (or windows of so many): those that have the adapter of token `slot` of theirs, if that is the first to have
 //             it; so every adapter of the window has one block, which takes them by tiles one after the other
-//   sorting   up to kSorted tokens and adapters: the block counts the tokens of each adapter by itself, which costs less than a launch in
+//   sorting   up to kSorted tokens: the block counts the tokens of each adapter by itself, which costs less than a launch in
 //             front and the two trips to memory for its results
 //   list      tile and tokens are what adapter_group_kernel has written
 struct Tile {
@@ -159,7 +159,7 @@ struct Tile {
 
 struct Finding {
     int tokens[kWindow];
-    int counts[kSorted + 1];
+    int counts[kMostGrouped + 1];
     int sums[2][kBlock / 64], parts[kSorted / 64];
     Tile tile;
     int first;
@@ -189,8 +189,16 @@ __device__ __forceinline__ Tile find_tile(const AdapterArgs &a, int index, Findi
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < kIds; ++j) {
-            const unsigned long long mine = peers(id[j], j * kBlock + thread < a.m);
-            if ((mine >> lane & 1) && before(mine, lane) == 0) atomicAdd(s.counts + id[j], __popcll(mine));
+            // (tokens of one request come one after the other: then the wavefront counts once)
+            const bool some = j * kBlock + thread < a.m;
+            const unsigned long long mine = __ballot(some);
+            if (mine == 0) continue;
+            const int leader = __builtin_amdgcn_readlane(id[j], __builtin_ctzll(mine));
+            if (__ballot(some && id[j] == leader) == mine) {
+                if (lane == 0) atomicAdd(s.counts + leader, __popcll(mine));
+            } else if (some) {
+                atomicAdd(s.counts + id[j], 1);
+            }
         }
         __syncthreads();
         const int each = (groups + kBlock - 1) / kBlock, begin = min(thread * each, groups), end = min(begin + each, groups);
@@ -218,13 +226,15 @@ __device__ __forceinline__ Tile find_tile(const AdapterArgs &a, int index, Findi
         __syncthreads();
         int place = -s.first;
 #pragma unroll
-        for (int j = 0; j < kIds; ++j)
+        for (int j = 0; j < kIds; ++j) {
+            if (j * kBlock >= a.m || place >= t.count) continue;
 #pragma unroll
             for (int w = 0; w < kBlock / 64; ++w) {
                 const int own = place + before(mine[j], lane);
                 if (w == wave && (mine[j] >> lane & 1) && own >= 0 && own < t.count) s.tokens[own] = j * kBlock + thread;
                 place += s.parts[j * (kBlock / 64) + w];
             }
+        }
     } else {
         const AdapterTile f = a.tiles[index];
         t = {f.id, f.count};

@@ -106,7 +106,9 @@ int parts_of(const fq_norm &d)
     const bool held = d.width <= kNormHeldWidth;
     if (held && groups <= kAloneGroups) return 1;
     const long long strips = held ? 1 : (d.width + kNormStrip - 1) / kNormStrip;
-    const long long chip = held ? (long long)s.blocks * kComputeUnits : strips < 2 * kComputeUnits ? 2 * kComputeUnits / strips : 1;
+    long long chip = held ? (long long)s.blocks * kComputeUnits : strips < 2 * kComputeUnits ? 2 * kComputeUnits / strips : 1;
+    // (a part of a wide row's width is as much to write, and to read again, as two or three rows: 403 x 4096 FP16 13.2 us in 128 parts, 17.7 in 403)
+    if (held && s.rows() == 1 && groups / 3 < chip) chip = groups / 3 > 128 ? groups / 3 : 128;
     const long long parts = groups < chip ? groups : least > chip ? least : chip, most = kMostParts / strips;
     return (int)(parts < most ? parts : most);
 }
