@@ -4,7 +4,9 @@
 `binding` (thin ctypes marshalling onto the C-ABI library built from csrc/); it is imported
 on first use and raises if the compiled library is missing -- there is no CPU fallback.
 `fake_quantize` (module `autograd`) wraps the forward and backward calls in a torch.autograd Function, `linear_int8` (module
-`linear`) the int8 linear layer, `AdamW` (module `optim`) the multi-tensor AdamW step in a torch.optim.Optimizer.
+`linear`) the int8 linear layer, `AdamW` (module `optim`) the multi-tensor AdamW step in a torch.optim.Optimizer, `layer_norm` and
+`layer_norm_int8` (module `norm`) layer norm, `dropout` (module `drop`) dropout whose mask is never stored, `add_adapters` (module
+`adapters`) the low-rank adapters beside a shared layer.
 """
 from . import workloads  # noqa: F401
 
@@ -17,7 +19,8 @@ _API = ("fq_forward", "fq_backward", "fq_multi_tensor", "fq_workspace_bytes", "f
         "FQ_F16", "FQ_F32", "FQ_FLAG_NO_DX", "FQ_FLAG_TWO_PASS", "FQ_FLAG_NO_POLL", "FQ_MODE_FORWARD", "FQ_MODE_BACKWARD")
 
 
-_FRONT_DOORS = {"fake_quantize": "autograd", "linear_int8": "linear", "AdamW": "optim"}
+_FRONT_DOORS = {"fake_quantize": "autograd", "linear_int8": "linear", "AdamW": "optim", "layer_norm": "norm",
+                "layer_norm_int8": "norm", "dropout": "drop", "add_adapters": "adapters"}
 
 
 def __getattr__(name):
