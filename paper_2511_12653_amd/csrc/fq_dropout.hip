@@ -2,9 +2,9 @@
 //
 //   y_i = (h_i >> 1 >= round(p 2^31) ? x_i / (1 - p) : 0) + residual_i,   h_i a hash of i under two keys of seed and step
 //
-// Bound by memory: x (and the residual) are read once, y is written once.  The hash is two 32-bit products, which take four times
-// the cycles of other instructions, and six of those: about 60 cycles of a SIMD for a wavefront's 64 elements, where memory takes 110
-// (FP16 in and out) and more.
+// Bound by memory: x (and the residual) are read once, y is written once: 36.9M FP16 values with a residual (221 MB) take 39 us, 5.6 TB/s.
+// The hash is two 32-bit products and six other instructions, all at the full rate; with the rest an element costs some fifteen, which
+// are 480 cycles of a SIMD for a wavefront's 512 elements, where memory takes 1350 (FP16 with a residual).
 #include "fq_dropout.h"
 #include "fq_rows.h"
 
@@ -49,9 +49,10 @@ template <typename T> __device__ __forceinline__ Eight<T> ask(const T *p)
     return r;
 }
 
-// A thread has V vectors of eight elements, 256 vectors apart; a block a run of 2048 V elements, all with the same upper 32
-// bits of their places.
-constexpr int kVecs = 2, kBlockElems = 256 * 8 * kVecs;
+// A thread has eight neighbouring elements, a block a run of 2048, all with the same upper 32 bits of their places.  (The 221 MB above:
+// 39.2 us; 40.2 with sixteen elements a thread, 42.4 with 32; 41 to 43 with 1024 to 4096 blocks that go from run to run.  Stores
+// past the caches make it 37.6, but then who reads y pays: a layer norm of the result of 16384 x 4096 128 us with it, 123 without.)
+constexpr int kBlockElems = 256 * 8;
 
 template <typename X, typename Y, bool ADD> __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a)
 {
@@ -64,35 +65,23 @@ template <typename X, typename Y, bool ADD> __global__ __launch_bounds__(256) vo
     const Keys keys = keys_of(a.seed, step, (unsigned)((uint64_t)begin >> 32));
     const unsigned place = (unsigned)begin;
     const int left = a.n - begin < kBlockElems ? (int)(a.n - begin) : kBlockElems;
-    Eight<X> vx[kVecs];
-    Eight<Y> vr[kVecs];
+    const int at = (int)threadIdx.x * 8;
+    if (at + 8 <= left) {
+        const auto from = __builtin_bit_cast(typename Values<X>::type, ask(x + at));
+        typename Values<Y>::type to;
+        if constexpr (ADD) to = __builtin_bit_cast(typename Values<Y>::type, ask(r + at));
 #pragma unroll
-    for (int j = 0; j < kVecs; ++j) {
-        const int at = (j * 256 + (int)threadIdx.x) * 8;
-        if (at + 8 > left) continue;
-        vx[j] = ask(x + at);
-        if constexpr (ADD) vr[j] = ask(r + at);
-    }
-#pragma unroll
-    for (int j = 0; j < kVecs; ++j) {
-        const int at = (j * 256 + (int)threadIdx.x) * 8;
-        if (at + 8 <= left) {
-            const auto from = __builtin_bit_cast(typename Values<X>::type, vx[j]);
-            typename Values<Y>::type to;
-            if constexpr (ADD) to = __builtin_bit_cast(typename Values<Y>::type, vr[j]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float v = bits_of(place + at + e, keys) >= a.threshold ? scaled((float)from[e], a.scale) : 0.0f;
-                if constexpr (ADD) v += (float)to[e];
-                to[e] = (Y)v;
-            }
-            __builtin_memcpy((FQ_GLOBAL Y *)(y + at), &to, sizeof to);
-        } else {
-            for (int i = at; i < left; ++i) {
-                float v = bits_of(place + i, keys) >= a.threshold ? scaled((float)ld_global(x + i), a.scale) : 0.0f;
-                if constexpr (ADD) v += (float)ld_global(r + i);
-                st_global(y + i, (Y)v);
-            }
+        for (int e = 0; e < 8; ++e) {
+            float v = bits_of(place + at + e, keys) >= a.threshold ? scaled((float)from[e], a.scale) : 0.0f;
+            if constexpr (ADD) v += (float)to[e];
+            to[e] = (Y)v;
+        }
+        __builtin_memcpy((FQ_GLOBAL Y *)(y + at), &to, sizeof to);
+    } else {
+        for (int i = at; i < left; ++i) {
+            float v = bits_of(place + i, keys) >= a.threshold ? scaled((float)ld_global(x + i), a.scale) : 0.0f;
+            if constexpr (ADD) v += (float)ld_global(r + i);
+            st_global(y + i, (Y)v);
         }
     }
 }
