@@ -10,7 +10,7 @@ namespace fq {
 namespace {
 
 constexpr size_t kAlign = 256;
-constexpr long long kMostSplits = 8, kUpBlocks = 4 * kComputeUnits;
+constexpr long long kMostSplits = 8;
 
 fq_status validate(const fq_adapters &d)
 {
@@ -55,8 +55,9 @@ unsigned fitting_bytes(const fq_adapters &d, long long m)
 // How m tokens of the call are cut up.  Tiles of 32 tokens read the adapters half as often as those of 16, but leave compute units without
 // work where there are few (us, 4096 x 4096 by 16 ranks, 4 adapters, tiles of 16 / 32 / 64: 512 tokens 15.4 / 16.9 / 27, 2048 tokens 28.4 / 26.0 / 33,
 // 8192 tokens 76 / 65.8 / 66.7); those of 64 pay where an adapter has many bytes (8192 tokens, 64 ranks: 144 / 87 / 80.5).  k goes in as
-// many parts as make a block for each compute unit (512 tokens: 15.4 in eight parts, 21 in one), channels in as many groups as make four
-// (2048 tokens: 26.0 in eight, 29 in four).
+// many parts as make a block for each compute unit (512 tokens: 15.4 in eight parts, 21 in one).  Channels go in as many
+// groups as make two blocks for each, and up to eight as long as a wavefront has two strips one after the other (us, in 4 / 8 / 16 / 32 groups:
+// 512 tokens 18 / 15.5 / 14.9 / 15; 2048 tokens 29.6 / 27.1 / 29.2 / 29.2; 8192 x 8192 by 64 ranks 132 / 124.6 / 122 / 130).
 AdapterArgs plan_of(const fq_adapters &d, long long m)
 {
     AdapterArgs a;
@@ -73,10 +74,11 @@ AdapterArgs plan_of(const fq_adapters &d, long long m)
     a.tiles_most = (int)(a.way != kWindows ? m / tile + some : ceiling(m, kWindow) * at_most(m, kWindow));
     const long long tiles = at_least(m / tile + at_most(a.count, m), 1), parts = tiles * at_least(a.chunks, 1);
     a.splits = (int)at_least(at_most(at_most((kComputeUnits + parts / 2) / parts, ceiling(d.k, 256)), kMostSplits), 1);
-    a.wide = d.n >= 4 && (a.token_tiles > 1 || tiles * ceiling(d.n, 64) > kUpBlocks) ? 4 : 2;
+    a.wide = d.n >= 4 && (a.token_tiles > 1 || tiles * ceiling(d.n, 64) > 4 * kComputeUnits) ? 4 : 2;
     const long long strips = ceiling(d.n, 64 * a.wide);          // that a block of four wavefronts takes at a time
     a.groups = 1;
-    while (a.groups * tiles < kUpBlocks && a.groups < strips) a.groups *= 2;
+    while ((a.groups * tiles < 2 * kComputeUnits && a.groups < strips) || (a.groups * tiles < 8 * kComputeUnits && a.groups * 4 <= strips))
+        a.groups *= 2;
     if (a.groups > strips) a.groups = (int)strips;
     return a;
 }
