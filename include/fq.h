@@ -397,8 +397,8 @@ fq_status fq_linear_forward(const fq_linear *d, void *workspace, size_t ws_bytes
  * what stands in front of a quantized layer.
  *   mean = (sum of x) / width,  rstd = 1 / sqrt((sum of (x - mean)^2) / width + eps),  h = (x - mean) * rstd
  *   y = h * weight + bias
- * The sums of a row are binary64; mean and rstd are rounded to binary32 once and the rest is binary32, but where y is
- * codes (y_dtype FQ_I8): there y is worked out in binary64, rounded to binary32 once, and quantized as fq_linear
+ * The sums of a row are binary64; mean (as two binary32 numbers, for y), rstd and all that follows are binary32, but where
+ * y is codes (y_dtype FQ_I8): there y is worked out in binary64, rounded to binary32 once, and quantized as fq_linear
  * quantizes FP32 rows:  ys = max|y| / 127,  code = clip(round(y / ys), -127, 127).
  * A row with a NaN or an infinity gives a row of NaN (codes 0, scale NaN).  Where all values of a row are equal and eps is
  * 0, rstd is infinite and the row NaN.
@@ -407,8 +407,8 @@ fq_status fq_linear_forward(const fq_linear *d, void *workspace, size_t ws_bytes
  *   gweight = sum over rows of gy * h,  gbias = sum over rows of gy      (rounded to w_dtype once)
  * No float atomics: sums are in a fixed order, results the same bit for bit from run to run.
  * Rows may lie any distance apart and at any address that their type allows.  y may be exactly x, gx exactly x or gy (same
- * type and distance).  Forward one launch, backward one or two (wide rows: three).  The workspace of the backward pass need not be initialised and may be
- * shared by calls that do not overlap in time.
+ * type and distance).  Forward one launch, backward one or two (with rows of more than 16384 values: up to three).  The
+ * workspace of the backward pass need not be initialised and may be shared by calls that do not overlap in time.
  */
 typedef struct fq_norm {
     int64_t rows, width;              /* any may be 0; width <= 2^24 */
@@ -462,11 +462,14 @@ fq_status fq_dropout(const fq_dropout_args *d, void *hip_stream);
  * request is added to its output):
  *   t[i][l] = (sum over j of x[i][j] * a[ids[i]][l][j]) (* xs[i]),   l < rank
  *   y[i][j] = base[i][j] + scale[ids[i]] * (sum over l of t[i][l] * b[ids[i]][j][l])
- * All sums and t are binary32 or better, y is rounded to its type once.  Tokens come in any order; ids outside [0, count)
- * mean no adapter (y = base).  A token's NaN or infinity stays in its row, an adapter's with its tokens.
+ * Products of FP16 values and codes are exact, those of FP32 tokens binary32; sums are binary32, in a fixed order.  t goes
+ * into its products as two FP16 numbers: 22 bits of each, or 2^-39 of the greatest of a token's t.  y is rounded to its type
+ * once.  Tokens come in any order; ids outside [0, count) mean no adapter (y = base).  A token's NaN or infinity stays in
+ * its row, an adapter's with its tokens.
  * Rows of x, base and y may lie any distance apart and at any address that their type allows; a and b are contiguous.
- * y may be exactly base (same type and distance).  Two launches.  The workspace need not be initialised and may be shared by
- * calls that do not overlap in time.  There is no backward pass.
+ * y may be exactly base (same type and distance).  Two launches, three with more than 1024 tokens and up to 1024 adapters;
+ * so many per 65536 tokens.  The workspace need not be initialised and may be shared by calls that do not overlap in time.
+ * There is no backward pass.
  */
 typedef struct fq_adapters {
     int64_t m, n, k;                  /* tokens, output channels, values per token; any may be 0; k and n <= 2^20 */
