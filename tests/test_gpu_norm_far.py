@@ -1,0 +1,131 @@
+"""Layer norm at its largest: rows far apart, more than 2^32 values, the widest rows, many parts; against the plain implementation in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2511_12653_amd import binding as fq
+
+import _gpu_harness as H
+import _more_operators_ref as R
+from test_gpu_norm import EPS, check_backward, check_forward, rng_of, tokens
+
+pytestmark = pytest.mark.gpu
+host = lambda t: t.cpu().numpy()     # noqa: E731
+
+
+def both(x, gy, w, y, gx, out_type=torch.float32):
+    """(stats, scales, gweight, gbias) of a forward pass into y and a backward pass into gx."""
+    rows, width = x.shape
+    stats, ys = torch.empty((rows, 2), device="cuda"), torch.empty(rows, device="cuda") if y.dtype == torch.int8 else None
+    gw, gb = torch.empty(width, device="cuda", dtype=out_type), torch.empty(width, device="cuda", dtype=out_type)
+    fq.fq_norm_forward(fq.FqNorm.from_torch(x, y=y, weight=w, y_scale=ys, stats=stats, eps=EPS))
+    d = fq.FqNorm.from_torch(x, weight=w, stats=stats, gy=gy, gx=gx, gweight=gw, gbias=gb, eps=EPS)
+    fq.fq_norm_backward(d, torch.empty(fq.fq_norm_workspace_bytes(d), dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    return stats, ys, gw, gb
+
+
+@pytest.mark.parametrize("width", [5, 384, 5000, 20000])
+def test_rows_far_apart(width):
+    rows, pitch = 2100, (1 << 20) + 8
+    rng = rng_of(20, width)
+    x, gy, w = tokens(rng, rows, width, np.float16), tokens(rng, rows, width, np.float16), (1 + 0.2 * rng.standard_normal(width)).astype(np.float32)
+    far = [torch.zeros((rows, pitch), dtype=torch.float16, device="cuda")[:, s:s + width] for s in (8, 16, 3, 1)]
+    far[0].copy_(H.dev(x))
+    far[1].copy_(H.dev(gy))
+    stats, _, gw, gb = both(far[0], far[1], H.dev(w), far[2], far[3])
+    y, off, _, _ = R.norm(x, w, None, EPS)
+    R.check(host(far[2]), y, off, True)
+    s = host(stats)
+    want = R.norm_backward(x, gy, w, s[:, 0], s[:, 1])
+    for name, got in (("gx", host(far[3])), ("gweight", host(gw)), ("gbias", host(gb))):
+        R.check(got, *want[name], got.dtype == np.float16, name)
+
+
+def test_more_than_32_bits_of_values():
+    """2^26 + 5 rows of 72 values, 4.8e9 of them, of which a few rows are looked at; columns against sums in 64 bits."""
+    rows, width = (1 << 26) + 5, 72
+    x, gy = torch.empty((rows, width), dtype=torch.float16, device="cuda"), torch.empty((rows, width), dtype=torch.float16, device="cuda")
+    step = 1 << 22
+    for i in range(0, rows, step):
+        gen = torch.Generator(device="cuda").manual_seed(i)
+        for t in (x, gy):
+            t[i:i + step] = torch.randn((min(step, rows - i), width), device="cuda", generator=gen).half()
+    w = 1 + 0.2 * torch.randn(width, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    y, gx = torch.empty_like(x), torch.empty_like(x)
+    stats, _, gw, gb = both(x, gy, w, y, gx)
+    look = torch.tensor([0, 1, 12345678, (1 << 32) // 72 - 1, (1 << 32) // 72, (1 << 32) // 72 + 1, rows - 2, rows - 1], device="cuda")
+    rows_x, rows_g = host(x[look]), host(gy[look])
+    value, off, _, _ = R.norm(rows_x, host(w), None, EPS)
+    R.check(host(y[look]), value, off, True)
+    s = host(stats[look])
+    value, off = R.norm_backward(rows_x, rows_g, host(w), s[:, 0], s[:, 1])["gx"]
+    R.check(host(gx[look]), value, off, True)
+    sums = torch.zeros((4, width), dtype=torch.float64, device="cuda")
+    for i in range(0, rows, step):
+        g, h = gy[i:i + step].double(), (x[i:i + step].double() - stats[i:i + step, :1].double()) * stats[i:i + step, 1:].double()
+        sums += torch.stack([(g * h).sum(0), g.sum(0), (g * h).abs().sum(0), g.abs().sum(0)])
+    sums = host(sums)
+    # up to 256 rows to a part in binary32, over 16 row groups, and the products: as for fewer rows
+    R.check(host(gw), sums[0], 267 * R.U32 * sums[2], False, "gweight")
+    R.check(host(gb), sums[1], 264 * R.U32 * sums[3], False, "gbias")
+
+
+@pytest.mark.parametrize("width", [(1 << 20) + 3, 1 << 24])
+def test_widest_rows(width):
+    rng = rng_of(21, width)
+    x, gy = tokens(rng, 2, width, np.float16), tokens(rng, 2, width, np.float16)
+    w = (1 + 0.2 * rng.standard_normal(width)).astype(np.float16)
+    for y_type in (np.float16, np.int8):
+        check_forward(x, w, None, y_type, str(width))
+    check_backward(x, gy, w, str(width), w_type=np.float16)
+
+
+@pytest.mark.parametrize("width,rows", [(3, 300000), (8, 2000003), (40, 700001), (16400, 3000)])
+def test_many_parts(width, rows):
+    rng = rng_of(22, width)
+    x, gy = tokens(rng, rows, width, np.float16), tokens(rng, rows, width, np.float32)
+    check_backward(x, gy, None, "%d x %d" % (rows, width))
+
+
+def test_two_graphs_of_one_workspace():
+    """Captured passes that use one workspace, one after the other, give what eager ones give, in every replay."""
+    sizes = ((5000, 200), (300, 4096), (2, 20000))
+    given = [[torch.randn(s, device="cuda").half() for _ in range(2)] for s in sizes]
+    outs, ds = [], []
+    for x, gy in given:
+        stats = torch.empty((x.shape[0], 2), device="cuda")
+        out = [torch.empty_like(x), torch.empty_like(x), torch.empty(x.shape[1], device="cuda"), torch.empty(x.shape[1], device="cuda")]
+        outs.append(out)
+        ds.append((fq.FqNorm.from_torch(x, y=out[0], stats=stats, eps=EPS), fq.FqNorm.from_torch(x, stats=stats, gy=gy, gx=out[1], gweight=out[2], gbias=out[3], eps=EPS)))
+    ws = torch.empty(max(fq.fq_norm_workspace_bytes(d) for _, d in ds), dtype=torch.uint8, device="cuda")
+
+    def run(d):
+        fq.fq_norm_forward(d[0])
+        fq.fq_norm_backward(d[1], ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graphs = [torch.cuda.CUDAGraph() for _ in ds]
+    for d in ds:
+        run(d)
+    torch.cuda.synchronize()
+    for graph, d in zip(graphs, ds):
+        with torch.cuda.graph(graph, stream=side):
+            run(d)
+    for seed in range(4):
+        torch.manual_seed(seed)
+        for x, gy in given:
+            x.normal_()
+            gy.normal_()
+        for d in ds:
+            run(d)
+        want = [[t.clone() for t in out] for out in outs]
+        for out in outs:
+            for t in out:
+                t.fill_(7)
+        ws.fill_(0xFF)
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(s, t) for a, b in zip(outs, want) for s, t in zip(a, b))
