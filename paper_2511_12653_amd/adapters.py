@@ -30,6 +30,8 @@ def add_adapters(base, x, ids, a, b, scale=None, x_scale=None, out=None, out_dty
     if ids.dtype.is_floating_point or ids.dtype == torch.bool:
         raise TypeError("ids must be whole numbers")
     m, k, n = x.shape[:-1].numel(), x.shape[-1], b.shape[1]
+    if ids.shape != x.shape[:-1] and ids.shape != (m,):
+        raise ValueError("ids %s are not one for each of x's %s tokens" % (tuple(ids.shape), tuple(x.shape[:-1])))
     if ids.dtype != torch.int32:               # (an int64 that is none of the adapters must not become one)
         ids = ids.long().clamp(-1, a.shape[0]).to(torch.int32)
     if out is None:

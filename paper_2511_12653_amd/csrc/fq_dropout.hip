@@ -53,10 +53,12 @@ template <typename T> __device__ __forceinline__ Eight<T> ask(const T *p)
 // 39.2 us; 40.2 with sixteen elements a thread, 42.4 with 32; 41 to 43 with 1024 to 4096 blocks that go from run to run.  Stores
 // past the caches make it 37.6, but then who reads y pays: a layer norm of the result of 16384 x 4096 128 us with it, 123 without.)
 constexpr int kBlockElems = 256 * 8;
+constexpr unsigned kMostAcross = 1u << 23;         // blocks along x: a grid has fewer than 2^32 threads along each of its sides
 
 template <typename X, typename Y, bool ADD> __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a)
 {
-    const long long begin = (long long)blockIdx.x * kBlockElems;
+    const long long begin = (long long)(blockIdx.y * gridDim.x + blockIdx.x) * kBlockElems;
+    if (begin >= a.n) return;
     const X *x = (const X *)a.x + begin;
     const Y *r = (const Y *)a.residual + begin;
     Y *y = (Y *)a.y + begin;
@@ -88,7 +90,8 @@ template <typename X, typename Y, bool ADD> __global__ __launch_bounds__(256) vo
 
 template <typename X, typename Y> int dropout(const DropoutArgs &a, hipStream_t stream)
 {
-    const unsigned blocks = (unsigned)((a.n + kBlockElems - 1) / kBlockElems);
+    const unsigned runs = (unsigned)((a.n + kBlockElems - 1) / kBlockElems);       // 2^24 at most
+    const dim3 blocks(runs < kMostAcross ? runs : kMostAcross, (runs + kMostAcross - 1) / kMostAcross);
     if (a.residual) dropout_kernel<X, Y, true><<<blocks, 256, 0, stream>>>(a);
     else dropout_kernel<X, Y, false><<<blocks, 256, 0, stream>>>(a);
     return (int)hipGetLastError();
