@@ -30,6 +30,7 @@ struct AdapterArgs {
     float *t;                  // [splits][m][pitch] sums over a part of k each
     int *order;                // kList: [m] tokens by adapter
     AdapterTile *tiles;        // kList: [tiles_most]
+    int *found;                // kSorting: [tiles_most][2 + 16 token_tiles], a tile's count, adapter and tokens
     long long ldx, ldy, ldbase;
     int m, n, k, count, rank;
     int pitch;                 // of a row of t: whole 16 values

@@ -151,7 +151,7 @@ __global__ __launch_bounds__(kGroupThreads) void adapter_group_kernel(AdapterArg
 //   windows   up to kWindow tokens (or windows of so many): those that have the adapter of token `slot` of theirs, if that is the first to have
 //             it; so every adapter of the window has one block, which takes them by tiles one after the other
 //   sorting   up to kSorted tokens: the block counts the tokens of each adapter by itself, which costs less than a launch in
-//             front and the two trips to memory for its results
+//             front and the two trips to memory for its results; adapter_down_kernel then leaves what it has found to adapter_up_kernel
 //   list      tile and tokens are what adapter_group_kernel has written
 struct Tile {
     int id, count;
@@ -164,6 +164,26 @@ struct Finding {
     Tile tile;
     int first;
 };
+
+// What adapter_down_kernel's block of a tile has found: count, adapter and tokens.
+__device__ __forceinline__ int *record_of(const AdapterArgs &a, int index) { return a.found + index * (2 + 16 * a.token_tiles); }
+
+__device__ __forceinline__ void leave_tile(const AdapterArgs &a, int index, const Tile &t, const Finding &s)
+{
+    int *const record = record_of(a, index);
+    if (threadIdx.x < 2) st_global(record + threadIdx.x, threadIdx.x ? t.id : t.count);
+    if ((int)threadIdx.x < t.count) st_global(record + 2 + threadIdx.x, s.tokens[threadIdx.x]);
+}
+
+__device__ __forceinline__ Tile left_tile(const AdapterArgs &a, int index, Finding &s)
+{
+    const int thread = threadIdx.x, v = thread < 2 + 16 * a.token_tiles ? ld_global(record_of(a, index) + thread) : 0;
+    if (thread == 0) s.tile.count = v;
+    else if (thread == 1) s.tile.id = v;
+    else if (thread < 2 + kWindow) s.tokens[thread - 2] = v;
+    __syncthreads();
+    return s.tile;
+}
 
 __device__ __forceinline__ Tile find_tile(const AdapterArgs &a, int index, Finding &s)
 {
@@ -389,6 +409,7 @@ __global__ __launch_bounds__(kBlock, SHORT ? 2 : 4) void adapter_down_kernel(Ada
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const Share share(a);
     const Tile tile = find_tile(a, share.index, finding);
+    if (a.way == kSorting && share.split == 0 && share.chunk == 0) leave_tile(a, share.index, tile, finding);
     if (tile.id < 0 || tile.count == 0) return;
     const _Float16 *ranks[NR];
 #pragma unroll
@@ -443,6 +464,7 @@ __global__ __launch_bounds__(kBlock) void adapter_down_ring_kernel(AdapterArgs a
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Share share(a);
     const Tile tile = find_tile(a, share.index, finding);
+    if (a.way == kSorting && share.split == 0 && share.chunk == 0) leave_tile(a, share.index, tile, finding);
     if (tile.id < 0 || tile.count == 0) return;
     const uint64_t x_at = (uint64_t)a.x, a_at = (uint64_t)a.a + (uint64_t)tile.id * (uint64_t)a.rank * (uint64_t)a.k * 2;
     // descriptors of raw buffers: the hardware answers loads behind their ends with zeros
@@ -601,7 +623,8 @@ __global__ __launch_bounds__(kBlock, J == 8 || SHORT ? 2 : N == 2 || J == 1 ? 4 
     __shared__ float factor[kWindow];
     const int *tokens = finding.tokens;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const Tile tile = find_tile(a, blockIdx.x / a.groups, finding);
+    const int index = (int)(blockIdx.x / a.groups);
+    const Tile tile = a.way == kSorting ? left_tile(a, index, finding) : find_tile(a, index, finding);
     const int deep = (a.rank + 31) / 32, row = deep * 32 + 8, most_tokens = TT * 16;
     const bool copy = tile.id < 0;
     if (copy && a.base == a.y && !a.no_base) return;

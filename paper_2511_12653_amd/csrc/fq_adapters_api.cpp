@@ -94,7 +94,8 @@ Workspace workspace_of(const fq_adapters &d)
     const AdapterArgs a = plan_of(d, at_most(d.m, kAdaptersMostTokens));
     at.tiles = round_up((size_t)a.m * sizeof(int), kAlign);
     // (the last tokens of a call may come in a launch of fewer, in smaller tiles; calls of several launches do not cut up k)
-    at.t = at.tiles + round_up((size_t)(a.way == kList ? a.m / 16 + at_most(a.count + 1LL, a.m) : 0) * sizeof(AdapterTile) + sizeof(int), kAlign);
+    const size_t list = a.way == kList ? (size_t)(a.m / 16 + at_most(a.count + 1LL, a.m)) * sizeof(AdapterTile) : 0;
+    at.t = at.tiles + round_up(a.way == kSorting ? (size_t)a.tiles_most * (size_t)(2 + 16 * a.token_tiles) * sizeof(int) : list, kAlign);
     at.bytes = at.t + round_up((size_t)a.m * (size_t)a.pitch * sizeof(float) * (size_t)(d.m > kAdaptersMostTokens ? 1 : a.splits), kAlign);
     return at;
 }
@@ -108,6 +109,7 @@ AdapterArgs args_of(const fq_adapters &d, long long m, void *workspace)
     if (a.count > 0) {
         a.order = (int *)(ws + at.order);
         a.tiles = (AdapterTile *)(ws + at.tiles);
+        a.found = (int *)(ws + at.tiles);
         a.t = (float *)(ws + at.t);
     }
     a.a = d.a; a.b = d.b; a.scale = d.scale;

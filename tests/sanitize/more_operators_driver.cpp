@@ -80,12 +80,16 @@ int launch_adapters(const AdapterArgs &a, void *)
     if (a.way == kList) {
         CHECK(a.count <= kMostGrouped);
         inside(a.order, (unsigned long long)a.m * 4);
-        // the tiles, and their number behind them or before: whole ones and one begun for each adapter
-        inside(a.tiles, (unsigned long long)a.tiles_most * sizeof(AdapterTile) + 4);
-        CHECK((char *)a.order + (size_t)a.m * 4 <= (char *)a.tiles && (char *)a.tiles + (size_t)a.tiles_most * sizeof(AdapterTile) + 4 <= (char *)a.t);
+        inside(a.tiles, (unsigned long long)a.tiles_most * sizeof(AdapterTile));
+        CHECK((char *)a.order + (size_t)a.m * 4 <= (char *)a.tiles && (char *)a.tiles + (size_t)a.tiles_most * sizeof(AdapterTile) <= (char *)a.t);
         CHECK(a.tiles_most >= ceiling(a.m, 16 * a.token_tiles));
     } else {
-        CHECK(a.way == kWindows ? a.tiles_most >= ceiling(a.m, kWindow) : a.m <= kSorted);
+        CHECK(a.way == kWindows ? a.tiles_most >= ceiling(a.m, kWindow) : a.m <= kSorted && a.token_tiles <= 2);
+        if (a.way == kSorting) {
+            const unsigned long long records = (unsigned long long)a.tiles_most * (unsigned)(2 + 16 * a.token_tiles) * 4;
+            inside(a.found, records);
+            CHECK((char *)a.found + records <= (char *)a.t);
+        }
     }
     if (a.x_bytes) CHECK((unsigned long long)a.x_bytes >= (unsigned long long)(a.m - 1) * (unsigned long long)a.ldx && a.k >= 16 && (uintptr_t)a.x % 16 == 0);
     return 0;
