@@ -467,7 +467,7 @@ fq_status fq_dropout(const fq_dropout_args *d, void *hip_stream);
  * once.  Tokens come in any order; ids outside [0, count) mean no adapter (y = base).  A token's NaN or infinity stays in
  * its row, an adapter's with its tokens.
  * Rows of x, base and y may lie any distance apart and at any address that their type allows; a and b are contiguous.
- * y may be exactly base (same type and distance).  Two launches, three with more than 1024 tokens and up to 1024 adapters;
+ * y may be exactly base (same type and distance).  Two launches, three with more than 4096 tokens and up to 1024 adapters;
  * so many per 65536 tokens.  The workspace need not be initialised and may be shared by calls that do not overlap in time.
  * There is no backward pass.
  */

@@ -10,7 +10,7 @@ constexpr long long kAdaptersMostWidth = 1LL << 20;
 constexpr int kAdaptersMostRank = 256;
 constexpr int kWindow = 64;                      // tokens that a wavefront sorts out by itself
 constexpr long long kAdaptersMostTokens = 1 << 16;       // of a launch
-constexpr int kSorted = 1024;                    // tokens that a block sorts out by itself
+constexpr int kSorted = 4096, kFewSorted = 1024;   // tokens that a block sorts out by itself; that cost it less
 constexpr int kMostGrouped = 1024;               // adapters that tokens are sorted by
 
 enum AdapterWay { kWindows, kSorting, kList };   // how a block comes to its tokens

@@ -151,7 +151,8 @@ __global__ __launch_bounds__(kGroupThreads) void adapter_group_kernel(AdapterArg
 //   windows   up to kWindow tokens (or windows of so many): those that have the adapter of token `slot` of theirs, if that is the first to have
 //             it; so every adapter of the window has one block, which takes them by tiles one after the other
 //   sorting   up to kSorted tokens: the block counts the tokens of each adapter by itself, which costs less than a launch in
-//             front and the two trips to memory for its results; adapter_down_kernel then leaves what it has found to adapter_up_kernel
+//             front and the two trips to memory for its results (us, 4096 x 4096 by 16 ranks: 2048 tokens 23.2, 27.1 with a list; 4000
+//             tokens 33.8, 36.8; 8192 x 8192 by 64 ranks, 8192 tokens: 122.8, 120.4); adapter_down_kernel then leaves what it has found to adapter_up_kernel
 //   list      tile and tokens are what adapter_group_kernel has written
 struct Tile {
     int id, count;
@@ -164,6 +165,69 @@ struct Finding {
     Tile tile;
     int first;
 };
+
+// Sorting (see find_tile), IDS tokens to a thread.
+template <int IDS> __device__ __forceinline__ Tile sorted_tile(const AdapterArgs &a, int index, Finding &s)
+{
+    const int thread = threadIdx.x, lane = thread & 63, wave = thread >> 6;
+    Tile t = {-1, 0};
+    const int groups = a.count + 1, tile = 16 * a.token_tiles;
+    int id[IDS];
+#pragma unroll
+    for (int j = 0; j < IDS; ++j) id[j] = group_of(a, j * kBlock + thread);
+    for (int i = thread; i < groups; i += kBlock) s.counts[i] = 0;
+    if (thread == 0) s.tile = t;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < IDS; ++j) {
+        // (tokens of one request come one after the other: then the wavefront counts once)
+        const bool some = j * kBlock + thread < a.m;
+        const unsigned long long mine = __ballot(some);
+        if (mine == 0) continue;
+        const int leader = __builtin_amdgcn_readlane(id[j], __builtin_ctzll(mine));
+        if (__ballot(some && id[j] == leader) == mine) {
+            if (lane == 0) atomicAdd(s.counts + leader, __popcll(mine));
+        } else if (some) {
+            atomicAdd(s.counts + id[j], 1);
+        }
+    }
+    __syncthreads();
+    const int each = (groups + kBlock - 1) / kBlock, begin = min(thread * each, groups), end = min(begin + each, groups);
+    int at = 0, none = 0, all;
+    for (int g = begin; g < end; ++g) at += (s.counts[g] + tile - 1) / tile;
+    sums_before(none, at, all, s.sums, lane, wave);
+    for (int g = begin; g < end; ++g) {
+        const int count = s.counts[g], tiles = (count + tile - 1) / tile;
+        if (index >= at && index < at + tiles) {
+            s.tile = {g < a.count ? g : -1, min(tile, count - (index - at) * tile)};
+            s.first = (index - at) * tile;
+        }
+        at += tiles;
+    }
+    __syncthreads();
+    t = s.tile;
+    if (t.count == 0) return t;
+    const int group = t.id < 0 ? a.count : t.id;
+    unsigned long long mine[IDS];
+#pragma unroll
+    for (int j = 0; j < IDS; ++j) {
+        mine[j] = __ballot(j * kBlock + thread < a.m && id[j] == group);
+        if (lane == 0) s.parts[j * (kBlock / 64) + wave] = __popcll(mine[j]);
+    }
+    __syncthreads();
+    int place = -s.first;
+#pragma unroll
+    for (int j = 0; j < IDS; ++j) {
+        if (j * kBlock >= a.m || place >= t.count) continue;
+#pragma unroll
+        for (int w = 0; w < kBlock / 64; ++w) {
+            const int own = place + before(mine[j], lane);
+            if (w == wave && (mine[j] >> lane & 1) && own >= 0 && own < t.count) s.tokens[own] = j * kBlock + thread;
+            place += s.parts[j * (kBlock / 64) + w];
+        }
+    }
+    return t;
+}
 
 // What adapter_down_kernel's block of a tile has found: count, adapter and tokens.
 __device__ __forceinline__ int *record_of(const AdapterArgs &a, int index) { return a.found + index * (2 + 16 * a.token_tiles); }
@@ -187,7 +251,7 @@ __device__ __forceinline__ Tile left_tile(const AdapterArgs &a, int index, Findi
 
 __device__ __forceinline__ Tile find_tile(const AdapterArgs &a, int index, Finding &s)
 {
-    const int thread = threadIdx.x, lane = thread & 63, wave = thread >> 6;
+    const int thread = threadIdx.x, lane = thread & 63;
     Tile t = {-1, 0};
     if (a.way == kWindows) {
         const int slots = min(a.m, kWindow), begin = index / slots * kWindow, slot = index % slots;
@@ -199,62 +263,7 @@ __device__ __forceinline__ Tile find_tile(const AdapterArgs &a, int index, Findi
         t.count = slot < left && __builtin_ctzll(mine) == slot ? __popcll(mine) : 0;
         if (thread < 64 && (mine >> lane & 1)) s.tokens[before(mine, lane)] = begin + lane;
     } else if (a.way == kSorting) {
-        constexpr int kIds = kSorted / kBlock;
-        const int groups = a.count + 1, tile = 16 * a.token_tiles;
-        int id[kIds];
-#pragma unroll
-        for (int j = 0; j < kIds; ++j) id[j] = group_of(a, j * kBlock + thread);
-        for (int i = thread; i < groups; i += kBlock) s.counts[i] = 0;
-        if (thread == 0) s.tile = t;
-        __syncthreads();
-#pragma unroll
-        for (int j = 0; j < kIds; ++j) {
-            // (tokens of one request come one after the other: then the wavefront counts once)
-            const bool some = j * kBlock + thread < a.m;
-            const unsigned long long mine = __ballot(some);
-            if (mine == 0) continue;
-            const int leader = __builtin_amdgcn_readlane(id[j], __builtin_ctzll(mine));
-            if (__ballot(some && id[j] == leader) == mine) {
-                if (lane == 0) atomicAdd(s.counts + leader, __popcll(mine));
-            } else if (some) {
-                atomicAdd(s.counts + id[j], 1);
-            }
-        }
-        __syncthreads();
-        const int each = (groups + kBlock - 1) / kBlock, begin = min(thread * each, groups), end = min(begin + each, groups);
-        int at = 0, none = 0, all;
-        for (int g = begin; g < end; ++g) at += (s.counts[g] + tile - 1) / tile;
-        sums_before(none, at, all, s.sums, lane, wave);
-        for (int g = begin; g < end; ++g) {
-            const int count = s.counts[g], tiles = (count + tile - 1) / tile;
-            if (index >= at && index < at + tiles) {
-                s.tile = {g < a.count ? g : -1, min(tile, count - (index - at) * tile)};
-                s.first = (index - at) * tile;
-            }
-            at += tiles;
-        }
-        __syncthreads();
-        t = s.tile;
-        if (t.count == 0) return t;
-        const int group = t.id < 0 ? a.count : t.id;
-        unsigned long long mine[kIds];
-#pragma unroll
-        for (int j = 0; j < kIds; ++j) {
-            mine[j] = __ballot(j * kBlock + thread < a.m && id[j] == group);
-            if (lane == 0) s.parts[j * (kBlock / 64) + wave] = __popcll(mine[j]);
-        }
-        __syncthreads();
-        int place = -s.first;
-#pragma unroll
-        for (int j = 0; j < kIds; ++j) {
-            if (j * kBlock >= a.m || place >= t.count) continue;
-#pragma unroll
-            for (int w = 0; w < kBlock / 64; ++w) {
-                const int own = place + before(mine[j], lane);
-                if (w == wave && (mine[j] >> lane & 1) && own >= 0 && own < t.count) s.tokens[own] = j * kBlock + thread;
-                place += s.parts[j * (kBlock / 64) + w];
-            }
-        }
+        t = a.m <= kFewSorted ? sorted_tile<kFewSorted / kBlock>(a, index, s) : sorted_tile<kSorted / kBlock>(a, index, s);
     } else {
         const AdapterTile f = a.tiles[index];
         t = {f.id, f.count};

@@ -87,15 +87,25 @@ struct Workspace {
     size_t order = 0, tiles = 0, t = 0, bytes = kAlign;
 };
 
+size_t list_bytes(const AdapterArgs &a)
+{
+    if (a.way == kWindows) return 0;
+    return (size_t)a.tiles_most * (a.way == kList ? sizeof(AdapterTile) : (size_t)(2 + 16 * a.token_tiles) * sizeof(int));
+}
+
 Workspace workspace_of(const fq_adapters &d)
 {
     Workspace at;
     if (d.m == 0 || d.n == 0 || d.count == 0 || d.rank == 0) return at;
     const AdapterArgs a = plan_of(d, at_most(d.m, kAdaptersMostTokens));
     at.tiles = round_up((size_t)a.m * sizeof(int), kAlign);
-    // (the last tokens of a call may come in a launch of fewer, in smaller tiles; calls of several launches do not cut up k)
-    const size_t list = a.way == kList ? (size_t)(a.m / 16 + at_most(a.count + 1LL, a.m)) * sizeof(AdapterTile) : 0;
-    at.t = at.tiles + round_up(a.way == kSorting ? (size_t)a.tiles_most * (size_t)(2 + 16 * a.token_tiles) * sizeof(int) : list, kAlign);
+    size_t list = list_bytes(a);
+    if (d.m > kAdaptersMostTokens && d.m % kAdaptersMostTokens != 0) {          // (the last tokens come in a launch of fewer)
+        const size_t last = list_bytes(plan_of(d, d.m % kAdaptersMostTokens));
+        if (last > list) list = last;
+    }
+    at.t = at.tiles + round_up(list, kAlign);
+    // (calls of several launches do not cut up k)
     at.bytes = at.t + round_up((size_t)a.m * (size_t)a.pitch * sizeof(float) * (size_t)(d.m > kAdaptersMostTokens ? 1 : a.splits), kAlign);
     return at;
 }

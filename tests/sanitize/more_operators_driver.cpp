@@ -84,7 +84,7 @@ int launch_adapters(const AdapterArgs &a, void *)
         CHECK((char *)a.order + (size_t)a.m * 4 <= (char *)a.tiles && (char *)a.tiles + (size_t)a.tiles_most * sizeof(AdapterTile) <= (char *)a.t);
         CHECK(a.tiles_most >= ceiling(a.m, 16 * a.token_tiles));
     } else {
-        CHECK(a.way == kWindows ? a.tiles_most >= ceiling(a.m, kWindow) : a.m <= kSorted && a.token_tiles <= 2);
+        CHECK(a.way == kWindows ? a.tiles_most >= ceiling(a.m, kWindow) : a.m <= kSorted);
         if (a.way == kSorting) {
             const unsigned long long records = (unsigned long long)a.tiles_most * (unsigned)(2 + 16 * a.token_tiles) * 4;
             inside(a.found, records);

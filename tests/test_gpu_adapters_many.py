@@ -14,7 +14,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("x_type", [np.float16, np.float32, np.int8])
-@pytest.mark.parametrize("m", [1023, 1024, 1025, 1100, 2049, 4095, 4103])
+@pytest.mark.parametrize("m", [1023, 1024, 1025, 1100, 2049, 4095, 4096, 4097, 4103])
 def test_tokens(m, x_type):
     for order, count, rank, k, n in (("runs", 3, 16, 128, 70), ("mixed", 5, 24, 72, 136), ("mixed", 61, 40, 64, 66), ("runs", 2, 64, 256, 129), ("mixed", 1, 100, 80, 40)):
         check(case(m, k, n, count, rank, x_type, np.float16, m + rank, order), np.float16, "%s %d adapters of %d" % (order, count, rank))
@@ -22,7 +22,7 @@ def test_tokens(m, x_type):
 
 @pytest.mark.parametrize("rank", [1, 5, 8, 16, 17, 32, 33, 47, 64, 65, 130, 256])
 def test_ranks(rank):
-    for m, x_type, shift in ((1500, np.float16, 0), (1500, np.float16, 1), (4500, np.int8, 0), (4500, np.float32, 0)):
+    for m, x_type, shift in ((1500, np.float16, 0), (1500, np.float16, 1), (2500, np.int8, 0), (4500, np.int8, 0), (4500, np.float32, 0)):
         check(case(m, 96, 48, 7, rank, x_type, np.float32, rank, "runs" if rank % 2 else "mixed"), np.float32, "%d %d" % (m, shift), shift=shift)
 
 
@@ -34,18 +34,18 @@ def test_channels(n):
 
 @pytest.mark.parametrize("k", [1, 8, 15, 16, 17, 40, 1000])
 def test_values_per_token(k):
-    for m, x_type in ((1300, np.float16), (4200, np.int8)):
+    for m, x_type in ((1300, np.float16), (4096, np.int8), (4200, np.int8)):
         check(case(m, k, 24, 4, 36, x_type, np.float16, k), np.float16, "%d" % m)
 
 
 @pytest.mark.parametrize("count", [1, 2, 15, 16, 63, 64, 65, 255, 1000, 1023, 1024, 1025, 3000])
 def test_adapters(count):
-    for m in (50, 900, 1300, 4133):
+    for m in (50, 900, 1300, 4096, 4133):
         check(case(m, 48, 40, count, 8, np.float16, np.float16, count + m), np.float16, "%d" % m)
 
 
 def test_all_of_one_or_of_none():
-    for m in (1024, 1025, 5000):
+    for m in (1024, 1025, 4096, 5000):
         c = case(m, 64, 32, 6, 16, np.float16, np.float16, m)
         for one in (0, 5, 6, -1):
             c["ids"][:] = one
@@ -57,6 +57,12 @@ def test_all_of_one_or_of_none():
 @pytest.mark.parametrize("m", [65535, 65536, 65537, 140001])
 def test_calls_that_go_in_parts(m):
     check(case(m, 24, 16, 5, 8, np.int8 if m % 2 else np.float16, np.float16, m, "mixed" if m < 100000 else "runs"), np.float16)
+
+
+@pytest.mark.parametrize("rest,count", [(100, 1000), (3000, 1000), (4097, 700), (20000, 1024), (700, 2000)])
+def test_the_last_part_is_cut_up_otherwise(rest, count):
+    """The last tokens are found by another way than the first 65536, or in smaller tiles, and what is found has to fit as well."""
+    check(case(65536 + rest, 24, 16, count, 8, np.float16, np.float16, rest), np.float16)
 
 
 def test_in_place_and_without_base():
@@ -151,9 +157,9 @@ def test_widest():
     check(case(2, 9, 1 << 20, 2, 2, np.float16, np.float16, 5), np.float16)
 
 
-def test_captured():
+@pytest.mark.parametrize("m", [2500, 6000])
+def test_captured(m):
     """With the tokens' order found anew in each replay."""
-    m = 2500
     c = case(m, 64, 48, 9, 16, np.float16, np.float16, 9)
     x, ids, a, b, base = (H.dev(c[n]) for n in ("x", "ids", "a", "b", "base"))
     y = torch.empty_like(base)
