@@ -21,6 +21,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ bool has_adapter(int id, int count) { return id >= 0 && id < count; }
 
@@ -612,6 +613,19 @@ template <int J> __device__ __forceinline__ void sum_of_parts(f32x4 (&s)[J], con
         for (int e = 0; e < 4; ++e) s[j][e] = (j * 8 + unit) * 4 + e < a.rank ? s[j][e] : 0.0f;
 }
 
+// Rows of b of fewer than eight ranks, that of channel c in the first places and zeros behind it: they lie one behind the other, so a whole vector
+// from there on has it, or at the end of the adapter's one that begins up to seven values before.
+__device__ __forceinline__ void short_row(Words<_Float16, 8> &to, const _Float16 *b, int c, int n, int rank, bool some)
+{
+    const int at = c * rank, from = min(at, n * rank - 8), off = (at - from) * 16;
+    __builtin_memcpy(&to, (const FQ_GLOBAL _Float16 *)(b + from), sizeof to);
+    const auto v = __builtin_bit_cast(u64x2, to.w);
+    const uint64_t high = off < 64 ? v[1] >> off : 0, low = off < 64 ? v[0] >> off | (v[1] << 1) << (63 - off) : v[1] >> (off - 64);
+    const int bits = some ? rank * 16 : 0;
+    const uint64_t keep_low = bits >= 64 ? ~0ull : (1ull << bits) - 1, keep_high = bits > 64 ? (1ull << (bits - 64)) - 1 : 0;
+    to.w = __builtin_bit_cast(typename Words<_Float16, 8>::W, u64x2{low & keep_low, high & keep_high});
+}
+
 // A value that the compiler takes for another at each use.  (What follows from it is then worked out where it is needed: the addresses of all
 // rows of a tile, kept over its strips, would take 64 registers.)
 __device__ __forceinline__ int anew(int v)
@@ -620,10 +634,10 @@ __device__ __forceinline__ int anew(int v)
     return v;
 }
 
-// TT: tokens of a tile in 16s, at most; J: of t's units, 32 J ranks at most; FEW: channels, fewer than N; SHORT: rows of b, fewer than eight
-// ranks.
+// TT: tokens of a tile in 16s, at most; J: of t's units, 32 J ranks at most; SHORT: rows of b, fewer than eight ranks; FEW: channels, fewer
+// than N, or values of b of an adapter, fewer than eight.
 template <typename Y, typename B, int N, int TT, int J, bool FEW, bool SHORT>
-__global__ __launch_bounds__(kBlock, J == 8 || SHORT ? 2 : N == 2 || J == 1 ? 4 : 3) void adapter_up_kernel(AdapterArgs a)
+__global__ __launch_bounds__(kBlock, J == 8 ? 2 : N == 2 || J == 1 ? 4 : 3) void adapter_up_kernel(AdapterArgs a)
 {
     constexpr int kHeld = J == 8 ? 1 : J;                             // vectors of b of a channel that are held: all, or one at a time
     constexpr int kAhead = TT > 1 ? 2 : 1;                            // tokens' tiles whose base is held
@@ -648,9 +662,13 @@ __global__ __launch_bounds__(kBlock, J == 8 || SHORT ? 2 : N == 2 || J == 1 ? 4 
         const auto ask_b = [&](int of) {
 #pragma unroll
             for (int c = 0; c < N; ++c) {
-                const _Float16 *from = channel(c, of);
+                if constexpr (SHORT && !FEW) {
+                    short_row(b[0][c], (const _Float16 *)a.b + (long long)tile.id * a.n * a.rank, begin_of(first_of(of), N, a.n) + c, a.n, a.rank, lane < 16);
+                } else {
+                    const _Float16 *from = channel(c, of);
 #pragma unroll
-                for (int d = 0; d < kHeld; ++d) load<SHORT>(b[d][c], from, begin_of(d * 32 + lane / 16 * 8, 8, a.rank), a.rank);
+                    for (int d = 0; d < kHeld; ++d) load<SHORT>(b[d][c], from, begin_of(d * 32 + lane / 16 * 8, 8, a.rank), a.rank);
+                }
             }
         };
         Words<B, N> base[kAhead][4];
@@ -661,9 +679,19 @@ __global__ __launch_bounds__(kBlock, J == 8 || SHORT ? 2 : N == 2 || J == 1 ? 4 
                 load<FEW>(base[n % kAhead][i], from, begin_of(first_of(of), N, a.n), a.n);
             }
         };
+        // (J == 8: vectors of b come one after the other, each for all tokens of the tile while the next is on its way)
+        Words<_Float16, 8> odd[kHeld][N];
+        const auto ask_deep = [&](Words<_Float16, 8> (&to)[N], int d, int of) {
+#pragma unroll
+            for (int c = 0; c < N; ++c) load<SHORT>(to[c], channel(c, of), begin_of(min(d, deep - 1) * 32 + lane / 16 * 8, 8, a.rank), a.rank);
+        };
         // (strips behind the last clamp to the end of the row: loads of what is left unused)
         if (!copy && J < 8) ask_b(strip);
         ask_base(0, strip);
+        if (J == 8) {
+            if (TT == 2) ask_base(1, strip);
+            if (!copy) ask_deep(b[0], 0, strip);
+        }
         if (!copy) {
             const int unit = threadIdx.x % 8;
             for (int i = threadIdx.x / 8; i < most_tokens; i += kBlock / 8) {
@@ -713,33 +741,48 @@ __global__ __launch_bounds__(kBlock, J == 8 || SHORT ? 2 : N == 2 || J == 1 ? 4 
         __syncthreads();
         while (strip * 16 * N < a.n) {
             const int after = strip + a.groups * kUpWaves;
+            f32x4 sums[J == 8 ? TT : 1][N];
+            if (J == 8) {
+#pragma unroll
+                for (int n = 0; n < TT; ++n)
+#pragma unroll
+                    for (int c = 0; c < N; ++c) sums[n][c] = (f32x4)0.0f;
+                if (!copy) {
+                    const auto multiply_all = [&](const Words<_Float16, 8> (&by)[N], int d) {
+#pragma unroll
+                        for (int n = 0; n < TT; ++n) {
+                            const _Float16 *t = shared + (n * 16 + lane % 16) * row + lane / 16 * 8 + d * 32;
+                            const f16x8 high = *(const f16x8 *)t, low = *(const f16x8 *)(t + most_tokens * row);
+#pragma unroll
+                            for (int c = 0; c < N; ++c) sums[n][c] = product(low, by[c].values(), product(high, by[c].values(), sums[n][c]));
+                        }
+                    };
+                    for (int d = 0; d < deep; d += 2) {
+                        ask_deep(odd[0], d + 1, strip);
+                        multiply_all(b[0], d);
+                        ask_deep(b[0], d + 2, strip);
+                        if (d + 1 < deep) multiply_all(odd[0], d + 1);
+                    }
+                    ask_deep(b[0], 0, after);
+                }
+            }
 #pragma unroll
             for (int n = 0; n < TT; ++n) {
-                if (TT > 1) {
+                if (TT > 1 && J < 8) {
                     if (n + 1 < TT) ask_base(n + 1, strip);
                     else ask_base(0, after);
                 }
                 f32x4 sum[N];
 #pragma unroll
-                for (int c = 0; c < N; ++c) sum[c] = (f32x4)0.0f;
-                if (!copy) {
+                for (int c = 0; c < N; ++c) sum[c] = J == 8 ? sums[J == 8 ? n : 0][c] : (f32x4)0.0f;
+                if (!copy && J < 8) {
                     const _Float16 *t = shared + (n * 16 + lane % 16) * row + lane / 16 * 8;
-                    const auto multiply = [&](const Words<_Float16, 8> (&by)[N], int d) {
+#pragma unroll
+                    for (int d = 0; d < kHeld; ++d) {
+                        if (d >= deep) continue;
                         const f16x8 high = *(const f16x8 *)(t + d * 32), low = *(const f16x8 *)(t + d * 32 + most_tokens * row);
 #pragma unroll
-                        for (int c = 0; c < N; ++c) sum[c] = product(low, by[c].values(), product(high, by[c].values(), sum[c]));
-                    };
-                    if constexpr (J < 8) {
-#pragma unroll
-                        for (int d = 0; d < kHeld; ++d)
-                            if (d < deep) multiply(b[d], d);
-                    } else {
-                        for (int d = 0; d < deep; ++d) {
-#pragma unroll
-                            for (int c = 0; c < N; ++c)
-                                load<SHORT>(b[0][c], channel(c, strip), begin_of(d * 32 + lane / 16 * 8, 8, a.rank), a.rank);
-                            multiply(b[0], d);
-                        }
+                        for (int c = 0; c < N; ++c) sum[c] = product(low, b[d][c].values(), product(high, b[d][c].values(), sum[c]));
                     }
                 }
 #pragma unroll
@@ -755,7 +798,7 @@ __global__ __launch_bounds__(kBlock, J == 8 || SHORT ? 2 : N == 2 || J == 1 ? 4 
                     }
                     if (token < count) store_channels<Y, N>((Y *)a.y + tokens[anew(sub + token)] * a.ldy, first_of(strip), a.n, y);
                 }
-                if (TT == 1) ask_base(0, after);
+                if (TT == 1 || J == 8) ask_base(n, after);
             }
             strip = after;
             if (!copy && J < 8) ask_b(strip);
@@ -803,7 +846,7 @@ template <typename Y, typename B> void up(const AdapterArgs &a, hipStream_t stre
 {
     const unsigned blocks = (unsigned)a.tiles_most * (unsigned)a.groups;
     const size_t lds = (size_t)2 * 16 * a.token_tiles * ((a.rank + 31) / 32 * 32 + 8) * sizeof(_Float16);
-    if (a.n < 2) adapter_up_kernel<Y, B, 2, 1, 8, true, true><<<blocks, kBlock, lds, stream>>>(a);
+    if (a.n < 2 || a.n * a.rank < 8) adapter_up_kernel<Y, B, 2, 1, 8, true, true><<<blocks, kBlock, lds, stream>>>(a);
     else if (a.rank < 8 && a.wide == 2) adapter_up_kernel<Y, B, 2, 1, 1, false, true><<<blocks, kBlock, lds, stream>>>(a);
     else if (a.rank < 8) adapter_up_kernel<Y, B, 4, 2, 1, false, true><<<blocks, kBlock, lds, stream>>>(a);
     else if (a.wide == 2) up_by<Y, B, 2, 1>(a, blocks, lds, stream);
