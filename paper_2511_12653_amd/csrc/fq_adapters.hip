@@ -637,7 +637,7 @@ __device__ __forceinline__ int anew(int v)
 // TT: tokens of a tile in 16s, at most; J: of t's units, 32 J ranks at most; SHORT: rows of b, fewer than eight ranks; FEW: channels, fewer
 // than N, or values of b of an adapter, fewer than eight.
 template <typename Y, typename B, int N, int TT, int J, bool FEW, bool SHORT>
-__global__ __launch_bounds__(kBlock, J == 8 ? 2 : N == 2 || J == 1 ? 4 : 3) void adapter_up_kernel(AdapterArgs a)
+__global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ? 3 : N == 2 || J == 1 ? 4 : 3) void adapter_up_kernel(AdapterArgs a)
 {
     constexpr int kHeld = J == 8 ? 1 : J;                             // vectors of b of a channel that are held: all, or one at a time
     constexpr int kAhead = TT > 1 ? 2 : 1;                            // tokens' tiles whose base is held
@@ -839,6 +839,7 @@ template <typename Y, typename B, int N, int TT> void up_by(const AdapterArgs &a
 {
     if (a.rank <= 32) adapter_up_kernel<Y, B, N, TT, 1, false, false><<<blocks, kBlock, lds, stream>>>(a);
     else if (a.rank <= 64) adapter_up_kernel<Y, B, N, TT, 2, false, false><<<blocks, kBlock, lds, stream>>>(a);
+    else if (a.rank <= 128) adapter_up_kernel<Y, B, N, TT, 4, false, false><<<blocks, kBlock, lds, stream>>>(a);
     else adapter_up_kernel<Y, B, N, TT, 8, false, false><<<blocks, kBlock, lds, stream>>>(a);
 }
 
