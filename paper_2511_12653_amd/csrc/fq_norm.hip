@@ -832,7 +832,9 @@ template <typename X, typename Y> int forward(const NormArgs &a, hipStream_t str
     else if (a.lanes == 64 && a.vecs == 3) forward_by<X, Y, 64, 3>(a, stream);
     else if (a.lanes == 64 && a.vecs == 4) forward_by<X, Y, 64, 4>(a, stream);
     else if (a.lanes == 256 && a.vecs == 2) forward_by<X, Y, 256, 2>(a, stream);
+    else if (a.lanes == 256 && a.vecs == 3) forward_by<X, Y, 256, 3>(a, stream);
     else if (a.lanes == 256 && a.vecs == 4) forward_by<X, Y, 256, 4>(a, stream);
+    else if (a.lanes == 512 && a.vecs == 3) forward_by<X, Y, 512, 3>(a, stream);
     else if (a.lanes == 512 && a.vecs == 4) forward_by<X, Y, 512, 4>(a, stream);
     else return (int)hipErrorInvalidValue;
     return (int)hipGetLastError();
@@ -856,7 +858,9 @@ template <typename X, typename G> int backward(const NormArgs &a, hipStream_t st
     else if (a.lanes == 64 && a.vecs == 2) backward_by<X, G, 64, 2>(a, stream);
     else if (a.lanes == 256 && a.vecs == 1) backward_by<X, G, 256, 1>(a, stream);
     else if (a.lanes == 256 && a.vecs == 2) backward_by<X, G, 256, 2>(a, stream);
+    else if (a.lanes == 256 && a.vecs == 3) backward_by<X, G, 256, 3>(a, stream);
     else if (a.lanes == 256 && a.vecs == 4) backward_by<X, G, 256, 4>(a, stream);
+    else if (a.lanes == 512 && a.vecs == 3) backward_by<X, G, 512, 3>(a, stream);
     else if (a.lanes == 512 && a.vecs == 4) backward_by<X, G, 512, 4>(a, stream);
     else return (int)hipErrorInvalidValue;
     return (int)hipGetLastError();

@@ -68,7 +68,9 @@ fq_status validate(const fq_norm &d, bool backward)
 // lanes have as many values as registers allow; more blocks hide more of it, fewer ask for weight and bias less often.  FP16, us, with the
 // shape here / others: forward 19200 x 384 (16, 3, 3) 7.6 / (64, 1) 11.2; 16384 x 2048 (64, 4, 2) 26.3 / (256, 1) 36.2; 32768 x 8192 (256, 4, 1)
 // 176 / (256, 4, 2) 195 / (512, 2, 2) 191; codes 16384 x 4096 (256, 2, 6) 58.2 / (256, 2, 2) 70 / (512, 2) 80; backward 19200 x 384 (64, 1, 2)
-// 15.5 / (16, 3, 2) 17.3; 1201 x 1155 (256, 1, 1) 11.4 / (64, 3, 1) 12.0; 32768 x 8192 (256, 4, 1) 285 / (512, 2, 1) 293.
+// 15.5 / (16, 3, 2) 17.3; 1201 x 1155 (256, 1, 1) 11.4 / (64, 3, 1) 12.0; 32768 x 8192 (256, 4, 1) 285 / (512, 2, 1) 293.  A vector that
+// no lane needs costs its registers and, in codes, its arithmetic: codes of FP32 8000 x 5120 (256, 3, 2) 45.7 / (256, 4, 6) 75, of 4000 x 12288
+// (512, 3, 1) 56 / (512, 4, 1) 105; backward 8000 x 5120 (256, 3, 1) 59 / (256, 4, 1) 68.
 struct Shape {
     int lanes, vecs, blocks;
     int rows() const { return norm_threads(lanes) / lanes; }         // of a block at a time
@@ -84,7 +86,8 @@ Shape shape_of(const fq_norm &d, bool backward)
         if (width <= 1024) return {64, width <= 512 ? 1 : 2, 2};
         if (width <= 2048) return {256, 1, 2};
         if (width <= 4096) return {256, 2, 2};
-        return {width <= 8192 ? 256 : 512, 4, 1};
+        if (width <= 8192) return {256, width <= 6144 ? 3 : 4, 1};
+        return {512, width <= 12288 ? 3 : 4, 1};
     }
     const bool codes = d.y_dtype == FQ_I8;
     if (width <= 128) return {16, 1, 6};
@@ -92,8 +95,9 @@ Shape shape_of(const fq_norm &d, bool backward)
     if (width <= 1536) return {64, width <= 1024 ? 2 : 3, codes ? 6 : 2};
     if (width <= 2048) return {64, 4, 2};
     if (width <= 4096) return {256, 2, codes ? 6 : 2};
+    if (width <= 6144) return {256, 3, codes || d.x_dtype == FQ_F16 ? 2 : 1};
     if (width <= 8192) return {256, 4, codes ? 6 : 1};
-    return {512, 4, 1};
+    return {512, width <= 12288 ? 3 : 4, 1};
 }
 
 // Blocks of the backward pass, each of which makes a partial sum of every column: as many as the chip holds, and enough for no

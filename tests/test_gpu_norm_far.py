@@ -88,6 +88,17 @@ def test_many_parts(width, rows):
     check_backward(x, gy, None, "%d x %d" % (rows, width))
 
 
+@pytest.mark.parametrize("width", [4097, 6144, 6145, 8193, 12288, 12289])
+def test_borders_between_forms(width):
+    """Widths at which rows go to another number of lanes or vectors, with rows enough for a block to go from one to the next."""
+    rng = rng_of(23, width)
+    for rows, x_type in ((3, np.float32), (1200, np.float16)):
+        x, w, b = tokens(rng, rows, width, x_type), (1 + 0.2 * rng.standard_normal(width)).astype(np.float32), rng.standard_normal(width).astype(np.float32)
+        for y_type in (np.float16, np.float32, np.int8):
+            check_forward(x, w, b, y_type, "%d x %d" % (rows, width), pitch=3, shift=1)
+        check_backward(x, tokens(rng, rows, width, np.float16), w, "%d x %d" % (rows, width), pitch=3, shift=1)
+
+
 def test_two_graphs_of_one_workspace():
     """Captured passes that use one workspace, one after the other, give what eager ones give, in every replay."""
     sizes = ((5000, 200), (300, 4096), (2, 20000))
