@@ -476,6 +476,13 @@ __device__ __forceinline__ void put_gradient(void *to, int at, float v, int w16)
     else st_global((float *)to + at, v);
 }
 
+__device__ __forceinline__ void put_gradients(void *to, int at, const float *v, int w16)
+{
+    if (!to) return;
+    if (w16) put8((_Float16 *)to, at, v);
+    else put8((float *)to, at, v);
+}
+
 // gx of a row of 8 to 8 L V values to L lanes, and the block's share of gw and gb: a lane adds up those of its columns over the block's rows.
 template <typename X, typename G, int L, int V>
 __global__ __launch_bounds__(norm_threads(L)) void norm_backward_kernel(NormArgs a)
@@ -575,12 +582,9 @@ __global__ __launch_bounds__(norm_threads(L)) void norm_backward_kernel(NormArgs
         for (int j = 0; j < V; ++j) {
             if (!p[j].there) continue;
             if (a.parts == 1) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (e < p[j].twice) continue;
-                    put_gradient(a.gw, p[j].at + e, gw[j][e], a.w16);
-                    put_gradient(a.gb, p[j].at + e, gb[j][e], a.w16);
-                }
+                // (what two vectors share is worked out and written by both, to the same bits)
+                put_gradients(a.gw, p[j].at, gw[j], a.w16);
+                put_gradients(a.gb, p[j].at, gb[j], a.w16);
             } else if (!p[j].twice) {
                 put8(to, p[j].at, gw[j]);
                 put8(to + k, p[j].at, gb[j]);

@@ -12,7 +12,6 @@ namespace {
 
 constexpr size_t kAlign = 256;
 constexpr long long kMostRows = 1LL << 36, kMostRowsOfPart = 256, kMostParts = 1LL << 21;
-constexpr long long kAloneGroups = 2;
 
 bool float_type(int32_t dtype) { return dtype == FQ_F16 || dtype == FQ_F32; }
 
@@ -108,7 +107,9 @@ int parts_of(const fq_norm &d)
     const Shape s = shape_of(d, true);
     const long long groups = (d.rows + s.rows() - 1) / s.rows(), least = (groups + kMostRowsOfPart - 1) / kMostRowsOfPart;
     const bool held = d.width <= kNormHeldWidth;
-    if (held && groups <= kAloneGroups) return 1;
+    // (us, in one part / in one for each group of rows a block has at a time: 4 x 1155 4.5 / 5.7, 6 x 1155 6.0 / 5.7, 3 x 4096 5.4 / 5.9, 4 x 4096 6.5 / 6.1,
+    // 2 x 9305 7.0 / 8.2, 3 x 9305 8.8 / 8.3)
+    if (held && groups <= (s.vecs == 1 ? 4 : s.vecs == 2 ? 3 : 2)) return 1;
     const long long strips = held ? 1 : (d.width + kNormStrip - 1) / kNormStrip;
     long long chip = held ? (long long)s.blocks * kComputeUnits : strips < 2 * kComputeUnits ? 2 * kComputeUnits / strips : 1;
     // (a part of a wide row's width is as much to write, and to read again, as two or three rows: 403 x 4096 FP16 13.2 us in 128 parts, 17.7 in 403)

@@ -140,3 +140,13 @@ def test_two_graphs_of_one_workspace():
             graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(s, t) for a, b in zip(outs, want) for s, t in zip(a, b))
+
+
+@pytest.mark.parametrize("width", [8, 9, 129, 300, 384, 1001, 1155, 2047, 4095, 6001, 9305, 16384])
+def test_backward_of_few_rows(width):
+    """Where one block does all rows and writes the gradients of weight and bias itself, and just above."""
+    rng = rng_of(24, width)
+    for rows in (1, 2, 3, 4, 5, 13, 16, 49, 64, 65):
+        x, gy, w = tokens(rng, rows, width, np.float16), tokens(rng, rows, width, np.float32), rng.standard_normal(width).astype(np.float16)
+        for w_type in (np.float16, np.float32):
+            check_backward(x, gy, w.astype(w_type), "%d x %d" % (rows, width), w_type=w_type)
