@@ -614,7 +614,8 @@ template <int J> __device__ __forceinline__ void sum_of_parts(f32x4 (&s)[J], con
 }
 
 // Rows of b of fewer than eight ranks, that of channel c in the first places and zeros behind it: they lie one behind the other, so a whole vector
-// from there on has it, or at the end of the adapter's one that begins up to seven values before.
+// from there on has it, or at the end of the adapter's one that begins up to seven values before.  (By single values, us: 27 tokens, 7953 channels
+// and 4 ranks 17.4, so 11.9; 3818 x 2501 x 7056 with 4 ranks 77, so 51.)
 __device__ __forceinline__ void short_row(Words<_Float16, 8> &to, const _Float16 *b, int c, int n, int rank, bool some)
 {
     const int at = c * rank, from = min(at, n * rank - 8), off = (at - from) * 16;
