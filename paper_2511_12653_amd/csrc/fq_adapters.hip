@@ -615,7 +615,7 @@ template <int J> __device__ __forceinline__ void sum_of_parts(f32x4 (&s)[J], con
 
 // Rows of b of fewer than eight ranks, that of channel c in the first places and zeros behind it: they lie one behind the other, so a whole vector
 // from there on has it, or at the end of the adapter's one that begins up to seven values before.  (By single values, us: 27 tokens, 7953 channels
-// and 4 ranks 17.4, so 11.9; 3818 x 2501 x 7056 with 4 ranks 77, so 51.)
+// and 4 ranks 17.4, so 10.6; 3818 x 2501 x 7056 with 4 ranks 77, so 51 to 55.)
 __device__ __forceinline__ void short_row(Words<_Float16, 8> &to, const _Float16 *b, int c, int n, int rank, bool some)
 {
     const int at = c * rank, from = min(at, n * rank - 8), off = (at - from) * 16;
@@ -635,6 +635,9 @@ __device__ __forceinline__ int anew(int v)
     return v;
 }
 
+// Values from a row of t in LDS to the next: whole 32 ranks, and eight more so that rows begin in different banks.
+__host__ __device__ constexpr int row_of_t(int rank) { return (rank + 31) / 32 * 32 + 8; }
+
 // TT: tokens of a tile in 16s, at most; J: of t's units, 32 J ranks at most; SHORT: rows of b, fewer than eight ranks; FEW: channels, fewer
 // than N, or values of b of an adapter, fewer than eight.
 template <typename Y, typename B, int N, int TT, int J, bool FEW, bool SHORT>
@@ -649,7 +652,7 @@ __global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ?
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int index = (int)(blockIdx.x / a.groups);
     const Tile tile = a.way == kSorting ? left_tile(a, index, finding) : find_tile(a, index, finding);
-    const int deep = (a.rank + 31) / 32, row = deep * 32 + 8, most_tokens = TT * 16;
+    const int deep = (a.rank + 31) / 32, row = row_of_t(a.rank), most_tokens = TT * 16;
     const bool copy = tile.id < 0;
     if (copy && a.base == a.y && !a.no_base) return;
     for (int sub = 0; sub < tile.count; sub += most_tokens) {
@@ -836,25 +839,28 @@ template <typename X> int down(const AdapterArgs &a, hipStream_t stream)
     return (int)hipGetLastError();
 }
 
-template <typename Y, typename B, int N, int TT> void up_by(const AdapterArgs &a, unsigned blocks, size_t lds, hipStream_t stream)
+template <typename Y, typename B, int N, int TT, int J, bool FEW, bool SHORT> void up_with(const AdapterArgs &a, hipStream_t stream)
 {
-    if (a.rank <= 32) adapter_up_kernel<Y, B, N, TT, 1, false, false><<<blocks, kBlock, lds, stream>>>(a);
-    else if (a.rank <= 64) adapter_up_kernel<Y, B, N, TT, 2, false, false><<<blocks, kBlock, lds, stream>>>(a);
-    else if (a.rank <= 128) adapter_up_kernel<Y, B, N, TT, 4, false, false><<<blocks, kBlock, lds, stream>>>(a);
-    else adapter_up_kernel<Y, B, N, TT, 8, false, false><<<blocks, kBlock, lds, stream>>>(a);
+    const size_t lds = (size_t)2 * 16 * TT * row_of_t(a.rank) * sizeof(_Float16);         // (what the kernel keeps goes by its own TT)
+    adapter_up_kernel<Y, B, N, TT, J, FEW, SHORT><<<(unsigned)a.tiles_most * (unsigned)a.groups, kBlock, lds, stream>>>(a);
+}
+
+template <typename Y, typename B, int N, int TT> void up_by(const AdapterArgs &a, hipStream_t stream)
+{
+    if (a.rank < 8) up_with<Y, B, N, TT, 1, false, true>(a, stream);
+    else if (a.rank <= 32) up_with<Y, B, N, TT, 1, false, false>(a, stream);
+    else if (a.rank <= 64) up_with<Y, B, N, TT, 2, false, false>(a, stream);
+    else if (a.rank <= 128) up_with<Y, B, N, TT, 4, false, false>(a, stream);
+    else up_with<Y, B, N, TT, 8, false, false>(a, stream);
 }
 
 template <typename Y, typename B> void up(const AdapterArgs &a, hipStream_t stream)
 {
-    const unsigned blocks = (unsigned)a.tiles_most * (unsigned)a.groups;
-    const size_t lds = (size_t)2 * 16 * a.token_tiles * ((a.rank + 31) / 32 * 32 + 8) * sizeof(_Float16);
-    if (a.n < 2 || a.n * a.rank < 8) adapter_up_kernel<Y, B, 2, 1, 8, true, true><<<blocks, kBlock, lds, stream>>>(a);
-    else if (a.rank < 8 && a.wide == 2) adapter_up_kernel<Y, B, 2, 1, 1, false, true><<<blocks, kBlock, lds, stream>>>(a);
-    else if (a.rank < 8) adapter_up_kernel<Y, B, 4, 2, 1, false, true><<<blocks, kBlock, lds, stream>>>(a);
-    else if (a.wide == 2) up_by<Y, B, 2, 1>(a, blocks, lds, stream);
-    else if (a.token_tiles == 1) up_by<Y, B, 4, 1>(a, blocks, lds, stream);
-    else if (a.token_tiles == 2) up_by<Y, B, 4, 2>(a, blocks, lds, stream);
-    else adapter_up_kernel<Y, B, 4, 4, 2, false, false><<<blocks, kBlock, lds, stream>>>(a);
+    if (a.n < 2 || a.n * a.rank < 8) up_with<Y, B, 2, 1, 8, true, true>(a, stream);
+    else if (a.wide == 2) up_by<Y, B, 2, 1>(a, stream);
+    else if (a.token_tiles == 1) up_by<Y, B, 4, 1>(a, stream);
+    else if (a.token_tiles == 2) up_by<Y, B, 4, 2>(a, stream);
+    else up_with<Y, B, 4, 4, 2, false, false>(a, stream);
 }
 
 }  // namespace
