@@ -465,7 +465,7 @@ fq_status fq_dropout(const fq_dropout_args *d, void *hip_stream);
  * Products of FP16 values and codes are exact, those of FP32 tokens binary32; sums are binary32, in a fixed order.  t goes
  * into its products as two FP16 numbers: 22 bits of each, or 2^-39 of the greatest of a token's t.  y is rounded to its type
  * once.  Tokens come in any order; ids outside [0, count) mean no adapter (y = base).  A token's NaN or infinity stays in
- * its row, an adapter's with its tokens.
+ * its row, an adapter's with its tokens, one in b with its channel; what they give is infinite or NaN as the formula says.
  * Rows of x, base and y may lie any distance apart and at any address that their type allows; a and b are contiguous.
  * y may be exactly base (same type and distance).  Two launches, three with more than 4096 tokens and up to 1024 adapters;
  * so many per 65536 tokens.  The workspace need not be initialised and may be shared by calls that do not overlap in time.

@@ -276,7 +276,7 @@ __device__ __forceinline__ Tile find_tile(const AdapterArgs &a, int index, Findi
 
 // All loads are of whole vectors, and no lane branches round one (else each would be waited for before the next is asked for): a vector that
 // would go over the end of a row of N or more values begins N before it instead, and what it then has of the vector before counts as
-// zero in one of the two factors.  SHORT: rows of less, value by value.
+// zero: for t in both factors (an infinity in one would make the other's zero NaN), for y in t.  SHORT: rows of less, value by value.
 __device__ __forceinline__ int begin_of(int at, int n, int width) { return max(min(at, width - n), 0); }
 
 // N values, in the words that they are loaded in.  (As an array of values they would be taken apart into a register each.)
@@ -319,19 +319,6 @@ __device__ __forceinline__ f16x8 halves_of(int low, int high)
 template <typename X> struct Piece {
     Words<X, 16> p;
     template <bool SHORT> __device__ __forceinline__ void fetch(const X *row, int at, int k) { load<SHORT>(p, row, at, k); }
-    // only those from `first` to `last` count
-    __device__ __forceinline__ void keep(int first, int last)
-    {
-        constexpr int kEach = 4 / (int)sizeof(X), kBits = 8 * (int)sizeof(X);
-#pragma unroll
-        for (int d = 0; d < Words<X, 16>::kWords; ++d) {
-            unsigned mask = 0;
-#pragma unroll
-            for (int e = 0; e < kEach; ++e)
-                mask |= d * kEach + e >= first && d * kEach + e <= last ? (unsigned)((1ull << kBits) - 1) << (e * kBits) : 0u;
-            p.w[d] &= (int)mask;
-        }
-    }
     __device__ __forceinline__ f16x8 half(int i) const
     {
         if constexpr (sizeof(X) == 1) return halves_of(p.w[2 * i], p.w[2 * i + 1]);
@@ -339,6 +326,21 @@ template <typename X> struct Piece {
     }
     __device__ __forceinline__ X value(int e) const { return p.values()[e]; }
 };
+
+// Only the values from `first` to `last` of each piece count.
+template <typename X, int N> __device__ __forceinline__ void keep(Piece<X> (&pieces)[N], int first, int last)
+{
+    constexpr int kEach = 4 / (int)sizeof(X), kBits = 8 * (int)sizeof(X);
+#pragma unroll
+    for (int d = 0; d < Words<X, 16>::kWords; ++d) {
+        unsigned mask = 0;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e)
+            mask |= d * kEach + e >= first && d * kEach + e <= last ? (unsigned)((1ull << kBits) - 1) << (e * kBits) : 0u;
+#pragma unroll
+        for (int n = 0; n < N; ++n) pieces[n].p.w[d] &= (int)mask;
+    }
+}
 
 // The products of 64 values of k: a lane has 16 neighbouring ones of a token, and of a rank.
 template <typename X, int NT, int NR> __device__ __forceinline__ void multiply(f32x4 (&sum)[NT][NR], const Piece<X> (&x)[NT], const Piece<_Float16> (&w)[NR])
@@ -443,8 +445,8 @@ __global__ __launch_bounds__(kBlock, SHORT ? 2 : 4) void adapter_down_kernel(Ada
 #pragma unroll
             for (int r = 0; r < NR; ++r) w[r].template fetch<SHORT>(ranks[r], from, a.k);
             if (share.step(i) * kDepth + kDepth > a.k) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n) x[n].keep(at - from, a.k - 1 - from);
+                keep(x, at - from, a.k - 1 - from);
+                keep(w, at - from, a.k - 1 - from);
             }
             multiply<X, NT, NR>(sum, x, w);
         }
@@ -539,8 +541,8 @@ __global__ __launch_bounds__(kBlock) void adapter_down_ring_kernel(AdapterArgs a
             }
             if (share.step(i) * kDepth + kDepth > a.k) {           // (what lies behind a row's end is the next row's)
                 const int at = share.step(i) * kDepth + lane / 16 * 16;
-#pragma unroll
-                for (int n = 0; n < NT; ++n) x[n].keep(0, a.k - 1 - at);
+                keep(x, 0, a.k - 1 - at);
+                keep(w, 0, a.k - 1 - at);
             }
             multiply<X, NT, NR>(sum, x, w);
             loads_but<63>();                                       // (the reads of this slot are done)
@@ -560,7 +562,30 @@ __global__ __launch_bounds__(kBlock) void adapter_down_ring_kernel(AdapterArgs a
 // channels for the columns, the N products' columns N apart: lane l has N neighbouring channels of four tokens, and the 16 lanes of a token
 // have neighbouring ones, so a load or store is of runs of 32 N bytes.  (8192 x 8192 FP16 by 64 ranks: 69 us, 3.9 TB/s; 80 with lanes of one
 // instruction in 16 rows, 16 bytes each, whose addresses are looked up one by one.  Eight channels to a lane: as four.)
+//
+// Infinities.  One among a token's t has 0 for its second number, and e goes by the others.  In b one times 0 - t's second number where the first is all
+// of it, or a place of no rank - would be NaN where the formula has an infinity: a wavefront that finds one in its vectors of b (it looks once a strip,
+// which costs 0 to 3 % of a call) leaves that strip to plain_strip.  A NaN does no harm: y of its channel is NaN in any case.
 constexpr int kUpWaves = kBlock / 64;
+
+// Adds 0 times all values of v, which is NaN where one is not finite.
+template <int N> __device__ __forceinline__ void look_at(f16x2 &wild, const Words<_Float16, 8> (&v)[N])
+{
+#pragma unroll
+    for (int c = 0; c < N; ++c)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) wild = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, (int)v[c].w[w]), (f16x2)(_Float16)0.0f, wild);
+}
+
+template <int N> __device__ __forceinline__ bool has_infinity(const Words<_Float16, 8> (&v)[N])
+{
+    bool some = false;
+#pragma unroll
+    for (int c = 0; c < N; ++c)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) some |= (v[c].w[w] & 0x7FFF) == 0x7C00 || (v[c].w[w] >> 16 & 0x7FFF) == 0x7C00;
+    return some;
+}
 
 __device__ __forceinline__ f32x4 product(f16x8 t, f16x8 b, f32x4 sum) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(t, b, sum, 0, 0, 0); }
 
@@ -638,10 +663,33 @@ __device__ __forceinline__ int anew(int v)
 // Values from a row of t in LDS to the next: whole 32 ranks, and eight more so that rows begin in different banks.
 __host__ __device__ constexpr int row_of_t(int rank) { return (rank + 31) / 32 * 32 + 8; }
 
+// y of a strip by sums of binary32 products, one channel after the other: of the lane's N from `first` on, as elsewhere.  (Slow, but rare and
+// out of the way: by matrix instructions with masked vectors the kernel took 10 to 120 registers more.)
+template <typename Y, typename B, int N, int TT>
+__device__ __forceinline__ void plain_strip(const AdapterArgs &a, int id, const _Float16 *heads, int row, const float *factor, const int *tokens, int count,
+                                            int first)
+{
+    const _Float16 *const rests = heads + TT * 16 * row, *const b = (const _Float16 *)a.b + (long long)id * a.n * a.rank;
+#pragma unroll 1
+    for (int i = 0; i < TT * 4 * N; ++i) {
+        const int token = i / (4 * N) * 16 + (threadIdx.x & 63) / 16 * 4 + i / N % 4, c = first + i % N;
+        if (token >= count || c >= a.n) continue;
+        float sum = 0.0f;
+#pragma unroll 4
+        for (int l = 0; l < a.rank; ++l) {
+            const int at = token * row + place_of_rank(l, a.rank);
+            sum += ((float)heads[at] + (float)rests[at]) * (float)ld_global(b + (long long)c * a.rank + l);
+        }
+        const float v = a.no_base ? 0.0f : (float)ld_global((const B *)a.base + tokens[token] * a.ldbase + c);
+        st_global((Y *)a.y + tokens[token] * a.ldy + c, (Y)(v + factor[token] * sum));
+    }
+}
+
 // TT: tokens of a tile in 16s, at most; J: of t's units, 32 J ranks at most; SHORT: rows of b, fewer than eight ranks; FEW: channels, fewer
-// than N, or values of b of an adapter, fewer than eight.
+// than N, or values of b of an adapter, fewer than eight.  Wavefronts to a SIMD: as many as leave each its registers (32 tokens with an FP32 base, whose two
+// tiles are 32 of them: 2048 x 4096 x 4096 by 16 ranks 27.4 us with three, 29.6 with four).
 template <typename Y, typename B, int N, int TT, int J, bool FEW, bool SHORT>
-__global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ? 3 : N == 2 || J == 1 ? 4 : 3) void adapter_up_kernel(AdapterArgs a)
+__global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ? 3 : N == 2 || (J == 1 && (TT == 1 || sizeof(B) == 2)) ? 4 : 3) void adapter_up_kernel(AdapterArgs a)
 {
     constexpr int kHeld = J == 8 ? 1 : J;                             // vectors of b of a channel that are held: all, or one at a time
     constexpr int kAhead = TT > 1 ? 2 : 1;                            // tokens' tiles whose base is held
@@ -706,11 +754,14 @@ __global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ?
 #pragma unroll
                 for (int j = 0; j < J; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) most = __builtin_fmaxf(most, __builtin_fabsf(s[j][e]));
+                    for (int e = 0; e < 4; ++e) {
+                        const float size = __builtin_fabsf(s[j][e]);
+                        most = __builtin_fmaxf(most, size < __builtin_inff() ? size : 0.0f);
+                    }
                 most = __builtin_fmaxf(most, __shfl_xor(most, 1));
                 most = __builtin_fmaxf(most, __shfl_xor(most, 2));
                 most = __builtin_fmaxf(most, __shfl_xor(most, 4));
-                const int e2 = most > 0.0f && most < __builtin_inff() ? 15 - __builtin_amdgcn_frexp_expf(most) : 0;
+                const int e2 = most > 0.0f ? 15 - __builtin_amdgcn_frexp_expf(most) : 0;
                 _Float16 *const heads = shared + i * row, *const rests = heads + most_tokens * row;
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
@@ -745,6 +796,8 @@ __global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ?
         __syncthreads();
         while (strip * 16 * N < a.n) {
             const int after = strip + a.groups * kUpWaves;
+            f16x2 wild = (f16x2)(_Float16)0.0f;
+            int written = count;                                          // tokens whose y the matrix instructions make: all, or none
             f32x4 sums[J == 8 ? TT : 1][N];
             if (J == 8) {
 #pragma unroll
@@ -753,6 +806,7 @@ __global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ?
                     for (int c = 0; c < N; ++c) sums[n][c] = (f32x4)0.0f;
                 if (!copy) {
                     const auto multiply_all = [&](const Words<_Float16, 8> (&by)[N], int d) {
+                        look_at(wild, by);
 #pragma unroll
                         for (int n = 0; n < TT; ++n) {
                             const _Float16 *t = shared + (n * 16 + lane % 16) * row + lane / 16 * 8 + d * 32;
@@ -775,6 +829,20 @@ __global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ?
                 if (TT > 1 && J < 8) {
                     if (n + 1 < TT) ask_base(n + 1, strip);
                     else ask_base(0, after);
+                }
+                if (n == 0) {
+                    if (!copy && J < 8) {
+#pragma unroll
+                        for (int d = 0; d < kHeld; ++d) look_at(wild, b[d]);
+                    }
+                    if (__builtin_expect(__ballot(wild[0] != 0 || wild[1] != 0) != 0, 0)) {
+                        bool some = J == 8;                                   // (whose vectors are no longer there)
+                        if (J < 8) {
+#pragma unroll
+                            for (int d = 0; d < kHeld; ++d) some |= has_infinity(b[d]);
+                        }
+                        if (__ballot(some)) written = 0;
+                    }
                 }
                 f32x4 sum[N];
 #pragma unroll
@@ -800,9 +868,15 @@ __global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ?
                         const float v = a.no_base ? 0.0f : (float)from[e];
                         y[e] = (Y)(copy ? v : v + f * sum[e][i]);
                     }
-                    if (token < count) store_channels<Y, N>((Y *)a.y + tokens[anew(sub + token)] * a.ldy, first_of(strip), a.n, y);
+                    if (token < written) store_channels<Y, N>((Y *)a.y + tokens[anew(sub + token)] * a.ldy, first_of(strip), a.n, y);
                 }
                 if (TT == 1 || J == 8) ask_base(n, after);
+            }
+            if (__builtin_expect(written == 0, 0)) {
+                plain_strip<Y, B, N, TT>(a, tile.id, shared, row, factor, tokens + sub, count, first_of(strip));
+#pragma unroll
+                for (int n = 0; n < kAhead; ++n)
+                    if (n == 0 || J == 8) ask_base(n, after);
             }
             strip = after;
             if (!copy && J < 8) ask_b(strip);
