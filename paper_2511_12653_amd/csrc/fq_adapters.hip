@@ -663,10 +663,27 @@ __device__ __forceinline__ int anew(int v)
 // Values from a row of t in LDS to the next: whole 32 ranks, and eight more so that rows begin in different banks.
 __host__ __device__ constexpr int row_of_t(int rank) { return (rank + 31) / 32 * 32 + 8; }
 
+// scale xs 2^-e of a token: a number, and a power of two that its finished sums are multiplied by.  By itself the product may be beyond binary32's range
+// where y is not (t of 2^-120 and b of 2^15); as a rule it is well within, and the power is 2^0.  Tiles with another go to plain_strip (to multiply all
+// sums by a power made 8192^3 by 64 ranks 2 % slower).
+struct Factors {
+    float number[kWindow];
+    int power[kWindow];
+};
+
+__device__ __forceinline__ void set_factor(Factors &to, int i, float scale, float xs, int e)
+{
+    const float number = __builtin_amdgcn_frexp_mantf(scale) * __builtin_amdgcn_frexp_mantf(xs);
+    const int power = __builtin_amdgcn_frexp_expf(scale) + __builtin_amdgcn_frexp_expf(xs) - e;
+    const bool within = power >= -100 && power <= 100;
+    to.number[i] = within ? __builtin_ldexpf(number, power) : number;
+    to.power[i] = within ? 0 : power;
+}
+
 // y of a strip by sums of binary32 products, one channel after the other: of the lane's N from `first` on, as elsewhere.  (Slow, but rare and
 // out of the way: by matrix instructions with masked vectors the kernel took 10 to 120 registers more.)
 template <typename Y, typename B, int N, int TT>
-__device__ __forceinline__ void plain_strip(const AdapterArgs &a, int id, const _Float16 *heads, int row, const float *factor, const int *tokens, int count,
+__device__ __forceinline__ void plain_strip(const AdapterArgs &a, int id, const _Float16 *heads, int row, const Factors &factors, const int *tokens, int count,
                                             int first)
 {
     const _Float16 *const rests = heads + TT * 16 * row, *const b = (const _Float16 *)a.b + (long long)id * a.n * a.rank;
@@ -681,7 +698,7 @@ __device__ __forceinline__ void plain_strip(const AdapterArgs &a, int id, const 
             sum += ((float)heads[at] + (float)rests[at]) * (float)ld_global(b + (long long)c * a.rank + l);
         }
         const float v = a.no_base ? 0.0f : (float)ld_global((const B *)a.base + tokens[token] * a.ldbase + c);
-        st_global((Y *)a.y + tokens[token] * a.ldy + c, (Y)(v + factor[token] * sum));
+        st_global((Y *)a.y + tokens[token] * a.ldy + c, (Y)(v + __builtin_ldexpf(factors.number[token] * sum, factors.power[token])));
     }
 }
 
@@ -695,7 +712,7 @@ __global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ?
     constexpr int kAhead = TT > 1 ? 2 : 1;                            // tokens' tiles whose base is held
     extern __shared__ __attribute__((aligned(16))) _Float16 shared[];          // [2][tile][row]
     __shared__ Finding finding;
-    __shared__ float factor[kWindow];
+    __shared__ Factors factors;
     const int *tokens = finding.tokens;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int index = (int)(blockIdx.x / a.groups);
@@ -787,17 +804,16 @@ __global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ?
                         }
                     }
                 }
-                if (unit == 0) {
-                    const float f = (a.scale ? ld_global(a.scale + tile.id) : 1.0f) * (a.xs ? ld_global(a.xs + (long long)token * a.xs_step) : 1.0f);
-                    factor[i] = __builtin_ldexpf(f, -e2);
-                }
+                if (unit == 0)
+                    set_factor(factors, i, a.scale ? ld_global(a.scale + tile.id) : 1.0f, a.xs ? ld_global(a.xs + (long long)token * a.xs_step) : 1.0f, e2);
             }
         }
         __syncthreads();
+        const bool far = !copy && __ballot(factors.power[lane % most_tokens] != 0) != 0;
         while (strip * 16 * N < a.n) {
             const int after = strip + a.groups * kUpWaves;
             f16x2 wild = (f16x2)(_Float16)0.0f;
-            int written = count;                                          // tokens whose y the matrix instructions make: all, or none
+            bool matrix = !far;                                           // whether the matrix instructions make the y of this strip
             f32x4 sums[J == 8 ? TT : 1][N];
             if (J == 8) {
 #pragma unroll
@@ -841,7 +857,7 @@ __global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ?
 #pragma unroll
                             for (int d = 0; d < kHeld; ++d) some |= has_infinity(b[d]);
                         }
-                        if (__ballot(some)) written = 0;
+                        if (__ballot(some)) matrix = false;
                     }
                 }
                 f32x4 sum[N];
@@ -860,7 +876,7 @@ __global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ?
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int token = n * 16 + lane / 16 * 4 + i;
-                    const float f = copy ? 0.0f : factor[token];
+                    const float f = copy ? 0.0f : factors.number[token];
                     const auto from = base[n % kAhead][i].values();
                     typename Words<Y, N>::V y;
 #pragma unroll
@@ -868,12 +884,12 @@ __global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ?
                         const float v = a.no_base ? 0.0f : (float)from[e];
                         y[e] = (Y)(copy ? v : v + f * sum[e][i]);
                     }
-                    if (token < written) store_channels<Y, N>((Y *)a.y + tokens[anew(sub + token)] * a.ldy, first_of(strip), a.n, y);
+                    if (token < count && matrix) store_channels<Y, N>((Y *)a.y + tokens[anew(sub + token)] * a.ldy, first_of(strip), a.n, y);
                 }
                 if (TT == 1 || J == 8) ask_base(n, after);
             }
-            if (__builtin_expect(written == 0, 0)) {
-                plain_strip<Y, B, N, TT>(a, tile.id, shared, row, factor, tokens + sub, count, first_of(strip));
+            if (__builtin_expect(!matrix, 0)) {
+                plain_strip<Y, B, N, TT>(a, tile.id, shared, row, factors, tokens + sub, count, first_of(strip));
 #pragma unroll
                 for (int n = 0; n < kAhead; ++n)
                     if (n == 0 || J == 8) ask_base(n, after);
