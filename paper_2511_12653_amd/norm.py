@@ -36,7 +36,7 @@ class _LayerNorm(torch.autograd.Function):
         width = x.shape[-1]
         x2 = _rows(x, width)
         y = torch.empty(x.shape, dtype=out_dtype or x.dtype, device=x.device)
-        stats = torch.empty((x2.shape[0], 2), device=x.device) if any(ctx.needs_input_grad) else None
+        stats = torch.empty((x2.shape[0], 2), dtype=torch.float32, device=x.device) if any(ctx.needs_input_grad) else None
         with torch.cuda.device(x.device):
             fq.fq_norm_forward(fq.FqNorm.from_torch(
                 x2, y=y.view(x2.shape), weight=None if weight is None else weight.contiguous(),
@@ -89,7 +89,7 @@ def layer_norm_int8(x, weight=None, bias=None, eps=1e-5):
     _check(x, weight, bias)
     x2 = _rows(x, x.shape[-1])
     codes = torch.empty(x.shape, dtype=torch.int8, device=x.device)
-    scales = torch.empty(x.shape[:-1], device=x.device)
+    scales = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     with torch.cuda.device(x.device):
         fq.fq_norm_forward(fq.FqNorm.from_torch(
             x2, y=codes.view(x2.shape), weight=None if weight is None else weight.contiguous(),

@@ -96,10 +96,10 @@ class AdamW(torch.optim.Optimizer):
             blocks = (p.numel() + 255) // 256
             for name in ("m", "v"):
                 state[name] = torch.zeros(p.shape, dtype=torch.float8_e4m3fn, device=p.device)
-                state[name + "_scale"] = torch.zeros(blocks, device=p.device)
+                state[name + "_scale"] = torch.zeros(blocks, dtype=torch.float32, device=p.device)
         else:
             for name in ("m", "v"):
-                state[name] = torch.zeros(p.shape, device=p.device)
+                state[name] = torch.zeros(p.shape, dtype=torch.float32, device=p.device)
 
     def _launches(self, index, group, grad_scale, made):
         """A launch for the parameters with a gradient, or, where some had their first one late, for those of each step number:
