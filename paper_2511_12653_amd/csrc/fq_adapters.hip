@@ -673,11 +673,29 @@ struct Factors {
 
 __device__ __forceinline__ void set_factor(Factors &to, int i, float scale, float xs, int e)
 {
-    const float number = __builtin_amdgcn_frexp_mantf(scale) * __builtin_amdgcn_frexp_mantf(xs);
-    const int power = __builtin_amdgcn_frexp_expf(scale) + __builtin_amdgcn_frexp_expf(xs) - e;
-    const bool within = power >= -100 && power <= 100;
-    to.number[i] = within ? __builtin_ldexpf(number, power) : number;
-    to.power[i] = within ? 0 : power;
+    float number = scale * xs;
+    const bool fits = __builtin_isnormal(number);
+    number = __builtin_ldexpf(number, -e);
+    int power = 0;
+    if (__builtin_expect(!fits || !__builtin_isnormal(number), 0)) {
+        number = __builtin_amdgcn_frexp_mantf(scale) * __builtin_amdgcn_frexp_mantf(xs);
+        power = __builtin_amdgcn_frexp_expf(scale) + __builtin_amdgcn_frexp_expf(xs) - e;
+        if (power >= -100 && power <= 100) {
+            number = __builtin_ldexpf(number, power);
+            power = 0;
+        }
+    }
+    to.number[i] = number;
+    to.power[i] = power;
+}
+
+// The greatest of the eight lanes that have a token's t, none of them negative or NaN.
+__device__ __forceinline__ float most_of_token(float most)
+{
+    unsigned v = __builtin_bit_cast(unsigned, most);
+    v = dpp_max<0xB1, 0xf>(v);
+    v = dpp_max<0x4E, 0xf>(v);
+    return __builtin_bit_cast(float, dpp_max<0x141, 0xf>(v));
 }
 
 // y of a strip by sums of binary32 products, one channel after the other: of the lane's N from `first` on, as elsewhere.  (Slow, but rare and
@@ -765,19 +783,26 @@ __global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ?
             const int unit = threadIdx.x % 8;
             for (int i = threadIdx.x / 8; i < most_tokens; i += kBlock / 8) {
                 const int token = tokens[sub + min(i, count - 1)];
+                const float scale = a.scale ? ld_global(a.scale + tile.id) : 1.0f, xs = a.xs ? ld_global(a.xs + (long long)token * a.xs_step) : 1.0f;
                 f32x4 s[J];
                 sum_of_parts<J>(s, a, a.t + (long long)token * a.pitch, unit);
                 float most = 0.0f;
 #pragma unroll
                 for (int j = 0; j < J; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float size = __builtin_fabsf(s[j][e]);
-                        most = __builtin_fmaxf(most, size < __builtin_inff() ? size : 0.0f);
-                    }
-                most = __builtin_fmaxf(most, __shfl_xor(most, 1));
-                most = __builtin_fmaxf(most, __shfl_xor(most, 2));
-                most = __builtin_fmaxf(most, __shfl_xor(most, 4));
+                    for (int e = 0; e < 4; ++e) most = __builtin_fmaxf(most, __builtin_fabsf(s[j][e]));
+                most = most_of_token(most);
+                if (__builtin_expect(most == __builtin_inff(), 0)) {            // (of all eight lanes of a token, or of none)
+                    most = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < J; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float size = __builtin_fabsf(s[j][e]);
+                            most = __builtin_fmaxf(most, size < __builtin_inff() ? size : 0.0f);
+                        }
+                    most = most_of_token(most);
+                }
                 const int e2 = most > 0.0f ? 15 - __builtin_amdgcn_frexp_expf(most) : 0;
                 _Float16 *const heads = shared + i * row, *const rests = heads + most_tokens * row;
 #pragma unroll
@@ -804,16 +829,14 @@ __global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ?
                         }
                     }
                 }
-                if (unit == 0)
-                    set_factor(factors, i, a.scale ? ld_global(a.scale + tile.id) : 1.0f, a.xs ? ld_global(a.xs + (long long)token * a.xs_step) : 1.0f, e2);
+                if (unit == 0) set_factor(factors, i, scale, xs, e2);
             }
         }
         __syncthreads();
-        const bool far = !copy && __ballot(factors.power[lane % most_tokens] != 0) != 0;
         while (strip * 16 * N < a.n) {
             const int after = strip + a.groups * kUpWaves;
             f16x2 wild = (f16x2)(_Float16)0.0f;
-            bool matrix = !far;                                           // whether the matrix instructions make the y of this strip
+            bool matrix = true;                                           // whether the matrix instructions make the y of this strip
             f32x4 sums[J == 8 ? TT : 1][N];
             if (J == 8) {
 #pragma unroll
@@ -846,20 +869,6 @@ __global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ?
                     if (n + 1 < TT) ask_base(n + 1, strip);
                     else ask_base(0, after);
                 }
-                if (n == 0) {
-                    if (!copy && J < 8) {
-#pragma unroll
-                        for (int d = 0; d < kHeld; ++d) look_at(wild, b[d]);
-                    }
-                    if (__builtin_expect(__ballot(wild[0] != 0 || wild[1] != 0) != 0, 0)) {
-                        bool some = J == 8;                                   // (whose vectors are no longer there)
-                        if (J < 8) {
-#pragma unroll
-                            for (int d = 0; d < kHeld; ++d) some |= has_infinity(b[d]);
-                        }
-                        if (__ballot(some)) matrix = false;
-                    }
-                }
                 f32x4 sum[N];
 #pragma unroll
                 for (int c = 0; c < N; ++c) sum[c] = J == 8 ? sums[J == 8 ? n : 0][c] : (f32x4)0.0f;
@@ -871,6 +880,21 @@ __global__ __launch_bounds__(kBlock, J == 8 || (J == 4 && N == 4) ? 2 : J == 4 ?
                         const f16x8 high = *(const f16x8 *)(t + d * 32), low = *(const f16x8 *)(t + d * 32 + most_tokens * row);
 #pragma unroll
                         for (int c = 0; c < N; ++c) sum[c] = product(low, b[d][c].values(), product(high, b[d][c].values(), sum[c]));
+                    }
+                }
+                if (n == 0) {
+                    if (!copy && J < 8) {
+#pragma unroll
+                        for (int d = 0; d < kHeld; ++d) look_at(wild, b[d]);
+                    }
+                    const int power = copy ? 0 : factors.power[lane % most_tokens];
+                    if (__builtin_expect(__ballot(wild[0] != 0 || wild[1] != 0 || power != 0) != 0, 0)) {
+                        bool some = J == 8 || power != 0;                     // (the vectors of J == 8 are no longer there)
+                        if (J < 8) {
+#pragma unroll
+                            for (int d = 0; d < kHeld; ++d) some |= has_infinity(b[d]);
+                        }
+                        if (__ballot(some)) matrix = false;
                     }
                 }
 #pragma unroll
