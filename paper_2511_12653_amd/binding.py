@@ -208,6 +208,20 @@ class FqAdamW(ctypes.Structure):
         self._keep = grad_scale
 
 
+def _pitch(t):
+    """From a row of a matrix to the next, in elements."""
+    rows, cols = t.shape
+    if rows == 0 or cols == 0:           # (whose strides may be anything, and stay so in a contiguous copy)
+        return cols
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("the values of a row must be contiguous")
+    if rows <= 1:
+        return cols
+    if t.stride(0) < cols:
+        raise ValueError("rows must not overlap")
+    return t.stride(0)
+
+
 class FqLinear(ctypes.Structure):
     """Mirror of `struct fq_linear` (host struct; the pointers inside are device pointers)."""
     _fields_ = [("m", ctypes.c_int64), ("n", ctypes.c_int64), ("k", ctypes.c_int64),
@@ -241,35 +255,13 @@ class FqLinear(ctypes.Structure):
                 raise ValueError("%s has %d values, want %d" % (name, t.numel(), count))
         _device_of((x, w, w_scale, y, bias, x_scale))
 
-        def pitch(t):
-            rows, cols = t.shape
-            if cols > 1 and t.stride(1) != 1:
-                raise ValueError("the values of a row must be contiguous")
-            if rows <= 1:
-                return cols
-            if t.stride(0) < cols:
-                raise ValueError("rows must not overlap")
-            return t.stride(0)
-
         ptr = lambda t: None if t is None else t.data_ptr()
-        self = cls(m, n, k, x_types[x.dtype], FQ_F16 if y.dtype == torch.float16 else FQ_F32, pitch(x), pitch(w), pitch(y),
+        self = cls(m, n, k, x_types[x.dtype], FQ_F16 if y.dtype == torch.float16 else FQ_F32, _pitch(x), _pitch(w), _pitch(y),
                    ptr(x), ptr(x_scale), ptr(w), ptr(w_scale), ptr(bias), ptr(y),
                    0 if x_scale is None or (x_scale.numel() == 1 and m != 1) else 1,
                    0 if w_scale.numel() == 1 and n != 1 else 1)
         self._keep = (x, w, w_scale, y, bias, x_scale)
         return self
-
-
-def _pitch(t):
-    """From a row of a matrix to the next, in elements."""
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
-        raise ValueError("the values of a row must be contiguous")
-    if rows <= 1:
-        return cols
-    if t.stride(0) < cols:
-        raise ValueError("rows must not overlap")
-    return t.stride(0)
 
 
 def _pointer(t):
