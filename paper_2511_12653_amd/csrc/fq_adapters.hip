@@ -3,8 +3,9 @@
 //   t = x a^T,   y = base + (xs scale) t b^T      a, b: those of the token's adapter
 //
 // Two steps, since all of t is needed for any y: adapter_down_kernel makes t, in parts of k where there are few tiles, and
-// adapter_up_kernel adds them up and makes y.  Both work on tiles of up to 16 (64) tokens of one adapter, whose rows they pick out
-// by a list: with up to 64 tokens a wavefront finds those of one adapter by itself; with more, adapter_group_kernel orders them first.
+// adapter_up_kernel adds them up and makes y.  Both work on tiles of 16, 32 or 64 tokens of one adapter, whose rows they pick out by a
+// list.  Up to 64 tokens, and any number for more than 1024 adapters, go in windows of 64, in which a wavefront finds those of an adapter by itself;
+// up to 4096 are sorted by the first kernel's blocks, which leave the second what they have found; more are ordered by adapter_group_kernel first.
 // Products go to the matrix cores.  Bound by memory (x, base and y once each: few operations to a byte, 2 rank of them) and, for few tokens,
 // by the launches.
 #include <type_traits>
